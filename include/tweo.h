@@ -1,7 +1,8 @@
 /*
  * tweo.h - C ABI of the MI355X (gfx950) library for the per-tensor FP8 linear
  * layer with the fused TWEO activation-outlier penalty, and for the W8A8
- * per-tensor static INT8 linear layer (TWEO, arXiv 2511.23225).
+ * per-tensor static INT8 linear layer (TWEO, arXiv 2511.23225), with what a training
+ * step needs around the linears: LayerNorm's gradients, the gradients' norm, AdamW.
  *
  * Conventions that hold for every entry point
  *   - Every data pointer is a DEVICE pointer owned by the caller; the library
@@ -53,7 +54,9 @@ enum {
     TWEO_OP_W8A8_LINEAR = 2,
     TWEO_OP_FP8_LINEAR_FWD_BF16 = 3,
     TWEO_OP_FP8_LINEAR_BWD_BF16 = 4,
-    TWEO_OP_LAYERNORM_QUANTIZE = 5 /* M = rows; N, K unused (pass 1) */
+    TWEO_OP_LAYERNORM_QUANTIZE = 5, /* M = rows; N, K unused (pass 1) */
+    TWEO_OP_LAYERNORM_BWD = 6,      /* M = rows, N = cols; K unused (pass 1) */
+    TWEO_OP_GRAD_SUMSQ = 7          /* the same for every table (pass 1, 1, 1) */
 };
 
 /* Bytes of device workspace the given operation can use for these sizes (a
@@ -201,6 +204,52 @@ tweo_status tweo_layernorm_quantize_e4m3_delayed(const void *x_bf16, const void 
                                                  int bootstrap, void *h_out_bf16, void *y_out_bf16,
                                                  uint8_t *q, uint8_t *qT, void *workspace,
                                                  size_t workspace_bytes, void *stream);
+
+/*
+ * LayerNorm to bf16 without a cast: in front of what is not an FP8 linear (a bf16
+ * head, attention), and for one token as for many.
+ *   h[r,c] = x[r,c]            or, with a residual, bf16( x[r,c] + residual[r,c] )
+ *   y[r,c] = bf16( (h[r,c] - mu_r) / sqrt(var_r + eps) * gamma[c] + beta[c] )
+ * mu and the biased var as in tweo_layernorm_quantize_e4m3; fp64, one rounding: y is
+ * bit for bit what that call's y_out is.
+ *   x_bf16, y_bf16 [rows, cols], any rows >= 1 and cols >= 1 (cols that are no multiple
+ *   of 8 start their rows at odd places and run slower).
+ *   residual_bf16 [rows, cols] or NULL; with it h_out_bf16 is required, without it
+ *   ignored.  h_out may be x or the residual, y may be x, the residual without h_out
+ *   being it (each exactly, in place); y and h_out differ, nothing else may overlap.
+ *   gamma_bf16 [cols]; beta_bf16 [cols] or NULL (= 0); eps >= 0.
+ *   stats_out NULL or fp64 [rows][2]: (mu, 1 / sqrt(var + eps)), as the LayerNorm -> cast
+ *   calls leave them in their workspace from byte 2304 on.
+ * Needs no workspace.  Errors: TWEO_ERR_INVALID_ARG (null, misaligned, negative or NaN
+ * eps, residual without h_out, h_out == y), TWEO_ERR_UNSUPPORTED (rows above 2^30 or
+ * cols above 2^24).
+ */
+tweo_status tweo_layernorm_fwd(const void *x_bf16, const void *residual_bf16, const void *gamma_bf16,
+                               const void *beta_bf16, int64_t rows, int64_t cols, float eps,
+                               void *h_out_bf16, void *y_bf16, double *stats_out, void *stream);
+
+/*
+ * Gradients of a LayerNorm, whichever call computed it.  With xhat = (h - mu) * rstd:
+ *   w       = dy * gamma
+ *   dx      = bf16( rstd * (w - mean_c(w) - xhat * mean_c(w * xhat)) + residual_grad )
+ *   dgamma  = sum_r dy * xhat,   dbeta = sum_r dy        (fp32, overwritten)
+ * fp32 arithmetic (h - mu to fp32's precision also where mu is far above the row's
+ * deviation), the column sums in a fixed order, no atomics.
+ *   dy_bf16, h_bf16, dx_bf16 [rows, cols]; h: what the norm normalised (with a residual
+ *   its h_out).  residual_grad_bf16 [rows, cols] or NULL: the gradient that reaches h
+ *   past the norm (the residual stream's), added before the one rounding.  dx may be dy
+ *   or residual_grad (exactly, in place), else nothing overlaps.
+ *   stats: fp64 [rows][2] from tweo_layernorm_fwd, or bytes 2304 and on of the workspace
+ *   after tweo_layernorm_quantize_e4m3 / _delayed.
+ *   gamma_bf16 [cols]; dgamma fp32 [cols]; dbeta fp32 [cols] or NULL.
+ *   workspace: tweo_workspace_bytes(TWEO_OP_LAYERNORM_BWD, rows, cols, 1).
+ * Errors: TWEO_ERR_INVALID_ARG (null, misaligned), TWEO_ERR_UNSUPPORTED (as above),
+ * TWEO_ERR_WORKSPACE.
+ */
+tweo_status tweo_layernorm_bwd(const void *dy_bf16, const void *h_bf16, const void *gamma_bf16,
+                               const double *stats, const void *residual_grad_bf16, int64_t rows,
+                               int64_t cols, void *dx_bf16, float *dgamma, float *dbeta, void *workspace,
+                               size_t workspace_bytes, void *stream);
 
 /*
  * FP8 linear forward with the TWEO penalty fused into the epilogue
@@ -494,6 +543,115 @@ tweo_status tweo_amax_quantize_f8(const void *x_bf16, int64_t rows, int64_t cols
  */
 tweo_status tweo_set_fused_cast(int on);
 tweo_status tweo_fused_cast_timeouts(unsigned *count);
+
+/*
+ * The tensors that an optimizer step goes over, described once: a table in device
+ * memory, read by the two calls below, which take one launch (the norm: two) for all
+ * tensors together.
+ *   param  the parameter, bf16 or fp32 (param_f32), updated in place
+ *   master fp32 copy of a bf16 parameter, or NULL.  With it the step reads and updates
+ *          the copy and stores its rounding to `param`; without it a bf16 parameter takes
+ *          its update by rounding, and what is below half a bf16 step (2^-9 of the
+ *          value) is lost.
+ *   grad   bf16 or fp32 (grad_f32): the weight gradients of the FP8 linears are bf16,
+ *          dgamma and dbeta above fp32
+ *   m, v   first and second moment: fp32 [n], or 8-bit codes [n] with
+ *   m_step, v_step: one fp32 for each 256 elements (the last may be short), the factor
+ *          of its codes: m = E4M3 code * m_step, v = E5M2 code * v_step.  All tensors of a table have 8-bit
+ *          states, or all fp32 ones (both steps NULL).  Zeros everywhere are the state before the first step.
+ *   n      elements, 1 .. 2^40;  weight_decay >= 0
+ * A table for the norm alone has grad and n, and NULL for param, master, m, v, m_step, v_step.
+ * Buffers that a step writes overlap no other buffer of the table.
+ */
+typedef struct {
+    void *param;
+    float *master;
+    const void *grad;
+    void *m;
+    void *v;
+    float *m_step;
+    float *v_step;
+    int64_t n;
+    float weight_decay;
+    int param_f32;
+    int grad_f32;
+} tweo_optim_tensor;
+
+/* Filled by tweo_optim_plan_init, read only. */
+typedef struct {
+    const void *table;
+    int64_t chunks;
+    int count;
+    int state_bits; /* 32, 8, or 0: gradients alone */
+} tweo_optim_plan;
+
+/* Bytes of device memory for the table of `count` tensors. */
+size_t tweo_optim_table_bytes(int count);
+
+/*
+ * Checks `tensors` (host array of `count`, 1 .. 65536; not needed after the call), writes
+ * the table (device memory, 16-byte aligned, at least tweo_optim_table_bytes(count) bytes,
+ * overlapping none of the buffers) on `stream` and fills *plan.  Table and buffers stay
+ * where they are as long as the plan is used; another call rewrites the table when buffers move.
+ * Errors: TWEO_ERR_INVALID_ARG (null, misaligned, overlapping buffers, a flag other than
+ * 0 / 1, a master of an fp32 parameter, one step without the other, tables of mixed
+ * states, negative, infinite or NaN weight_decay), TWEO_ERR_UNSUPPORTED (count or n out of range),
+ * TWEO_ERR_WORKSPACE (table_bytes).
+ */
+tweo_status tweo_optim_plan_init(const tweo_optim_tensor *tensors, int count, void *table, size_t table_bytes,
+                                 tweo_optim_plan *plan, void *stream);
+
+/*
+ * Sum of the squares of all gradients of a table, in fp64 (fp64 products, fixed order).  The sum
+ * and not the norm: shards add theirs exactly, and tweo_adamw_step takes it as it is.  A gradient that
+ * is not finite makes it infinite or NaN.
+ *   sumsq_out one fp64 on the device.   workspace: tweo_workspace_bytes(TWEO_OP_GRAD_SUMSQ, 1, 1, 1).
+ * Errors: TWEO_ERR_INVALID_ARG, TWEO_ERR_WORKSPACE.
+ */
+tweo_status tweo_grad_sumsq(const tweo_optim_plan *plan, double *sumsq_out, void *workspace,
+                            size_t workspace_bytes, void *stream);
+
+/* Two words in device memory that take the place of tweo_adamw_cfg's lr and step when the kernel runs: a captured step
+ * is replayed with what they then hold. */
+typedef struct {
+    float lr;
+    uint32_t step;
+} tweo_adamw_schedule;
+
+/* doubles: 1 - beta of a beta that has gone through fp32 is off by 5e-5 at 0.999 */
+typedef struct {
+    double lr;       /* >= 0 */
+    double beta1;    /* 0 <= beta < 1 */
+    double beta2;
+    double eps;      /* >= 0 */
+    double max_norm; /* > 0; used with grad_sumsq */
+    int64_t step;    /* t of this step, 1 .. 2^32 - 1 */
+} tweo_adamw_cfg;
+
+/*
+ * One AdamW step on all tensors of a table:
+ *   g = clip * grad,  clip = min(1, max_norm / (sqrt(*grad_sumsq) + 1e-6)), 1 without grad_sumsq
+ *   m = beta1 * m + (1 - beta1) * g,   v = beta2 * v + (1 - beta2) * g^2
+ *   p = p - lr * weight_decay * p - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in fp32.  If *grad_sumsq is not finite nothing is changed (one bad gradient must not reach every
+ * parameter through the clip): the caller sees it there, and decides whether t counts the step.
+ * 8-bit states: p takes the moments before they are rounded to codes.  Of a block of 256 elements
+ *   scale = 448 / max|m| (E4M3) or 57344 / max v (E5M2), guards as tweo_quantize_e4m3;  step = 1 / scale
+ *   code  = the magnitude's code at or below |m| * scale, or the next one if what is cut off, as
+ *           a fraction of the distance to it, plus u is at least 1
+ *   u     = top 20 (E4M3) or 21 (E5M2) bits of ( i * 0x6A09E667 + t * 0x9E3779B9 mod 2^32 ) as a fraction,
+ *           i the element's index in its tensor
+ * v moves by less than half a code step at a time, and rounded to nearest it would stay where it is; u runs evenly over
+ * [0, 1) with t and with i.  Over 300 steps at beta2 = 0.99 the coded v is 1.5 % below the fp32 one on average with a
+ * spread of 25 % (12 % of its root); to nearest 23 % above with 35 %.  A positive v never becomes 0.  An infinity or NaN in a block makes its step NaN and the
+ * block NaN from then on.
+ *   grad_sumsq: one fp64 on the device, or NULL.  schedule: device memory, or NULL; with it lr and step of cfg are not
+ *   used (a step of 0 there gives NaN or infinite parameters).
+ * A plan's calls must not overlap in time with each other, on whatever streams.
+ * Errors: TWEO_ERR_INVALID_ARG (null, cfg out of range, a plan for gradients alone).
+ */
+tweo_status tweo_adamw_step(const tweo_optim_plan *plan, const tweo_adamw_cfg *cfg, const double *grad_sumsq,
+                            const tweo_adamw_schedule *schedule, void *stream);
 
 /*
  * Tuning hook for benchmarks and tests: forces the GEMM kernel variant.

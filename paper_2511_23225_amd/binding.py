@@ -15,7 +15,7 @@ LIB_PATH = os.path.join(_PKG, "libtweo_hip.so")
 
 TWEO_OK, TWEO_ERR_INVALID_ARG, TWEO_ERR_UNSUPPORTED, TWEO_ERR_WORKSPACE, TWEO_ERR_HIP = range(5)
 (TWEO_OP_FP8_LINEAR_FWD, TWEO_OP_FP8_LINEAR_BWD, TWEO_OP_W8A8_LINEAR, TWEO_OP_FP8_LINEAR_FWD_BF16,
- TWEO_OP_FP8_LINEAR_BWD_BF16, TWEO_OP_LAYERNORM_QUANTIZE) = range(6)
+ TWEO_OP_FP8_LINEAR_BWD_BF16, TWEO_OP_LAYERNORM_QUANTIZE, TWEO_OP_LAYERNORM_BWD, TWEO_OP_GRAD_SUMSQ) = range(8)
 
 EXPORTS = ("tweo_workspace_bytes", "tweo_status_string", "tweo_amax", "tweo_quantize_e4m3",
            "tweo_fp8_linear_fwd", "tweo_fp8_linear_bwd", "tweo_quantize_i8", "tweo_w8a8_linear",
@@ -28,7 +28,9 @@ EXPORTS = ("tweo_workspace_bytes", "tweo_status_string", "tweo_amax", "tweo_quan
            "tweo_quantize_e5m2_delayed", "tweo_fp8_linear_bwd_bf16_inject",
            "tweo_fp8_linear_fwd_static", "tweo_static_scratch_bytes",
            "tweo_layernorm_quantize_e4m3", "tweo_layernorm_quantize_e4m3_delayed",
-           "tweo_fp8_linear_fwd_bf16_delayed", "tweo_fp8_linear_bwd_bf16_delayed")
+           "tweo_fp8_linear_fwd_bf16_delayed", "tweo_fp8_linear_bwd_bf16_delayed",
+           "tweo_layernorm_fwd", "tweo_layernorm_bwd", "tweo_optim_table_bytes", "tweo_optim_plan_init",
+           "tweo_grad_sumsq", "tweo_adamw_step")
 
 
 class TweoError(RuntimeError):
@@ -48,6 +50,19 @@ class GemmPlan(ctypes.Structure):
 class Fp8Saved(ctypes.Structure):
     _fields_ = [("xq", ctypes.c_void_p), ("xqT", ctypes.c_void_p), ("wq", ctypes.c_void_p),
                 ("wqT", ctypes.c_void_p), ("scalars", ctypes.c_void_p)]
+
+
+class OptimTensor(ctypes.Structure):
+    _fields_ = ([(k, ctypes.c_void_p) for k in ("param", "master", "grad", "m", "v", "m_step", "v_step")] +
+                [("n", ctypes.c_int64), ("weight_decay", ctypes.c_float), ("param_f32", ctypes.c_int), ("grad_f32", ctypes.c_int)])
+
+
+class OptimPlan(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("chunks", ctypes.c_int64), ("count", ctypes.c_int), ("state_bits", ctypes.c_int)]
+
+
+class AdamwCfg(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_double) for k in ("lr", "beta1", "beta2", "eps", "max_norm")] + [("step", ctypes.c_int64)]
 
 
 _lib = None
@@ -111,9 +126,16 @@ def load():
     L.tweo_quantize_e4m3_delayed.argtypes = [vp, i64, i64, vp, ctypes.c_int, vp, vp, vp]
     L.tweo_quantize_e5m2_delayed.argtypes = [vp, i64, i64, vp, ctypes.c_int, vp, vp, vp]
     L.tweo_penalty_grad_inject.argtypes = [vp, vp, i64, ctypes.POINTER(PenaltyCfg), ctypes.c_float, vp, vp]
+    L.tweo_layernorm_fwd.argtypes = [vp, vp, vp, vp, i64, i64, f32, vp, vp, vp, vp]
+    L.tweo_layernorm_bwd.argtypes = [vp, vp, vp, vp, vp, i64, i64, vp, vp, vp, vp, sz, vp]
+    L.tweo_optim_table_bytes.argtypes = [ctypes.c_int]
+    L.tweo_optim_table_bytes.restype = sz
+    L.tweo_optim_plan_init.argtypes = [ctypes.POINTER(OptimTensor), ctypes.c_int, vp, sz, ctypes.POINTER(OptimPlan), vp]
+    L.tweo_grad_sumsq.argtypes = [ctypes.POINTER(OptimPlan), vp, vp, sz, vp]
+    L.tweo_adamw_step.argtypes = [ctypes.POINTER(OptimPlan), ctypes.POINTER(AdamwCfg), vp, vp, vp]
     for name in EXPORTS:
         if name not in ("tweo_workspace_bytes", "tweo_status_string", "tweo_delayed_state_bytes",
-                        "tweo_static_scratch_bytes"):
+                        "tweo_static_scratch_bytes", "tweo_optim_table_bytes"):
             getattr(L, name).restype = ctypes.c_int
     _lib = L
     return L
@@ -437,3 +459,119 @@ def tweo_fp8_linear_bwd_bf16_hybrid(dy_bf16, saved, K, dyq, dyqT, dx_bf16=None, 
     _check(load().tweo_fp8_linear_bwd_bf16_hybrid(_ptr(dy_bf16), ctypes.byref(saved), M, N, K, _ptr(dyq),
                                                   _ptr(dyqT), _ptr(dx_bf16), _ptr(dw_bf16), wp, wb,
                                                   _stream()), "tweo_fp8_linear_bwd_bf16_hybrid")
+
+
+def _same(device, shape, dtype, **tensors):
+    """Refuses what a kernel would read as something else: another shape or type, strides, another device than the current one."""
+    for name, t in tensors.items():
+        if t is not None and (t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != device):
+            raise ValueError("%s: a contiguous %s tensor of shape %s on cuda:%d, the current device, is needed, got %s of %s on %s" %
+                             (name, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
+
+
+def _device():
+    _stream()  # _current is set, or the GPU can't be used
+    return _current[0]()
+
+
+def tweo_layernorm_fwd(x_bf16, gamma_bf16, y_bf16, beta_bf16=None, residual_bf16=None, eps=1e-5, h_out_bf16=None,
+                       stats_out=None):
+    import torch
+    if x_bf16.dim() != 2:
+        raise ValueError("x_bf16: two dimensions are needed")
+    rows, cols = shape = x_bf16.shape
+    dev = _device()
+    _same(dev, shape, torch.bfloat16, x_bf16=x_bf16, y_bf16=y_bf16, residual_bf16=residual_bf16,
+          h_out_bf16=None if residual_bf16 is None else h_out_bf16)
+    _same(dev, shape[1:], torch.bfloat16, gamma_bf16=gamma_bf16, beta_bf16=beta_bf16)
+    _same(dev, (rows, 2), torch.float64, stats_out=stats_out)
+    _check(load().tweo_layernorm_fwd(_ptr(x_bf16), _ptr(residual_bf16), _ptr(gamma_bf16), _ptr(beta_bf16), rows, cols,
+                                     float(eps), _ptr(h_out_bf16), _ptr(y_bf16), _ptr(stats_out), _stream()),
+           "tweo_layernorm_fwd")
+
+
+def layernorm_stats(workspace, rows):
+    """The row statistics (mean, 1 / sqrt(var + eps)), fp64 [rows, 2], that a LayerNorm -> cast call left in its workspace."""
+    import torch
+    return workspace[2304:2304 + 16 * rows].view(torch.float64).view(rows, 2)
+
+
+def tweo_layernorm_bwd(dy_bf16, h_bf16, gamma_bf16, stats, dx_bf16, dgamma, dbeta=None, residual_grad_bf16=None,
+                       workspace=None):
+    import torch
+    if dy_bf16.dim() != 2:
+        raise ValueError("dy_bf16: two dimensions are needed")
+    rows, cols = shape = dy_bf16.shape
+    dev = _device()
+    _same(dev, shape, torch.bfloat16, dy_bf16=dy_bf16, h_bf16=h_bf16, dx_bf16=dx_bf16, residual_grad_bf16=residual_grad_bf16)
+    _same(dev, shape[1:], torch.bfloat16, gamma_bf16=gamma_bf16)
+    _same(dev, shape[1:], torch.float32, dgamma=dgamma, dbeta=dbeta)
+    _same(dev, (rows, 2), torch.float64, stats=stats)
+    wp, wb = _ws(workspace)
+    _check(load().tweo_layernorm_bwd(_ptr(dy_bf16), _ptr(h_bf16), _ptr(gamma_bf16), _ptr(stats), _ptr(residual_grad_bf16),
+                                     rows, cols, _ptr(dx_bf16), _ptr(dgamma), _ptr(dbeta), wp, wb, _stream()),
+           "tweo_layernorm_bwd")
+
+
+def optim_tensor(grad, param=None, m=None, v=None, m_step=None, v_step=None, master=None, weight_decay=0.0):
+    """One row of an optimizer's table, checked: grad (bf16 or fp32) alone for the norm, else with param, m and v of as many
+    elements (uint8 codes with their steps, or fp32) and, for a bf16 param, its fp32 copy if there is one."""
+    import torch
+    floats, n, dev = (torch.bfloat16, torch.float32), grad.numel(), grad.get_device()
+    eight = m_step is not None or v_step is not None
+    state = torch.uint8 if eight else torch.float32
+    for name, t, kinds, numel in (("grad", grad, floats, n), ("param", param, floats, n), ("master", master, floats[1:], n),
+                                  ("m", m, (state,), n), ("v", v, (state,), n), ("m_step", m_step, floats[1:], -(-n // 256)),
+                                  ("v_step", v_step, floats[1:], -(-n // 256))):
+        if t is not None and (t.dtype not in kinds or t.numel() != numel or not t.is_contiguous() or t.get_device() != dev):
+            raise ValueError("%s: a contiguous tensor of %d elements of %s on the gradient's device is needed, got %s of %s on %s" %
+                             (name, numel, " or ".join(map(str, kinds)), t.dtype, tuple(t.shape), t.device))
+    row = OptimTensor(_ptr(param), _ptr(master), _ptr(grad), _ptr(m), _ptr(v), _ptr(m_step), _ptr(v_step), n, float(weight_decay),
+                      int(param is not None and param.dtype is torch.float32), int(grad.dtype is torch.float32))
+    row.tensors = [t for t in (param, master, grad, m, v, m_step, v_step) if t is not None]
+    return row
+
+
+def tweo_optim_table_bytes(count):
+    return int(load().tweo_optim_table_bytes(int(count)))
+
+
+def make_optim_plan(rows, table):
+    """The plan of tweo_grad_sumsq and tweo_adamw_step over `rows` (optim_tensor), whose table is written into `table`, a uint8
+    tensor of tweo_optim_table_bytes(len(rows)), on the current stream.  Keeps the tensors alive."""
+    dev = _device()
+    for t in [table] + [t for r in rows for t in r.tensors]:
+        if t.get_device() != dev:
+            raise ValueError("a tensor on %s, but cuda:%d is current" % (t.device, dev))
+    plan = OptimPlan()
+    wp, wb = _ws(table)
+    _check(load().tweo_optim_plan_init((OptimTensor * len(rows))(*rows), len(rows), wp, wb, ctypes.byref(plan), _stream()),
+           "tweo_optim_plan_init")
+    plan.device, plan.tensors = dev, [table] + [t for r in rows for t in r.tensors]
+    return plan
+
+
+def _on_device(plan, sumsq=None, **more):
+    import torch
+    dev = _device()
+    if dev != plan.device:
+        raise ValueError("a plan of cuda:%d, but cuda:%d is current" % (plan.device, dev))
+    if sumsq is not None and sumsq.dtype is not torch.float64:
+        raise ValueError("the sum of squares is one torch.float64, got %s" % sumsq.dtype)
+    for name, t in dict(more, sumsq=sumsq).items():
+        if t is not None and (t.get_device() != dev or t.nbytes < 8):
+            raise ValueError("%s: at least 8 bytes on cuda:%d are needed, got %d on %s" % (name, dev, t.nbytes, t.device))
+
+
+def tweo_grad_sumsq(plan, sumsq_out, workspace):
+    _on_device(plan, sumsq_out, workspace=workspace)
+    wp, wb = _ws(workspace)
+    _check(load().tweo_grad_sumsq(ctypes.byref(plan), _ptr(sumsq_out), wp, wb, _stream()), "tweo_grad_sumsq")
+
+
+def tweo_adamw_step(plan, lr=0.0, step=1, beta1=0.9, beta2=0.999, eps=1e-8, grad_sumsq=None, max_norm=1.0, schedule=None):
+    """schedule: two 32-bit words on the device, lr as fp32 and step as an integer, in the place of `lr` and `step`."""
+    _on_device(plan, grad_sumsq, schedule=schedule)
+    cfg = AdamwCfg(lr, beta1, beta2, eps, max_norm, step)
+    _check(load().tweo_adamw_step(ctypes.byref(plan), ctypes.byref(cfg), _ptr(grad_sumsq), _ptr(schedule), _stream()),
+           "tweo_adamw_step")

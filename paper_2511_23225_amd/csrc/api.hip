@@ -2,6 +2,8 @@
 // Nothing here allocates, frees or synchronises; everything is enqueued on the
 // caller's stream.
 #include <algorithm>
+#include <memory>
+#include <new>
 #include "../../include/tweo.h"
 #include "kernels.h"
 
@@ -10,9 +12,11 @@ using namespace tweo;
 namespace {
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned8(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
 inline size_t round256(size_t b) { return b == 0 ? 256 : (b + 255) / 256 * 256; }
 inline tweo_status hip_status(hipError_t e) { return e == hipSuccess ? TWEO_OK : TWEO_ERR_HIP; }
 constexpr int64_t kMaxDim = (int64_t)1 << 30;
+constexpr int64_t kMaxCols = (int64_t)1 << 24;
 
 inline bool dims_ok(int64_t M, int64_t N, int64_t K)
 {
@@ -134,6 +138,10 @@ size_t tweo_workspace_bytes(int op, int64_t M, int64_t N, int64_t K)
                                        i8_gemm_ksplit_bytes(M, N, K)));
     case TWEO_OP_LAYERNORM_QUANTIZE:  // M rows (N, K unused)
         return kAmaxPartialsMax * sizeof(uint32_t) + 256 + round256((size_t)M * 2 * sizeof(double));
+    case TWEO_OP_LAYERNORM_BWD:  // M rows of N columns
+        return M <= kMaxDim && N <= kMaxCols ? round256(layernorm_bwd_bytes(M, N)) : 256;
+    case TWEO_OP_GRAD_SUMSQ:
+        return kSumsqPartials * sizeof(double);
     default:
         return 256;
     }
@@ -539,6 +547,152 @@ tweo_status tweo_layernorm_quantize_e4m3_delayed(const void *x_bf16, const void 
     return layernorm_quantize_impl(x_bf16, residual_bf16, gamma_bf16, beta_bf16, rows, cols, eps, state, bootstrap,
                                    h_out_bf16, y_out_bf16, nullptr, q, qT, nullptr, nullptr, workspace, workspace_bytes,
                                    stream);
+}
+
+tweo_status tweo_layernorm_fwd(const void *x_bf16, const void *residual_bf16, const void *gamma_bf16,
+                               const void *beta_bf16, int64_t rows, int64_t cols, float eps, void *h_out_bf16,
+                               void *y_bf16, double *stats_out, void *stream)
+{
+    if (!x_bf16 || !gamma_bf16 || !y_bf16 || rows <= 0 || cols <= 0 || !aligned16(x_bf16) || !aligned16(gamma_bf16) ||
+        !aligned16(y_bf16) || (beta_bf16 && !aligned16(beta_bf16)) || (stats_out && !aligned16(stats_out)) || !(eps >= 0.0f))
+        return TWEO_ERR_INVALID_ARG;
+    if (residual_bf16 && (!h_out_bf16 || !aligned16(residual_bf16) || !aligned16(h_out_bf16) || h_out_bf16 == y_bf16))
+        return TWEO_ERR_INVALID_ARG;
+    if (rows > kMaxDim || cols > kMaxCols)
+        return TWEO_ERR_UNSUPPORTED;
+    return hip_status(launch_layernorm_fwd(x_bf16, residual_bf16, gamma_bf16, beta_bf16, rows, cols, (double)eps, h_out_bf16,
+                                           y_bf16, stats_out, (hipStream_t)stream));
+}
+
+tweo_status tweo_layernorm_bwd(const void *dy_bf16, const void *h_bf16, const void *gamma_bf16, const double *stats,
+                               const void *residual_grad_bf16, int64_t rows, int64_t cols, void *dx_bf16, float *dgamma,
+                               float *dbeta, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!dy_bf16 || !h_bf16 || !gamma_bf16 || !stats || !dx_bf16 || !dgamma || rows <= 0 || cols <= 0 || !aligned16(dy_bf16) ||
+        !aligned16(h_bf16) || !aligned16(gamma_bf16) || !aligned16(stats) || !aligned16(dx_bf16) || !aligned16(dgamma) ||
+        (residual_grad_bf16 && !aligned16(residual_grad_bf16)) || (dbeta && !aligned16(dbeta)))
+        return TWEO_ERR_INVALID_ARG;
+    if (rows > kMaxDim || cols > kMaxCols)
+        return TWEO_ERR_UNSUPPORTED;
+    if (!workspace || !aligned16(workspace) || workspace_bytes < layernorm_bwd_bytes(rows, cols))
+        return TWEO_ERR_WORKSPACE;
+    return hip_status(launch_layernorm_bwd(dy_bf16, h_bf16, gamma_bf16, stats, residual_grad_bf16, rows, cols, dx_bf16, dgamma,
+                                           dbeta, workspace, (hipStream_t)stream));
+}
+
+namespace {
+constexpr int kMaxOptimTensors = 1 << 16;
+
+// the buffers of a table: what a step writes overlaps nothing
+struct Range {
+    uintptr_t from, to;
+    bool written;
+};
+
+bool ranges_clash(Range *r, size_t n)
+{
+    std::sort(r, r + n, [](const Range &a, const Range &b) { return a.from < b.from; });
+    uintptr_t any = 0, written = 0;  // ends of the ranges so far
+    for (size_t i = 0; i < n; ++i) {
+        if (r[i].from < (r[i].written ? any : written))
+            return true;
+        any = std::max(any, r[i].to);
+        if (r[i].written)
+            written = std::max(written, r[i].to);
+    }
+    return false;
+}
+
+int optim_state_bits(const tweo_optim_tensor &t) { return !t.param ? 0 : t.m_step ? 8 : 32; }
+
+tweo_status check_optim_tensor(const tweo_optim_tensor &t, int state_bits)
+{
+    auto flag = [](int f) { return f == 0 || f == 1; };
+    if (!t.grad || !aligned16(t.grad) || t.n <= 0 || !flag(t.param_f32) || !flag(t.grad_f32) || optim_state_bits(t) != state_bits)
+        return TWEO_ERR_INVALID_ARG;
+    const void *mine[] = {t.param, t.master, t.m, t.v, t.m_step, t.v_step};
+    for (const void *p : mine)
+        if (p && (!aligned16(p) || state_bits == 0))
+            return TWEO_ERR_INVALID_ARG;
+    if (state_bits != 0 && (!t.m || !t.v || (t.master && t.param_f32) || !t.m_step != !t.v_step || !(t.weight_decay >= 0.0f) ||
+                            t.weight_decay > 3.402823466e+38f))
+        return TWEO_ERR_INVALID_ARG;
+    return t.n > ((int64_t)1 << 40) ? TWEO_ERR_UNSUPPORTED : TWEO_OK;
+}
+
+bool plan_ok(const tweo_optim_plan *plan) { return plan && plan->table && plan->count > 0 && plan->chunks > 0; }
+}  // namespace
+
+size_t tweo_optim_table_bytes(int count) { return round256(count > 0 ? (size_t)count * kOptimEntryBytes : 0); }
+
+tweo_status tweo_optim_plan_init(const tweo_optim_tensor *tensors, int count, void *table, size_t table_bytes,
+                                 tweo_optim_plan *plan, void *stream)
+{
+    if (!tensors || count <= 0 || !plan || (table && !aligned16(table)))
+        return TWEO_ERR_INVALID_ARG;
+    if (count > kMaxOptimTensors)
+        return TWEO_ERR_UNSUPPORTED;
+    if (!table || table_bytes < tweo_optim_table_bytes(count))
+        return TWEO_ERR_WORKSPACE;
+    const int bits = optim_state_bits(tensors[0]);
+    const size_t entries = (size_t)count;
+    std::unique_ptr<Range[]> ranges(new (std::nothrow) Range[7 * entries + 1]);
+    std::unique_ptr<OptimTensor[]> rows(new (std::nothrow) OptimTensor[entries]);
+    if (!ranges || !rows)
+        return TWEO_ERR_UNSUPPORTED;
+    size_t n = 0;
+    int64_t chunks = 0;
+    auto add = [&](const void *p, size_t bytes, bool written) {
+        if (p)
+            ranges[n++] = {(uintptr_t)p, (uintptr_t)p + bytes, written};
+    };
+    add(table, tweo_optim_table_bytes(count), true);
+    for (int i = 0; i < count; ++i) {
+        const tweo_optim_tensor &t = tensors[i];
+        const tweo_status st = check_optim_tensor(t, bits);
+        if (st != TWEO_OK)
+            return st;
+        const size_t k = (size_t)t.n, state = bits == 8 ? 1 : 4, blocks = (k + 255) / 256;
+        add(t.grad, k * (t.grad_f32 ? 4 : 2), false);
+        add(t.param, k * (t.param_f32 ? 4 : 2), true);
+        add(t.master, 4 * k, true);
+        add(t.m, state * k, true);
+        add(t.v, state * k, true);
+        add(t.m_step, 4 * blocks, true);
+        add(t.v_step, 4 * blocks, true);
+        rows[i] = {t.param, t.master, t.grad, t.m, t.v, t.m_step, t.v_step, t.n, t.weight_decay,
+                   (t.param_f32 ? kOptimParamF32 : 0u) | (t.master ? kOptimMaster : 0u) | (t.grad_f32 ? kOptimGradF32 : 0u)};
+        chunks += optim_chunks(t.n);
+    }
+    if (ranges_clash(ranges.get(), n))
+        return TWEO_ERR_INVALID_ARG;
+    *plan = {table, chunks, count, bits};
+    return hip_status(launch_optim_table(rows.get(), count, table, (hipStream_t)stream));
+}
+
+tweo_status tweo_grad_sumsq(const tweo_optim_plan *plan, double *sumsq_out, void *workspace, size_t workspace_bytes,
+                            void *stream)
+{
+    if (!plan_ok(plan) || !sumsq_out || !aligned8(sumsq_out))
+        return TWEO_ERR_INVALID_ARG;
+    if (!workspace || !aligned16(workspace) || workspace_bytes < kSumsqPartials * sizeof(double))
+        return TWEO_ERR_WORKSPACE;
+    return hip_status(launch_grad_sumsq(plan->table, plan->count, plan->chunks, sumsq_out, (double *)workspace, (hipStream_t)stream));
+}
+
+tweo_status tweo_adamw_step(const tweo_optim_plan *plan, const tweo_adamw_cfg *cfg, const double *grad_sumsq,
+                            const tweo_adamw_schedule *schedule, void *stream)
+{
+    if (!plan_ok(plan) || plan->state_bits == 0 || !cfg || (grad_sumsq && !aligned8(grad_sumsq)) || (schedule && !aligned8(schedule)))
+        return TWEO_ERR_INVALID_ARG;
+    auto beta_ok = [](double b) { return b >= 0.0 && b < 1.0; };
+    auto positive = [](double v, double least) { return v >= least && v <= 3.4028234663852886e+38; };
+    if (!beta_ok(cfg->beta1) || !beta_ok(cfg->beta2) || !positive(cfg->eps, 0.0) || (grad_sumsq && !(cfg->max_norm > 0.0)) ||
+        (!schedule && (!positive(cfg->lr, 0.0) || cfg->step < 1 || cfg->step > 0xFFFFFFFFll)))
+        return TWEO_ERR_INVALID_ARG;
+    const AdamwCall call{cfg->lr, cfg->beta1, cfg->beta2, cfg->eps, cfg->max_norm, schedule ? 1u : (uint32_t)cfg->step, grad_sumsq,
+                         (const OptimSchedule *)schedule};
+    return hip_status(launch_adamw(plan->table, plan->count, plan->chunks, plan->state_bits == 8, call, (hipStream_t)stream));
 }
 
 tweo_status tweo_quantize_i8(const void *x_bf16, int64_t n, float inv_step, int8_t *out,

@@ -84,6 +84,61 @@ hipError_t launch_layernorm_quantize(const void *x_bf16, const void *res_bf16, c
                                      void *y_out, uint8_t *q, uint8_t *qT, double *stats, uint32_t *partials,
                                      float *amax_out, float *scale_out, float *scale_inv_out, void *state,
                                      int bootstrap, hipStream_t s);
+// LayerNorm to bf16 and its gradients (layernorm.hip); stats: (mean, 1 / sqrt(var + eps)) of each row.
+hipError_t launch_layernorm_fwd(const void *x_bf16, const void *res_bf16, const void *gamma_bf16, const void *beta_bf16,
+                                int64_t rows, int64_t cols, double eps, void *h_out, void *y, double *stats, hipStream_t s);
+size_t layernorm_bwd_bytes(int64_t rows, int64_t cols);
+hipError_t launch_layernorm_bwd(const void *dy_bf16, const void *h_bf16, const void *gamma_bf16, const double *stats,
+                                const void *dres_bf16, int64_t rows, int64_t cols, void *dx, float *dgamma, float *dbeta,
+                                void *workspace, hipStream_t s);
+
+// Gradient norm and AdamW over a table of tensors (optim.hip).
+enum OptimKind : uint32_t { kOptimParamF32 = 1, kOptimMaster = 2, kOptimGradF32 = 4 };
+constexpr int kOptimChunk = 1024, kOptimEntryBytes = 80;
+constexpr int kSumsqPartials = 2048;  // doubles of workspace
+struct OptimTensor {
+    void *param;
+    float *master;
+    const void *grad;
+    void *m, *v;
+    float *m_step, *v_step;
+    int64_t n;
+    float weight_decay;
+    uint32_t kind;
+};
+struct OptimSchedule {  // in device memory
+    float lr;
+    uint32_t step;
+};
+struct AdamwCall {
+    double lr, beta1, beta2, eps, max_norm;
+    uint32_t step;
+    const double *grad_sumsq;
+    const OptimSchedule *schedule;
+};
+struct AdamwScalars {
+    float step_size, inv_sqrt_bc2;
+};
+// what a step derives from t, on the host or the device with the same bits: powers by squaring, in products alone
+__host__ __device__ inline AdamwScalars adamw_scalars(double lr, double beta1, double beta2, uint32_t t)
+{
+#pragma clang fp contract(off)
+    double p1 = 1.0, p2 = 1.0, b1 = beta1, b2 = beta2;
+    for (; t != 0; t >>= 1) {
+        if (t & 1) {
+            p1 *= b1;
+            p2 *= b2;
+        }
+        b1 *= b1;
+        b2 *= b2;
+    }
+    return {(float)(lr / (1.0 - p1)), (float)(1.0 / __builtin_sqrt(1.0 - p2))};
+}
+int64_t optim_chunks(int64_t n);
+hipError_t launch_optim_table(const OptimTensor *tensors, int count, void *table, hipStream_t s);
+hipError_t launch_grad_sumsq(const void *table, int count, int64_t chunks, double *out, double *partials, hipStream_t s);
+hipError_t launch_adamw(const void *table, int count, int64_t chunks, bool eight_bits, const AdamwCall &c, hipStream_t s);
+
 hipError_t launch_quantize_i8(const void *x_bf16, int64_t n, float inv_step, int8_t *out,
                               hipStream_t s);
 // Row-granular AbsMax INT8: q [rows, cols] and one dequantisation step per row (cols % 8 == 0).
