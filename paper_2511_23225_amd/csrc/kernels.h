@@ -95,7 +95,7 @@ hipError_t launch_layernorm_bwd(const void *dy_bf16, const void *h_bf16, const v
 // Gradient norm and AdamW over a table of tensors (optim.hip).
 enum OptimKind : uint32_t { kOptimParamF32 = 1, kOptimMaster = 2, kOptimGradF32 = 4 };
 constexpr int kOptimChunk = 1024, kOptimEntryBytes = 80;
-constexpr int kSumsqPartials = 2048;  // doubles of workspace
+constexpr int kSumsqPartials = 1024;  // doubles of workspace
 struct OptimTensor {
     void *param;
     float *master;

@@ -40,90 +40,188 @@ __global__ __launch_bounds__(kWave) void optim_table_kernel(EntryBatch b, int co
         to[i] = from[i];
 }
 
-// the entry that holds chunk c
-__device__ __forceinline__ int find_entry(const Entry *table, int count, int64_t c)
+// The table's addresses are of global memory, the table itself is read through the scalar cache: told to the compiler, which takes what it
+// reads from memory for an address in any space (FLAT accesses) and the table for something that the stores could change.
+#define GLOBAL __attribute__((address_space(1)))
+#define CONSTANT __attribute__((address_space(4)))
+typedef const CONSTANT Entry *Table;
+
+// The entry that holds chunk c: the wave's lanes look at 64 entries at once, so that up to 64 tensors take one load's time and
+// up to 4096 two.  (Halving took six to eight loads that wait for each other.)
+__device__ __forceinline__ int find_entry(Table table, int count, int64_t c)
 {
-    int lo = 0, hi = count;  // table[lo].first_chunk <= c < table[hi].first_chunk
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (table[mid].first_chunk <= c)
-            lo = mid;
-        else
-            hi = mid;
+    const int lane = threadIdx.x & (kWave - 1);
+    int from = 0, to = count;  // table[from].first_chunk <= c
+    while (to - from > 1) {
+        const int step = (to - from + kWave - 1) / kWave, i = from + lane * step;
+        const bool below = i < to && table[i].first_chunk <= c;
+        const int last = __builtin_popcountll(__builtin_amdgcn_ballot_w64(below)) - 1;  // lane 0's is always below
+        from += last * step;
+        to = from + step < to ? from + step : to;
     }
-    return lo;
+    return __builtin_amdgcn_readfirstlane(from);
 }
 
-// Four consecutive elements from an address that is a multiple of four elements; with those past the tensor's end as zeros.
+// Loads and stores of four consecutive elements, `at` bytes behind a base that all lanes share.  ONCE: past the caches, for a model whose
+// buffers together are more than the memory-side cache keeps from one step to the next.
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 template <bool F32>
 struct Four;
 template <>
 struct Four<true> {
-    typedef float4 raw;
-    static __device__ __forceinline__ raw load(const void *p, int64_t i) { return *(const float4 *)((const float *)p + i); }
-    static __device__ __forceinline__ raw load_some(const void *p, int64_t i, int n)
+    typedef f32x4 raw;
+    static constexpr uint32_t kBytes = 4;
+    template <bool ONCE>
+    static __device__ __forceinline__ raw load(const GLOBAL uint8_t *p, uint32_t at)
     {
-        const float *f = (const float *)p + i;
-        return make_float4(n > 0 ? f[0] : 0.0f, n > 1 ? f[1] : 0.0f, n > 2 ? f[2] : 0.0f, n > 3 ? f[3] : 0.0f);
+        const GLOBAL raw *q = (const GLOBAL raw *)(p + at);
+        return ONCE ? __builtin_nontemporal_load(q) : *q;
     }
-    static __device__ __forceinline__ void widen(raw r, float (&out)[4]) { out[0] = r.x, out[1] = r.y, out[2] = r.z, out[3] = r.w; }
-    static __device__ __forceinline__ void store(void *p, int64_t i, const float (&v)[4])
+    static __device__ __forceinline__ raw load_some(const GLOBAL uint8_t *p, uint32_t at, int n)
     {
-        *(float4 *)((float *)p + i) = make_float4(v[0], v[1], v[2], v[3]);
+        const GLOBAL float *f = (const GLOBAL float *)(p + at);
+        return raw{n > 0 ? f[0] : 0.0f, n > 1 ? f[1] : 0.0f, n > 2 ? f[2] : 0.0f, n > 3 ? f[3] : 0.0f};
     }
-    static __device__ __forceinline__ void store_some(void *p, int64_t i, int n, const float (&v)[4])
+    static __device__ __forceinline__ void widen(raw r, float (&out)[4]) { out[0] = r[0], out[1] = r[1], out[2] = r[2], out[3] = r[3]; }
+    template <bool ONCE>
+    static __device__ __forceinline__ void store(GLOBAL uint8_t *p, uint32_t at, const float (&v)[4])
+    {
+        GLOBAL raw *q = (GLOBAL raw *)(p + at);
+        const raw r{v[0], v[1], v[2], v[3]};
+        if constexpr (ONCE)
+            __builtin_nontemporal_store(r, q);
+        else
+            *q = r;
+    }
+    static __device__ __forceinline__ void store_some(GLOBAL uint8_t *p, uint32_t at, int n, const float (&v)[4])
     {
 #pragma unroll
         for (int k = 0; k < 4; ++k)
             if (k < n)
-                ((float *)p)[i + k] = v[k];
+                ((GLOBAL float *)(p + at))[k] = v[k];
     }
 };
+// (half the bytes of a line at a time: measured slower past the caches)
 template <>
 struct Four<false> {
-    typedef uint2 raw;
-    static __device__ __forceinline__ raw load(const void *p, int64_t i) { return *(const uint2 *)((const uint16_t *)p + i); }
-    static __device__ __forceinline__ raw load_some(const void *p, int64_t i, int n)
+    typedef uint32_t raw __attribute__((ext_vector_type(2)));
+    static constexpr uint32_t kBytes = 2;
+    template <bool>
+    static __device__ __forceinline__ raw load(const GLOBAL uint8_t *p, uint32_t at) { return *(const GLOBAL raw *)(p + at); }
+    static __device__ __forceinline__ raw load_some(const GLOBAL uint8_t *p, uint32_t at, int n)
     {
-        const uint16_t *h = (const uint16_t *)p + i;
+        const GLOBAL uint16_t *h = (const GLOBAL uint16_t *)(p + at);
         const uint32_t e0 = n > 0 ? h[0] : 0u, e1 = n > 1 ? h[1] : 0u, e2 = n > 2 ? h[2] : 0u, e3 = n > 3 ? h[3] : 0u;
-        return make_uint2(e0 | e1 << 16, e2 | e3 << 16);
+        return raw{e0 | e1 << 16, e2 | e3 << 16};
     }
     static __device__ __forceinline__ void widen(raw r, float (&out)[4])
     {
         out[0] = bf16lo_to_f32(r.x), out[1] = bf16hi_to_f32(r.x), out[2] = bf16lo_to_f32(r.y), out[3] = bf16hi_to_f32(r.y);
     }
-    static __device__ __forceinline__ void store(void *p, int64_t i, const float (&v)[4])
+    template <bool>
+    static __device__ __forceinline__ void store(GLOBAL uint8_t *p, uint32_t at, const float (&v)[4])
     {
-        *(uint2 *)((uint16_t *)p + i) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+        *(GLOBAL raw *)(p + at) = raw{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
     }
-    static __device__ __forceinline__ void store_some(void *p, int64_t i, int n, const float (&v)[4])
+    static __device__ __forceinline__ void store_some(GLOBAL uint8_t *p, uint32_t at, int n, const float (&v)[4])
     {
         const uint32_t lo = pack_bf16x2(v[0], v[1]), hi = pack_bf16x2(v[2], v[3]);
 #pragma unroll
         for (int k = 0; k < 4; ++k)
             if (k < n)
-                ((uint16_t *)p)[i + k] = (uint16_t)((k < 2 ? lo : hi) >> (16 * (k & 1)));
+                ((GLOBAL uint16_t *)(p + at))[k] = (uint16_t)((k < 2 ? lo : hi) >> (16 * (k & 1)));
     }
 };
+// four codes
+struct Codes {
+    typedef uint32_t raw;
+    static constexpr uint32_t kBytes = 1;
+    template <bool>
+    static __device__ __forceinline__ raw load(const GLOBAL uint8_t *p, uint32_t at) { return *(const GLOBAL uint32_t *)(p + at); }
+    static __device__ __forceinline__ raw load_some(const GLOBAL uint8_t *p, uint32_t at, int n)
+    {
+        const GLOBAL uint8_t *c = p + at;
+        const uint32_t c0 = n > 0 ? c[0] : 0u, c1 = n > 1 ? c[1] : 0u, c2 = n > 2 ? c[2] : 0u, c3 = n > 3 ? c[3] : 0u;
+        return c0 | c1 << 8 | c2 << 16 | c3 << 24;
+    }
+    template <bool>
+    static __device__ __forceinline__ void store(GLOBAL uint8_t *p, uint32_t at, raw c) { *(GLOBAL uint32_t *)(p + at) = c; }
+    static __device__ __forceinline__ void store_some(GLOBAL uint8_t *p, uint32_t at, int n, raw c)
+    {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (k < n)
+                (p + at)[k] = (uint8_t)(c >> (8 * k));
+    }
+};
+// a buffer's element `base`, the same for all lanes
+template <typename F>
+__device__ __forceinline__ GLOBAL uint8_t *from(const void *p, int64_t base)
+{
+    return (GLOBAL uint8_t *)p + base * F::kBytes;
+}
+template <typename F, bool FULL, bool ONCE>
+__device__ __forceinline__ typename F::raw load4(const GLOBAL uint8_t *p, uint32_t element, int left)
+{
+    if (FULL || left >= 4)
+        return F::template load<ONCE>(p, element * F::kBytes);
+    return F::load_some(p, element * F::kBytes, left);
+}
+template <typename F, bool FULL, bool ONCE, typename V>
+__device__ __forceinline__ void store4(GLOBAL uint8_t *p, uint32_t element, int left, const V &v)
+{
+    if (FULL || left >= 4)
+        F::template store<ONCE>(p, element * F::kBytes, v);
+    else
+        F::store_some(p, element * F::kBytes, left, v);
+}
 
 // ---------------------------------------------------------------------------
 // Sum of squares of all gradients.  2 (bf16) or 4 bytes an element read, nothing else.  fp64 from the square on: bf16 and fp32 gradients
 // have squares outside fp32's range, and a sum over 10^9 elements in fp32 would lose what a clipping threshold compares.  A wave
-// takes consecutive chunks; workgroup b leaves its sum in partials[b], and one more workgroup adds those in a fixed order.
+// takes consecutive chunks, four (fp32: two) at a time where the tensor has them: 8 KB under way in each.  Workgroup b leaves its sum in
+// partials[b], and one more workgroup adds those in a fixed order: a counter at which the last one is found takes 12 ns a workgroup.
+// 205 M bf16 gradients 68 us, 6.0 TB/s, what tweo_amax reads at; a chunk of 8-byte loads at a time 83; 3 M in 61 tensors 7.5, two launches.
 constexpr int kSumsqThreads = 256;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-template <bool F32>
-__device__ __forceinline__ double sumsq_chunk(const Entry &e, int64_t base)
+
+// whole chunks: 16 bytes a lane and load, all of them under way at once
+template <bool F32, bool ONCE, int CHUNKS>
+__device__ __forceinline__ double sumsq_whole(const GLOBAL uint8_t *grad)
 {
-    const int lane = threadIdx.x & (kWave - 1);
+    constexpr int LOADS = CHUNKS * kChunk * (F32 ? 4 : 2) / (16 * kWave);
+    const GLOBAL u32x4 *p = (const GLOBAL u32x4 *)grad + (threadIdx.x & (kWave - 1));
+    u32x4 r[LOADS];
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j)
+        r[j] = ONCE ? __builtin_nontemporal_load(p + j * kWave) : p[j * kWave];
+    double s[2] = {0.0, 0.0};
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if constexpr (F32) {
+                const double g = (double)bits_to_f32(r[j][k]);
+                s[k & 1] = __builtin_fma(g, g, s[k & 1]);
+            } else {
+                const double lo = (double)bf16lo_to_f32(r[j][k]), hi = (double)bf16hi_to_f32(r[j][k]);
+                s[0] = __builtin_fma(lo, lo, s[0]);
+                s[1] = __builtin_fma(hi, hi, s[1]);
+            }
+        }
+    return s[0] + s[1];
+}
+
+// the last chunk of a tensor
+template <bool F32>
+__device__ __forceinline__ double sumsq_rest(const GLOBAL uint8_t *grad, int n)
+{
+    const uint32_t first = 4 * (threadIdx.x & (kWave - 1));
     typename Four<F32>::raw r[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int64_t i = base + 4 * (j * kWave + lane);
-        const int64_t left = e.n - i;
-        r[j] = left >= 4 ? Four<F32>::load(e.grad, i) : Four<F32>::load_some(e.grad, i, left > 0 ? (int)left : 0);
-    }
+    for (int j = 0; j < 4; ++j)
+        r[j] = load4<Four<F32>, false, false>(grad, first + 256 * j, n - (int)first - 256 * j);
     double s = 0.0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -134,6 +232,21 @@ __device__ __forceinline__ double sumsq_chunk(const Entry &e, int64_t base)
             s = __builtin_fma((double)g[k], (double)g[k], s);
     }
     return s;
+}
+
+// chunks c to `to` of one tensor (no further than its end); how many of them were taken
+template <bool F32, bool ONCE>
+__device__ __forceinline__ int sumsq_step(const CONSTANT Entry &e, int64_t c, int64_t to, double &s)
+{
+    const int64_t base = (c - e.first_chunk) * kChunk, n = e.n - base;
+    const GLOBAL uint8_t *grad = from<Four<F32>>(e.grad, base);
+    constexpr int MANY = F32 ? 2 : 4;
+    if (n >= MANY * kChunk && to - c >= MANY) {
+        s += sumsq_whole<F32, ONCE, MANY>(grad);
+        return MANY;
+    }
+    s += n >= kChunk ? sumsq_whole<F32, ONCE, 1>(grad) : sumsq_rest<F32>(grad, (int)n);
+    return 1;
 }
 
 __device__ __forceinline__ double workgroup_sum(double v, double *red, int threads)
@@ -148,22 +261,20 @@ __device__ __forceinline__ double workgroup_sum(double v, double *red, int threa
     return s;
 }
 
-__global__ __launch_bounds__(kSumsqThreads) void grad_sumsq_kernel(const Entry *__restrict__ table, int count, int64_t chunks,
+template <bool ONCE>
+__global__ __launch_bounds__(kSumsqThreads) void grad_sumsq_kernel(const Entry *entries, int count, int64_t chunks,
                                                                    double *__restrict__ partials)
 {
     const int64_t waves = (int64_t)gridDim.x * (kSumsqThreads / kWave),
                   wave = (int64_t)blockIdx.x * (kSumsqThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int64_t from = chunks * wave / waves, to = chunks * (wave + 1) / waves;
+    const Table table = (Table)entries;
     double s = 0.0;
-    if (from < to) {
-        int at = find_entry(table, count, from);
-        for (int64_t c = from; c < to; ++c) {
-            while (at + 1 < count && table[at + 1].first_chunk <= c)
-                ++at;
-            const Entry &e = table[at];
-            const int64_t base = (c - e.first_chunk) * kChunk;
-            s += e.kind & kOptimGradF32 ? sumsq_chunk<true>(e, base) : sumsq_chunk<false>(e, base);
-        }
+    for (int64_t c = from; c < to;) {
+        const CONSTANT Entry &e = table[find_entry(table, count, c)];
+        const int64_t end = e.first_chunk + (e.n + kChunk - 1) / kChunk, stop = end < to ? end : to;
+        while (c < stop)
+            c += e.kind & kOptimGradF32 ? sumsq_step<true, ONCE>(e, c, stop, s) : sumsq_step<false, ONCE>(e, c, stop, s);
     }
     __shared__ double red[kSumsqThreads / kWave];
     s = workgroup_sum(s, red, kSumsqThreads);
@@ -185,6 +296,10 @@ __global__ __launch_bounds__(kSumsqThreads) void grad_sumsq_finish_kernel(const 
 // ---------------------------------------------------------------------------
 // AdamW: with the clipped gradient g' = c g, c = min(1, max_norm / (sqrt(S) + 1e-6)),
 //   m = b1 m + (1 - b1) g',  v = b2 v + (1 - b2) g'^2,  p = p - lr wd p - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps).
+// Bound by memory: 28 B an element with fp32 states beside an fp32 copy, 22 without; 18 and 10 with 8-bit states.  A wave takes one chunk, all of
+// whose loads (20 to 28 of 4 to 16 bytes a lane) are under way before the first is waited for, and workgroups walk the tensors in order: 51 M elements with
+// master, fp32 states 241 us (6.0 TB/s), 205 M with 8-bit states 580 (5.7), without master 374 (5.5, half of its time the SIMDs issue).  Persistent
+// waves, each on a run of chunks of its own, took 301, 703 and 450; persistent ones in turns, the streams of all side by side, 284 and 665.
 //
 // 8-bit states: a block of 256 elements shares an fp32 step for m (E4M3 codes) and one for v (E5M2: no square root is taken on the way,
 // and 2^32 between the largest and the smallest).  A block is 16 lanes of a wave with 16 elements each, four at a time 64 apart, so that its
@@ -263,82 +378,79 @@ __device__ __forceinline__ BlockScale block_scale(uint32_t amax_bits, float top)
     return {scale, amax_bits < 0x7F800000u ? 1.0f / scale : __builtin_nanf("")};
 }
 
+// least: 1 for what must not become zero
 template <int CUT>
-__device__ __forceinline__ uint32_t encode(float magnitude, float scale, float to_field, uint32_t largest, uint32_t u)
+__device__ __forceinline__ uint32_t encode(float magnitude, float scale, float to_field, uint32_t least, uint32_t largest, uint32_t u)
 {
     const float y = fmul(fmul(magnitude, scale), to_field);
     const uint32_t code = (f32_to_bits(y) + (u >> (32 - CUT))) >> CUT;
-    return code < largest ? code : largest;
+    const uint32_t up = code > least ? code : least;
+    return up < largest ? up : largest;
 }
 
 constexpr uint32_t kDitherElement = 0x6A09E667u, kDitherStep = 0x9E3779B9u;  // 2^32 (sqrt(2) - 1), 2^32 (sqrt(5) - 1) / 2, odd
 
-// KIND: kOptimParamF32, kOptimMaster, kOptimGradF32.  FULL: the chunk has all of its elements.
-template <bool EIGHT, uint32_t KIND, bool FULL>
-__device__ __forceinline__ void adamw_chunk(const Entry &e, int64_t base, const AdamwArgs &a, const StepScalars &k)
+// What a step needs beside its tensors; false: nothing may change.
+__device__ __forceinline__ bool step_scalars(const AdamwArgs &a, StepScalars &k)
+{
+    k = {a.lr, a.step_size, a.inv_sqrt_bc2, 1.0f, a.step * kDitherStep};
+    if (a.schedule != nullptr) {
+        const AdamwScalars s = adamw_scalars((double)a.schedule->lr, a.beta1_d, a.beta2_d, a.schedule->step);
+        k = {a.schedule->lr, s.step_size, s.inv_sqrt_bc2, 1.0f, a.schedule->step * kDitherStep};
+    }
+    if (a.grad_sumsq != nullptr) {
+        const double norm = __builtin_sqrt(*a.grad_sumsq);
+        if (!(norm < __builtin_inf()))
+            return false;  // a gradient that is not finite
+        const double c = a.max_norm / (norm + 1e-6);
+        k.clip = c < 1.0 ? (float)c : 1.0f;
+    }
+    return true;
+}
+
+// KIND: kOptimParamF32, kOptimMaster, kOptimGradF32.  FULL: the chunk has all of its elements.  ONCE: see Four.
+template <bool EIGHT, bool ONCE, uint32_t KIND, bool FULL>
+__device__ __forceinline__ void adamw_chunk(const CONSTANT Entry &e, int64_t base, const AdamwArgs &a)
 {
     constexpr bool P32 = (KIND & kOptimParamF32) != 0, MASTER = (KIND & kOptimMaster) != 0, G32 = (KIND & kOptimGradF32) != 0;
     typedef Four<P32 || MASTER> P;
     typedef Four<G32> G;
+    typedef std::conditional_t<EIGHT, Codes, Four<true>> S;
+    // with an fp32 copy nothing but the optimizer reads it; a parameter by itself is what the next forward pass reads
+    constexpr bool P_ONCE = ONCE && MASTER;
     const int lane = threadIdx.x & (kWave - 1);
-    void *weights = MASTER ? (void *)e.master : e.param;
-    const int64_t n = e.n;
-    // the lane's four elements of pass j
-    auto at = [&](int j) { return base + (EIGHT ? (lane >> 4) * 256 + j * 64 + (lane & 15) * 4 : j * 256 + lane * 4); };
-    auto some = [&](int64_t i) { return n - i < 4 ? (n - i > 0 ? (int)(n - i) : 0) : 4; };
-    auto load = [&](auto four, const void *p, int64_t i) {
-        typedef decltype(four) F;
-        return FULL || some(i) == 4 ? F::load(p, i) : F::load_some(p, i, some(i));
-    };
-    auto store = [&](auto four, void *p, int64_t i, const float (&x)[4]) {
-        typedef decltype(four) F;
-        if (FULL || some(i) == 4)
-            F::store(p, i, x);
-        else
-            F::store_some(p, i, some(i), x);
-    };
-    auto load_codes = [&](const void *p, int64_t i) {
-        if (FULL || some(i) == 4)
-            return *(const uint32_t *)((const uint8_t *)p + i);
-        uint32_t c = 0;
-        for (int b = 0; b < some(i); ++b)
-            c |= (uint32_t)((const uint8_t *)p)[i + b] << (8 * b);
-        return c;
-    };
-    auto store_codes = [&](void *p, int64_t i, uint32_t c) {
-        if (FULL || some(i) == 4) {
-            *(uint32_t *)((uint8_t *)p + i) = c;
-            return;
-        }
-        for (int b = 0; b < some(i); ++b)
-            ((uint8_t *)p)[i + b] = (uint8_t)(c >> (8 * b));
-    };
+    GLOBAL uint8_t *const weights = from<P>(MASTER ? (void *)e.master : e.param, base), *const param = from<Four<false>>(e.param, base),
+                          *const em = from<S>(e.m, base), *const ev = from<S>(e.v, base);
+    const GLOBAL uint8_t *const grad = from<G>(e.grad, base);
+    const int n = FULL ? kChunk : (int)(e.n - base);  // of the chunk
+    // the lane's four elements of pass j begin at `first` + j * STEP
+    constexpr int STEP = EIGHT ? 64 : 256;
+    const uint32_t first = EIGHT ? (lane >> 4) * 256 + (lane & 15) * 4 : lane * 4;
+    const int left = n - (int)first;
     typename P::raw pr[4];
     typename G::raw gr[4];
-    float4 mr[4], vr[4];
-    uint32_t mc[4], vc[4];
+    typename S::raw mr[4], vr[4];
     float m_step = 0.0f, v_step = 0.0f;
     const int64_t block = base / 256 + (lane >> 4);
-    const bool has_block = FULL || base + (lane >> 4) * 256 < n;
+    const bool has_block = FULL || (lane >> 4) * 256 < n;
     if constexpr (EIGHT) {
         if (has_block) {
-            m_step = e.m_step[block];
-            v_step = e.v_step[block];
+            m_step = ((const GLOBAL float *)e.m_step)[block];
+            v_step = ((const GLOBAL float *)e.v_step)[block];
         }
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const int64_t i = at(j);
-        gr[j] = load(G{}, e.grad, i);
-        if constexpr (EIGHT) {
-            mc[j] = load_codes(e.m, i);
-            vc[j] = load_codes(e.v, i);
-        } else {
-            mr[j] = load(Four<true>{}, e.m, i);
-            vr[j] = load(Four<true>{}, e.v, i);
-        }
-        pr[j] = load(P{}, weights, i);
+        const uint32_t i = first + j * STEP;
+        gr[j] = load4<G, FULL, ONCE>(grad, i, left - j * STEP);
+        mr[j] = load4<S, FULL, ONCE>(em, i, left - j * STEP);
+        vr[j] = load4<S, FULL, ONCE>(ev, i, left - j * STEP);
+        pr[j] = load4<P, FULL, P_ONCE>(weights, i, left - j * STEP);
     }
+    // while these are on their way
+    StepScalars k;
+    if (!step_scalars(a, k))
+        return;
     const float lr_decay = k.lr * e.weight_decay;
     float m[4][4], v[4][4];
     uint32_t m_max = 0, v_max = 0;
@@ -348,13 +460,13 @@ __device__ __forceinline__ void adamw_chunk(const Entry &e, int64_t base, const 
         G::widen(gr[j], g);
         P::widen(pr[j], p);
         if constexpr (EIGHT) {
-            const v2f m0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mc[j], false), m1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mc[j], true);
-            const v2f v0 = __builtin_amdgcn_cvt_pk_f32_bf8((int)vc[j], false), v1 = __builtin_amdgcn_cvt_pk_f32_bf8((int)vc[j], true);
+            const v2f m0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mr[j], false), m1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mr[j], true);
+            const v2f v0 = __builtin_amdgcn_cvt_pk_f32_bf8((int)vr[j], false), v1 = __builtin_amdgcn_cvt_pk_f32_bf8((int)vr[j], true);
             m[j][0] = fmul(m0[0], m_step), m[j][1] = fmul(m0[1], m_step), m[j][2] = fmul(m1[0], m_step), m[j][3] = fmul(m1[1], m_step);
             v[j][0] = fmul(v0[0], v_step), v[j][1] = fmul(v0[1], v_step), v[j][2] = fmul(v1[0], v_step), v[j][3] = fmul(v1[1], v_step);
         } else {
-            Four<true>::widen(mr[j], m[j]);
-            Four<true>::widen(vr[j], v[j]);
+            S::widen(mr[j], m[j]);
+            S::widen(vr[j], v[j]);
         }
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -363,94 +475,84 @@ __device__ __forceinline__ void adamw_chunk(const Entry &e, int64_t base, const 
             v[j][q] = blend(a.beta2, v[j][q], a.one_minus_beta2, fmul(gc, gc));
             p[q] = updated(p[q], m[j][q], v[j][q], lr_decay, k, a.eps);
             if constexpr (EIGHT) {
-                // what lies behind the tensor's end is zero in all of them and no maximum
-                const uint32_t mb = f32_to_bits(m[j][q]) & 0x7FFFFFFFu, vb = f32_to_bits(v[j][q]) & 0x7FFFFFFFu;
+                // as patterns a NaN is the largest, whatever its sign in v; what lies behind the tensor's end is zero and no maximum
+                const uint32_t mb = f32_to_bits(m[j][q]) & 0x7FFFFFFFu, vb = f32_to_bits(v[j][q]);
                 m_max = mb > m_max ? mb : m_max;
                 v_max = vb > v_max ? vb : v_max;
             }
         }
-        const int64_t i = at(j);
-        store(P{}, weights, i, p);
+        const uint32_t i = first + j * STEP;
+        store4<P, FULL, P_ONCE>(weights, i, left - j * STEP, p);
         if constexpr (MASTER)
-            store(Four<false>{}, e.param, i, p);
+            store4<Four<false>, FULL, false>(param, i, left - j * STEP, p);
         if constexpr (!EIGHT) {
-            store(Four<true>{}, e.m, i, m[j]);
-            store(Four<true>{}, e.v, i, v[j]);
+            store4<S, FULL, ONCE>(em, i, left - j * STEP, m[j]);
+            store4<S, FULL, ONCE>(ev, i, left - j * STEP, v[j]);
         }
     }
     if constexpr (EIGHT) {
         const BlockScale ms = block_scale(row_max_u32(m_max), 448.0f), vs = block_scale(row_max_u32(v_max), 57344.0f);
+        const uint32_t u0 = ((uint32_t)base + first) * kDitherElement + k.dither;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int64_t i = at(j);
-            uint32_t mo = 0, vo = 0, u = (uint32_t)i * kDitherElement + k.dither;
+            uint32_t mo = 0, vo = 0;
 #pragma unroll
-            for (int q = 0; q < 4; ++q, u += kDitherElement) {
-                uint32_t c = encode<20>(__builtin_fabsf(m[j][q]), ms.scale, 0x1p-120f, 0x7Eu, u);
-                mo |= (c | (f32_to_bits(m[j][q]) >> 24 & 0x80u)) << (8 * q);
-                c = encode<21>(__builtin_fabsf(v[j][q]), vs.scale, 0x1p-112f, 0x7Bu, u);
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t u = u0 + (uint32_t)(j * STEP + q) * kDitherElement, mb = f32_to_bits(m[j][q]), vb = f32_to_bits(v[j][q]);
+                const uint32_t mc = encode<20>(__builtin_fabsf(m[j][q]), ms.scale, 0x1p-120f, 0u, 0x7Eu, u);
+                mo |= (mc | (mb >> 24 & 0x80u)) << (8 * q);
                 // a positive second moment stays positive: it is a divisor
-                vo |= (c == 0u && v[j][q] > 0.0f ? 1u : c) << (8 * q);
+                vo |= encode<21>(__builtin_fabsf(v[j][q]), vs.scale, 0x1p-112f, vb < 1u ? vb : 1u, 0x7Bu, u) << (8 * q);
             }
-            store_codes(e.m, i, mo);
-            store_codes(e.v, i, vo);
+            store4<S, FULL, false>(em, first + j * STEP, left - j * STEP, mo);
+            store4<S, FULL, false>(ev, first + j * STEP, left - j * STEP, vo);
         }
         if ((lane & 15) == 0 && has_block) {
-            e.m_step[block] = ms.step;
-            e.v_step[block] = vs.step;
+            ((GLOBAL float *)e.m_step)[block] = ms.step;
+            ((GLOBAL float *)e.v_step)[block] = vs.step;
         }
     }
 }
 
-template <bool EIGHT, bool FULL>
-__device__ __forceinline__ void adamw_any(const Entry &e, int64_t base, const AdamwArgs &a, const StepScalars &k)
+template <bool EIGHT, bool ONCE, bool FULL>
+__device__ __forceinline__ void adamw_any(const CONSTANT Entry &e, int64_t base, const AdamwArgs &a)
 {
     switch (e.kind) {
-    case 0: adamw_chunk<EIGHT, 0, FULL>(e, base, a, k); break;
-    case kOptimGradF32: adamw_chunk<EIGHT, kOptimGradF32, FULL>(e, base, a, k); break;
-    case kOptimParamF32: adamw_chunk<EIGHT, kOptimParamF32, FULL>(e, base, a, k); break;
-    case kOptimParamF32 | kOptimGradF32: adamw_chunk<EIGHT, kOptimParamF32 | kOptimGradF32, FULL>(e, base, a, k); break;
-    case kOptimMaster: adamw_chunk<EIGHT, kOptimMaster, FULL>(e, base, a, k); break;
-    default: adamw_chunk<EIGHT, kOptimMaster | kOptimGradF32, FULL>(e, base, a, k); break;
+    case 0: adamw_chunk<EIGHT, ONCE, 0, FULL>(e, base, a); break;
+    case kOptimGradF32: adamw_chunk<EIGHT, ONCE, kOptimGradF32, FULL>(e, base, a); break;
+    case kOptimParamF32: adamw_chunk<EIGHT, ONCE, kOptimParamF32, FULL>(e, base, a); break;
+    case kOptimParamF32 | kOptimGradF32: adamw_chunk<EIGHT, ONCE, kOptimParamF32 | kOptimGradF32, FULL>(e, base, a); break;
+    case kOptimMaster: adamw_chunk<EIGHT, ONCE, kOptimMaster, FULL>(e, base, a); break;
+    default: adamw_chunk<EIGHT, ONCE, kOptimMaster | kOptimGradF32, FULL>(e, base, a); break;
     }
 }
 
 constexpr int kAdamwThreads = 256;
 
-template <bool EIGHT>
+template <bool EIGHT, bool ONCE>
 __global__ __launch_bounds__(kAdamwThreads) void adamw_kernel(AdamwArgs a)
 {
-    StepScalars k{a.lr, a.step_size, a.inv_sqrt_bc2, 1.0f, a.step * kDitherStep};
-    if (a.schedule != nullptr) {
-        const AdamwScalars s = adamw_scalars((double)a.schedule->lr, a.beta1_d, a.beta2_d, a.schedule->step);
-        k = {a.schedule->lr, s.step_size, s.inv_sqrt_bc2, 1.0f, a.schedule->step * kDitherStep};
-    }
-    if (a.grad_sumsq != nullptr) {
-        const double norm = __builtin_sqrt(*a.grad_sumsq);
-        if (!(norm < __builtin_inf()))
-            return;  // a gradient that is not finite: no tensor changes
-        const double c = a.max_norm / (norm + 1e-6);
-        k.clip = c < 1.0 ? (float)c : 1.0f;
-    }
     const int64_t waves = (int64_t)gridDim.x * (kAdamwThreads / kWave),
                   wave = (int64_t)blockIdx.x * (kAdamwThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int64_t from = a.chunks * wave / waves, to = a.chunks * (wave + 1) / waves;
-    if (from >= to)
-        return;
-    int at = find_entry(a.table, a.count, from);
-    for (int64_t c = from; c < to; ++c) {
-        while (at + 1 < a.count && a.table[at + 1].first_chunk <= c)
-            ++at;
-        const Entry &e = a.table[at];
+    const Table table = (Table)a.table;
+    for (int64_t c = wave; c < a.chunks; c += waves) {
+        const CONSTANT Entry &e = table[find_entry(table, a.count, c)];
         const int64_t base = (c - e.first_chunk) * kChunk;
         if (base + kChunk <= e.n)
-            adamw_any<EIGHT, true>(e, base, a, k);
+            adamw_any<EIGHT, ONCE, true>(e, base, a);
         else
-            adamw_any<EIGHT, false>(e, base, a, k);
+            adamw_any<EIGHT, ONCE, false>(e, base, a);
     }
 }
 
-constexpr int kCus = 256;
+constexpr int64_t kAdamwMostGroups = 1 << 20;
+
+// Whether buffers of so many bytes an element are more than the memory-side cache (256 MB) gives back to the next step.  One step after the
+// other, without and with accesses past the caches: fp32 states beside a master, 28 B an element, 3 M elements 15.3 us and 17.7, 5 M 24.7 and
+// 25.9, 7 M 36.9 and 34.8, 20 M 108 and 87; 8-bit ones, 18 B, 5 M 19.0 and 20.7, 10 M 32.8 and 30.9, 20 M 67 and 58.
+// (The norm, bf16 gradients: 103 MB 22.9 and 22.9, 411 MB 77 and 68.)
+constexpr int64_t kKeptBytes = 160 << 20;
+bool past_caches(int64_t chunks, int64_t bytes) { return chunks * kChunk * bytes > kKeptBytes; }
 
 }  // namespace
 
@@ -478,7 +580,8 @@ hipError_t launch_optim_table(const OptimTensor *tensors, int count, void *table
 hipError_t launch_grad_sumsq(const void *table, int count, int64_t chunks, double *out, double *partials, hipStream_t s)
 {
     const int groups = (int)std::min<int64_t>((chunks + 3) / 4, kSumsqPartials);
-    hipLaunchKernelGGL(grad_sumsq_kernel, dim3(groups), dim3(kSumsqThreads), 0, s, (const Entry *)table, count, chunks, partials);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(groups), dim3(kSumsqThreads), 0, s, (const Entry *)table, count, chunks, partials); };
+    past_caches(chunks, 2) ? go(grad_sumsq_kernel<true>) : go(grad_sumsq_kernel<false>);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess)
         return e;
@@ -491,11 +594,12 @@ hipError_t launch_adamw(const void *table, int count, int64_t chunks, bool eight
     const AdamwScalars k = adamw_scalars(c.lr, c.beta1, c.beta2, c.step);
     const AdamwArgs a{(const Entry *)table, count, chunks, (float)c.beta1, (float)(1.0 - c.beta1), (float)c.beta2, (float)(1.0 - c.beta2),
                       (float)c.eps, (float)c.lr, k.step_size, k.inv_sqrt_bc2, c.beta1, c.beta2, c.max_norm, c.step, c.grad_sumsq, c.schedule};
-    const unsigned groups = (unsigned)std::min<int64_t>((chunks + 3) / 4, 4 * kCus);
-    if (eight_bits)
-        hipLaunchKernelGGL(adamw_kernel<true>, dim3(groups), dim3(kAdamwThreads), 0, s, a);
+    const unsigned groups = (unsigned)std::min<int64_t>((chunks + 3) / 4, kAdamwMostGroups);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(groups), dim3(kAdamwThreads), 0, s, a); };
+    if (past_caches(chunks, eight_bits ? 18 : 28))
+        eight_bits ? go(adamw_kernel<true, true>) : go(adamw_kernel<false, true>);
     else
-        hipLaunchKernelGGL(adamw_kernel<false>, dim3(groups), dim3(kAdamwThreads), 0, s, a);
+        eight_bits ? go(adamw_kernel<true, false>) : go(adamw_kernel<false, false>);
     return hipGetLastError();
 }
 
