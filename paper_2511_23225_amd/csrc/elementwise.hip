@@ -507,6 +507,61 @@ struct LnArgs {
     const uint16_t *gamma, *beta;  // bf16 [cols]; beta may be nullptr
 };
 
+// eight elements (see ln_pairs); g64 / b64: the eight columns' parameters
+__device__ __forceinline__ uint4 ln_vec(uint4 x, double mean, double rstd, const double (&g64)[8], const double (&b64)[8],
+                                        bool has_beta)
+{
+    const uint32_t xx[4] = {x.x, x.y, x.z, x.w};
+    uint32_t r[4];
+    ln_pairs<8>(xx, mean, rstd, g64, b64, has_beta, r);
+    return make_uint4(r[0], r[1], r[2], r[3]);
+}
+
+__device__ __forceinline__ void widen8(uint4 v, double (&out)[8])
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        out[2 * k] = (double)bf16lo_to_f32(w[k]);
+        out[2 * k + 1] = (double)bf16hi_to_f32(w[k]);
+    }
+}
+
+// h = bf16(x + r) on eight elements: the fp32 sum of two bf16 values rounded to bf16 equals the
+// exact sum rounded once (the fp32 sum is exact unless the smaller term lies below the bf16
+// rounding position of the larger one by more than fp32 can hold, and then it decides nothing)
+__device__ __forceinline__ uint4 add_bf16x8(uint4 a, uint4 b)
+{
+    const uint32_t aa[4] = {a.x, a.y, a.z, a.w}, bb[4] = {b.x, b.y, b.z, b.w};
+    uint32_t r[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        r[k] = pack_bf16x2(bf16lo_to_f32(aa[k]) + bf16lo_to_f32(bb[k]), bf16hi_to_f32(aa[k]) + bf16hi_to_f32(bb[k]));
+    return make_uint4(r[0], r[1], r[2], r[3]);
+}
+
+__device__ __forceinline__ double sum8_f64(uint4 v)
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    double s = 0.0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        s += (double)bf16lo_to_f32(w[k]) + (double)bf16hi_to_f32(w[k]);
+    return s;
+}
+
+__device__ __forceinline__ double sumsq8_f64(uint4 v, double mean)
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    double s = 0.0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const double d0 = (double)bf16lo_to_f32(w[k]) - mean, d1 = (double)bf16hi_to_f32(w[k]) - mean;
+        s += d0 * d0 + d1 * d1;
+    }
+    return s;
+}
+
 // Maximum over a wave without LDS: DPP row shifts, then the two row broadcasts; lane 63 holds it.
 template <int CTRL, int ROW_MASK>
 __device__ __forceinline__ float dpp_max_f32(float v)

@@ -19,28 +19,27 @@ __device__ __forceinline__ float f64_to_f32_for_bf16(double v)
     return (float)__builtin_bit_cast(double, b);
 }
 
-// eight elements of a row: y = (x - mean) * (rstd * gamma) + beta in fp64 (one rounding more or
+// N elements of a row: y = (x - mean) * (rstd * gamma) + beta in fp64 (one rounding more or
 // less than the textbook order of operations: 1e-16 relative, far below anything a bf16 rounding
-// sees), as packed bf16 pairs.  g64 / b64: the eight columns' parameters, widened by the caller.
+// sees), as packed bf16 pairs.  g / b: the columns' parameters, widened by the caller.
 // The way to bf16 goes through the nearest fp32: rounding twice differs from rounding once only if
 // the fp32 value is exactly half way between two bf16 values (low half 0x8000), which one element
 // in 65536 is; a vector that holds one (and then the wave, once in about 130 vectors) is rounded
 // again through the round-to-odd fp32.  Four integer operations per element fewer than that way
 // for all (16384x2048: cast 34.4 -> 33.0 us).
-__device__ __forceinline__ uint4 ln_vec(uint4 x, double mean, double rstd, const double (&g64)[8], const double (&b64)[8],
-                                        bool has_beta)
+template <int N, typename Param>
+__device__ __forceinline__ void ln_pairs(const uint32_t (&x)[N / 2], double mean, double rstd, const Param (&g)[N], const Param (&b)[N],
+                                         bool has_beta, uint32_t (&r)[N / 2])
 {
-    const uint32_t xx[4] = {x.x, x.y, x.z, x.w};
-    uint32_t r[4];
-    double y[8];
+    double y[N];
     u16x2 tie = {0xFFFF, 0xFFFF};
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const double d0 = (double)bf16lo_to_f32(xx[k]) - mean, d1 = (double)bf16hi_to_f32(xx[k]) - mean;
-        const double a0 = rstd * g64[2 * k], a1 = rstd * g64[2 * k + 1];
+    for (int k = 0; k < N / 2; ++k) {
+        const double d0 = (double)bf16lo_to_f32(x[k]) - mean, d1 = (double)bf16hi_to_f32(x[k]) - mean;
+        const double a0 = rstd * (double)g[2 * k], a1 = rstd * (double)g[2 * k + 1];
         // without a beta nothing is added, so that a zero keeps the sign the product gives it
-        y[2 * k] = has_beta ? __builtin_fma(d0, a0, b64[2 * k]) : d0 * a0;
-        y[2 * k + 1] = has_beta ? __builtin_fma(d1, a1, b64[2 * k + 1]) : d1 * a1;
+        y[2 * k] = has_beta ? __builtin_fma(d0, a0, (double)b[2 * k]) : d0 * a0;
+        y[2 * k + 1] = has_beta ? __builtin_fma(d1, a1, (double)b[2 * k + 1]) : d1 * a1;
         const float f0 = (float)y[2 * k], f1 = (float)y[2 * k + 1];
         const uint32_t low = __builtin_amdgcn_perm(f32_to_bits(f1), f32_to_bits(f0), 0x05040100u) ^ 0x80008000u;
         tie = __builtin_elementwise_min(tie, __builtin_bit_cast(u16x2, low));
@@ -48,59 +47,13 @@ __device__ __forceinline__ uint4 ln_vec(uint4 x, double mean, double rstd, const
     }
     if (tie[0] == 0 || tie[1] == 0) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < N / 2; ++k)
             r[k] = pack_bf16x2(f64_to_f32_for_bf16(y[2 * k]), f64_to_f32_for_bf16(y[2 * k + 1]));
     }
-    return make_uint4(r[0], r[1], r[2], r[3]);
 }
 
-__device__ __forceinline__ void widen8(uint4 v, double (&out)[8])
-{
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        out[2 * k] = (double)bf16lo_to_f32(w[k]);
-        out[2 * k + 1] = (double)bf16hi_to_f32(w[k]);
-    }
-}
-
-// h = bf16(x + r) on eight elements: the fp32 sum of two bf16 values rounded to bf16 equals the
-// exact sum rounded once (the fp32 sum is exact unless the smaller term lies below the bf16
-// rounding position of the larger one by more than fp32 can hold, and then it decides nothing)
-__device__ __forceinline__ uint4 add_bf16x8(uint4 a, uint4 b)
-{
-    const uint32_t aa[4] = {a.x, a.y, a.z, a.w}, bb[4] = {b.x, b.y, b.z, b.w};
-    uint32_t r[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-        r[k] = pack_bf16x2(bf16lo_to_f32(aa[k]) + bf16lo_to_f32(bb[k]), bf16hi_to_f32(aa[k]) + bf16hi_to_f32(bb[k]));
-    return make_uint4(r[0], r[1], r[2], r[3]);
-}
-
-__device__ __forceinline__ double sum8_f64(uint4 v)
-{
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    double s = 0.0;
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-        s += (double)bf16lo_to_f32(w[k]) + (double)bf16hi_to_f32(w[k]);
-    return s;
-}
-
-__device__ __forceinline__ double sumsq8_f64(uint4 v, double mean)
-{
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    double s = 0.0;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const double d0 = (double)bf16lo_to_f32(w[k]) - mean, d1 = (double)bf16hi_to_f32(w[k]) - mean;
-        s += d0 * d0 + d1 * d1;
-    }
-    return s;
-}
-
-// Sum over a wave without LDS: DPP row shifts, then the two row broadcasts (every lane gets it; a shuffle through the LDS
-// takes ten times as long, and these sums are a chain in the middle of a row).
+// Sum over a wave without LDS: DPP row shifts, then the two row broadcasts (every lane gets it; a shuffle through the
+// LDS takes ten times as long, and these sums are a chain in the middle of a row).
 template <int CTRL, int ROW_MASK>
 __device__ __forceinline__ double dpp_add_f64(double v)
 {

@@ -1,5 +1,6 @@
 // LayerNorm to bf16, forward and backward.  Rows of any length; gfx950 only.
 #include <algorithm>
+#include <type_traits>
 #include "kernels.h"
 #include "layernorm.h"
 
@@ -8,81 +9,125 @@ namespace tweo {
 namespace {
 
 // ---------------------------------------------------------------------------
-// A row is worked on by a team of T waves; lane l of the team holds the 16-byte pieces (eight elements) l, l + 64 T, ... of it,
-// P of them, in registers.  RAGGED: cols is no multiple of eight, so rows start at any even address and their last piece is short.
+// A row is worked on by a team of T waves; lane l of the team holds the pieces l, l + 64 T, ... of it, P of them, V elements (4 or 8:
+// 8 or 16 bytes) each, in registers.  RAGGED: cols is no multiple of V, so that rows start at any even address and their last piece is
+// short.  ONCE: past the caches.
 
-typedef uint32_t loose_u4 __attribute__((ext_vector_type(4), aligned(2)));  // 16 bytes at any even address
+template <int V>
+struct Piece {
+    uint32_t w[V / 2];  // packed pairs
+    __device__ __forceinline__ float at(int k) const { return k & 1 ? bf16hi_to_f32(w[k >> 1]) : bf16lo_to_f32(w[k >> 1]); }
+    // keeps the packed form in registers, not its widened values, over what comes next
+    __device__ __forceinline__ void keep()
+    {
+#pragma unroll
+        for (int k = 0; k < V / 2; ++k)
+            asm volatile("" : "+v"(w[k]));
+    }
+};
 
-template <bool RAGGED>
+template <int V, bool RAGGED>
 struct Row {
+    typedef uint32_t vec __attribute__((ext_vector_type(V / 2), aligned(RAGGED ? 2 : 2 * V)));
     int cols, pieces;
-    __device__ __forceinline__ explicit Row(int cols_) : cols(cols_), pieces(RAGGED ? (cols_ + 7) >> 3 : cols_ >> 3) {}
+    __device__ __forceinline__ explicit Row(int cols_) : cols(cols_), pieces((cols_ + V - 1) / V) {}
     // elements of piece i
     __device__ __forceinline__ int count(int i) const
     {
-        if constexpr (!RAGGED)
-            return i < pieces ? 8 : 0;
-        const int left = cols - 8 * i;
-        return left < 0 ? 0 : left < 8 ? left : 8;
+        const int left = cols - V * i;
+        return left < 0 ? 0 : left < V ? left : V;
     }
-    // piece i of the row at p, with zeros behind its end; a lane without a piece gets one of the row's (aligned rows: with a
-    // branch around each load the compiler waits for one before it issues the next) or zeros
-    __device__ __forceinline__ uint4 load(const uint16_t *p, int i) const
+    // A lane without a piece gets the row's last one: with a branch around each load the compiler waits for one before it issues the
+    // next.  (Of a ragged row only pieces that are whole are loaded this way.)
+    template <bool ONCE>
+    __device__ __forceinline__ Piece<V> whole(const uint16_t *p, int i) const
     {
-        if constexpr (!RAGGED) {
-            const int last = pieces - 1, j = i < last ? i : last;
-            return *(const uint4 *)((const uint8_t *)p + (uint64_t)((uint32_t)j * 16u));
-        }
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        const int n = count(i);
-        if (n == 8) {
-            const loose_u4 l = *(const loose_u4 *)(p + 8 * (int64_t)i);
-            v = make_uint4(l[0], l[1], l[2], l[3]);
-        } else if (n > 0) {
-            uint32_t e[8];
+        const int last = pieces - 1, j = RAGGED || i < last ? i : last;
+        const vec *q = (const vec *)((const uint8_t *)p + (uint64_t)((uint32_t)j * (2u * V)));
+        const vec v = ONCE ? __builtin_nontemporal_load(q) : *q;
+        Piece<V> r;
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                e[k] = k < n ? p[8 * (int64_t)i + k] : 0u;
-            v = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
-        }
-        return v;
+        for (int k = 0; k < V / 2; ++k)
+            r.w[k] = v[k];
+        return r;
     }
-    __device__ __forceinline__ void store(uint16_t *p, int i, uint4 v) const
+    // a ragged row's last piece, or none: zeros behind the end
+    __device__ __forceinline__ Piece<V> rest(const uint16_t *p, int i) const
     {
-        if constexpr (!RAGGED) {
-            if (i < pieces)
-                *(uint4 *)((uint8_t *)p + (uint64_t)((uint32_t)i * 16u)) = v;
-            return;
-        }
         const int n = count(i);
-        if (n == 8) {
-            *(loose_u4 *)(p + 8 * (int64_t)i) = loose_u4{v.x, v.y, v.z, v.w};
-        } else if (n > 0) {
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        uint32_t e[V];
 #pragma unroll
-            for (int k = 0; k < 7; ++k)
+        for (int k = 0; k < V; ++k)
+            e[k] = k < n ? p[V * (int64_t)i + k] : 0u;
+        Piece<V> r;
+#pragma unroll
+        for (int k = 0; k < V / 2; ++k)
+            r.w[k] = e[2 * k] | e[2 * k + 1] << 16;
+        return r;
+    }
+    template <bool ONCE = false>
+    __device__ __forceinline__ Piece<V> load(const uint16_t *p, int i) const
+    {
+        return !RAGGED || count(i) == V ? whole<ONCE>(p, i) : rest(p, i);
+    }
+    template <bool ONCE = false>
+    __device__ __forceinline__ void store(uint16_t *p, int i, const Piece<V> &v) const
+    {
+        vec x;
+#pragma unroll
+        for (int k = 0; k < V / 2; ++k)
+            x[k] = v.w[k];
+        const int n = count(i);
+        if (RAGGED ? n == V : n > 0) {
+            vec *q = (vec *)((uint8_t *)p + (uint64_t)((uint32_t)i * (2u * V)));
+            if constexpr (ONCE)
+                __builtin_nontemporal_store(x, q);
+            else
+                *q = x;
+        } else if (RAGGED && n > 0) {
+#pragma unroll
+            for (int k = 0; k < V - 1; ++k)
                 if (k < n)
-                    p[8 * (int64_t)i + k] = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
+                    p[V * (int64_t)i + k] = (uint16_t)(v.w[k >> 1] >> (16 * (k & 1)));
         }
     }
 };
 
-// sum of squared differences of the first n elements of a piece
-template <bool RAGGED>
-__device__ __forceinline__ double squares(uint4 v, double mean, int n)
+// bytes that a call moves from which on what is not read again soon goes past the caches (the memory-side one has 256 MB)
+constexpr int64_t kKeptBytes = 100 << 20;
+
+template <int V>
+__device__ __forceinline__ Piece<V> sum_of(const Piece<V> &a, const Piece<V> &b)
 {
-    if constexpr (!RAGGED) {
-        const double t = sumsq8_f64(v, mean);
-        return n > 0 ? t : 0.0;
-    }
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    // bf16(x + r): the fp32 sum of two bf16 values rounded to bf16 equals the exact sum rounded once
+    Piece<V> r;
+#pragma unroll
+    for (int k = 0; k < V / 2; ++k)
+        r.w[k] = pack_bf16x2(a.at(2 * k) + b.at(2 * k), a.at(2 * k + 1) + b.at(2 * k + 1));
+    return r;
+}
+
+template <int V>
+__device__ __forceinline__ double sum64(const Piece<V> &v)
+{
     double s = 0.0;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const double d0 = (double)bf16lo_to_f32(w[k]) - mean, d1 = (double)bf16hi_to_f32(w[k]) - mean;
-        s += (2 * k < n ? d0 * d0 : 0.0) + (2 * k + 1 < n ? d1 * d1 : 0.0);
-    }
+    for (int k = 0; k < V; ++k)
+        s += (double)v.at(k);
     return s;
+}
+
+// sum of squared differences of the first n elements
+template <int V, bool RAGGED>
+__device__ __forceinline__ double squares64(const Piece<V> &v, double mean, int n)
+{
+    double s = 0.0;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        const double d = (double)v.at(k) - mean;
+        s += !RAGGED || k < n ? d * d : 0.0;
+    }
+    return n > 0 ? s : 0.0;
 }
 
 // Sum over the T waves of a team: of each wave through DPP, then through LDS, added in the waves' order by all of them.  `red`: the
@@ -106,7 +151,11 @@ __device__ __forceinline__ double team_sum(double v, double *red, int wave)
 // ---------------------------------------------------------------------------
 // Forward: y = (h - mu) / sqrt(var + eps) * gamma + beta, h = x or bf16(x + residual).  One read of a row (2 B an element, 4 with a
 // residual), one write (2, 4): mean and squared differences are taken of the registers, in fp64 as in the pass in front of the
-// FP8 cast, whose stored activation this one's equals bit for bit.
+// FP8 cast, whose stored activation this one's equals bit for bit (fp32 in its place: no faster where memory bounds it, 54.4 us and 54.1 at 16384x2048;
+// 19.2 and 15.8 at 16384x1024, which the caches hold).  The next row is under way while one is worked on.  With a residual x and it are
+// read for the last time, and h, the stream, is next read a whole layer later: large calls load and store them past the caches (16384x2048 52.4 us,
+// 48.3, the stores alone 53.7; 8192x768, 50 MB, 13.3 and 14.3).
+// 16384x2048 with a residual 48.3 us, 5.6 TB/s; 50432x768 56; 8192x768 13.3; one row of 2048 4.9 of which 3 run.
 struct LnFwdArgs {
     const uint16_t *x, *res, *gamma, *beta;
     uint16_t *h, *y;
@@ -116,53 +165,73 @@ struct LnFwdArgs {
     double eps;
 };
 
-template <int T>
-constexpr int kFwdWaves = T > 4 ? T : 4;
-
-template <int T, int P, bool RES, bool RAGGED>
-__global__ __launch_bounds__(kFwdWaves<T> *kWave) void ln_fwd_kernel(LnFwdArgs a)
+template <int T, int P, int V, int WAVES, bool RES, bool RAGGED, bool ONCE>
+__global__ __launch_bounds__(WAVES *kWave) void ln_fwd_kernel(LnFwdArgs a)
 {
-    constexpr int WAVES = kFwdWaves<T>, TEAMS = WAVES / T;
+    constexpr int TEAMS = WAVES / T;
+    constexpr bool AHEAD = !RAGGED;  // (a ragged row's loads branch, and are waited for one after the other)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), team = wave / T;
     const int lane = (int)threadIdx.x - team * T * kWave;
-    const Row<RAGGED> row(a.cols);
+    const Row<V, RAGGED> row(a.cols);
     const double n = (double)a.cols;
     __shared__ double red[2][WAVES];
-    for (int64_t r0 = (int64_t)blockIdx.x * TEAMS; r0 < a.rows; r0 += (int64_t)gridDim.x * TEAMS) {
-        // a team without a row goes through the last one's sums with the others (barriers) and stores nothing
-        const bool mine = r0 + team < a.rows;
-        const int64_t r = mine ? r0 + team : a.rows - 1;
-        if (T == 1 && !mine)
-            return;
-        uint4 c[P];
-        double s = 0.0;
-#pragma unroll
-        for (int u = 0; u < P; ++u)
-            c[u] = row.load(a.x + r * a.cols, lane + u * T * kWave);
-        if constexpr (RES) {
-            uint4 d[P];
-#pragma unroll
-            for (int u = 0; u < P; ++u)
-                d[u] = row.load(a.res + r * a.cols, lane + u * T * kWave);
-#pragma unroll
-            for (int u = 0; u < P; ++u) {
-                c[u] = add_bf16x8(c[u], d[u]);
-                if (mine)
-                    row.store(a.h + r * a.cols, lane + u * T * kWave, c[u]);
-            }
-        }
+    // a team without a row goes through the last one's sums with the others (barriers) and stores nothing
+    Piece<V> nx[P], nr[RES ? P : 1];
+    auto request = [&](int64_t r0) {
+        const int64_t r = r0 + team < a.rows ? r0 + team : a.rows - 1, at = r * a.cols;
 #pragma unroll
         for (int u = 0; u < P; ++u) {
-            const double t = sum8_f64(c[u]);
-            s += row.count(lane + u * T * kWave) > 0 ? t : 0.0;
+            nx[u] = row.template load<ONCE>(a.x + at, lane + u * T * kWave);
+            if constexpr (RES)
+                nr[u] = row.template load<ONCE>(a.res + at, lane + u * T * kWave);
+        }
+    };
+    if (AHEAD && (int64_t)blockIdx.x * TEAMS < a.rows)
+        request((int64_t)blockIdx.x * TEAMS);
+    float gamma[P][V], beta[P][V];
+#pragma unroll
+    for (int u = 0; u < P; ++u) {
+        const int i = lane + u * T * kWave;
+        const Piece<V> g = row.load(a.gamma, i);
+        Piece<V> b{};
+        if (a.beta != nullptr)
+            b = row.load(a.beta, i);
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            gamma[u][k] = g.at(k), beta[u][k] = b.at(k);
+    }
+    for (int64_t r0 = (int64_t)blockIdx.x * TEAMS; r0 < a.rows; r0 += (int64_t)gridDim.x * TEAMS) {
+        const bool mine = r0 + team < a.rows;
+        const int64_t r = mine ? r0 + team : a.rows - 1, at = r * a.cols;
+        if (T == 1 && !mine)
+            return;
+        if (!AHEAD)
+            request(r0);
+        Piece<V> c[P];
+#pragma unroll
+        for (int u = 0; u < P; ++u) {
+            c[u] = nx[u];
+            if constexpr (RES)
+                c[u] = sum_of(nx[u], nr[u]);
+        }
+        // before this row's stores: they may overwrite x or the residual, but never another row of them
+        if (AHEAD && r0 + (int64_t)gridDim.x * TEAMS < a.rows)
+            request(r0 + (int64_t)gridDim.x * TEAMS);
+        double s = 0.0;
+#pragma unroll
+        for (int u = 0; u < P; ++u) {
+            const int i = lane + u * T * kWave;
+            if (RES && mine)
+                row.template store<ONCE>(a.h + at, i, c[u]);
+            const double t = sum64(c[u]);
+            s += row.count(i) > 0 ? t : 0.0;
         }
         const double mean = team_sum<T>(s, &red[0][team * T], wave - team * T) / n;
         double ss = 0.0;
 #pragma unroll
         for (int u = 0; u < P; ++u) {
-            // the packed form is what stays in registers, not its widened values
-            asm volatile("" : "+v"(c[u].x), "+v"(c[u].y), "+v"(c[u].z), "+v"(c[u].w));
-            ss += squares<RAGGED>(c[u], mean, row.count(lane + u * T * kWave));
+            c[u].keep();
+            ss += squares64<V, RAGGED>(c[u], mean, row.count(lane + u * T * kWave));
         }
         const double rstd = 1.0 / __builtin_sqrt(team_sum<T>(ss, &red[1][team * T], wave - team * T) / n + a.eps);
         if (!mine)
@@ -173,12 +242,10 @@ __global__ __launch_bounds__(kFwdWaves<T> *kWave) void ln_fwd_kernel(LnFwdArgs a
         }
 #pragma unroll
         for (int u = 0; u < P; ++u) {
-            asm volatile("" : "+v"(c[u].x), "+v"(c[u].y), "+v"(c[u].z), "+v"(c[u].w));
-            const int i = lane + u * T * kWave;
-            double g[8], b[8];
-            widen8(row.load(a.gamma, i), g);
-            widen8(a.beta != nullptr ? row.load(a.beta, i) : make_uint4(0u, 0u, 0u, 0u), b);
-            row.store(a.y + r * a.cols, i, ln_vec(c[u], mean, rstd, g, b, a.beta != nullptr));
+            c[u].keep();
+            Piece<V> y;
+            ln_pairs<V>(c[u].w, mean, rstd, gamma[u], beta[u], a.beta != nullptr, y.w);
+            row.store(a.y + at, lane + u * T * kWave, y);
         }
     }
 }
@@ -191,53 +258,62 @@ __global__ __launch_bounds__(kWideThreads) void ln_fwd_wide_kernel(LnFwdArgs a)
 {
     constexpr int T = kWideThreads / kWave;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const Row<RAGGED> row(a.cols);
+    const Row<8, RAGGED> row(a.cols);
     const double n = (double)a.cols;
     __shared__ double red[2][T];
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         double s = 0.0;
         for (int i = threadIdx.x; i < row.pieces; i += kWideThreads) {
-            uint4 v = row.load(a.x + r * a.cols, i);
+            Piece<8> v = row.load(a.x + r * a.cols, i);
             if constexpr (RES) {
-                v = add_bf16x8(v, row.load(a.res + r * a.cols, i));
+                v = sum_of(v, row.load(a.res + r * a.cols, i));
                 row.store(a.h + r * a.cols, i, v);
             }
-            s += sum8_f64(v);
+            s += sum64(v);
         }
         // h may be x or the residual itself: what this thread has stored is read back, not formed again
-        const uint16_t *h = RES ? a.h : a.x;
+        const uint16_t *h = (RES ? a.h : a.x) + r * a.cols;
         const double mean = team_sum<T>(s, red[0], wave) / n;
         double ss = 0.0;
         for (int i = threadIdx.x; i < row.pieces; i += kWideThreads)
-            ss += squares<RAGGED>(row.load(h + r * a.cols, i), mean, row.count(i));
+            ss += squares64<8, RAGGED>(row.load(h, i), mean, row.count(i));
         const double rstd = 1.0 / __builtin_sqrt(team_sum<T>(ss, red[1], wave) / n + a.eps);
         if (a.stats != nullptr && threadIdx.x == 0) {
             a.stats[2 * r] = mean;
             a.stats[2 * r + 1] = rstd;
         }
         for (int i = threadIdx.x; i < row.pieces; i += kWideThreads) {
-            double g[8], b[8];
-            widen8(row.load(a.gamma, i), g);
-            widen8(a.beta != nullptr ? row.load(a.beta, i) : make_uint4(0u, 0u, 0u, 0u), b);
-            row.store(a.y + r * a.cols, i, ln_vec(row.load(h + r * a.cols, i), mean, rstd, g, b, a.beta != nullptr));
+            const Piece<8> x = row.load(h, i), g = row.load(a.gamma, i);
+            Piece<8> b{}, y;
+            if (a.beta != nullptr)
+                b = row.load(a.beta, i);
+            float gamma[8], beta[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                gamma[k] = g.at(k), beta[k] = b.at(k);
+            ln_pairs<8>(x.w, mean, rstd, gamma, beta, a.beta != nullptr, y.w);
+            row.store(a.y + r * a.cols, i, y);
         }
     }
 }
 
 constexpr int kCus = 256;  // of an MI355X; a device with more or fewer runs the same grids
 
-template <int T, int P>
+template <int T, int P, int V, int WAVES>
 void launch_fwd(const LnFwdArgs &a, hipStream_t s)
 {
-    constexpr int TEAMS = kFwdWaves<T> / T;
-    const int64_t wanted = (a.rows + TEAMS - 1) / TEAMS, most = kCus * 32 / kFwdWaves<T>;
+    // as many workgroups as hide each other's barriers: 32 waves a CU, 16 where a team is eight waves and more (4096x8192 52.5 us, with 32 54.1)
+    constexpr int TEAMS = WAVES / T, WAVES_PER_CU = T >= 8 ? 16 : 32;
+    const int64_t wanted = (a.rows + TEAMS - 1) / TEAMS, most = kCus * WAVES_PER_CU / WAVES;
     auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(wanted, most)), dim3(kFwdWaves<T> * kWave), 0, s, a);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(wanted, most)), dim3(WAVES * kWave), 0, s, a);
     };
-    if (a.cols % 8 != 0)
-        a.res ? go(ln_fwd_kernel<T, P, true, true>) : go(ln_fwd_kernel<T, P, false, true>);
+    if (a.cols % V != 0)
+        a.res ? go(ln_fwd_kernel<T, P, V, WAVES, true, true, false>) : go(ln_fwd_kernel<T, P, V, WAVES, false, true, false>);
+    else if (a.res && a.rows * a.cols * 8 > kKeptBytes)
+        go(ln_fwd_kernel<T, P, V, WAVES, true, false, true>);
     else
-        a.res ? go(ln_fwd_kernel<T, P, true, false>) : go(ln_fwd_kernel<T, P, false, false>);
+        a.res ? go(ln_fwd_kernel<T, P, V, WAVES, true, false, false>) : go(ln_fwd_kernel<T, P, V, WAVES, false, false, false>);
 }
 
 // ---------------------------------------------------------------------------
@@ -245,13 +321,17 @@ void launch_fwd(const LnFwdArgs &a, hipStream_t s)
 //   dx = rstd (w - mean(w) - xhat mean(w xhat)) + dres,   dgamma = sum over rows of dy xhat,   dbeta = sum over rows of dy.
 // One read of h, dy and dres, one write of dx (6 B an element, 8 with dres).  The column sums stay in registers over the rows that a
 // team works on, are added over a workgroup's teams through LDS, and leave the workgroup as one row of partial sums in the
-// workspace, which a second launch adds in their order (no atomics: the same bits on every run).  fp32 throughout but for
-// h - mu: mu is a double and is subtracted in two parts, since rows whose mean is far above their deviation cancel there.
+// workspace, which a second launch adds in their order (no atomics: the same bits on every run).  512 workgroups of eight waves, two a CU: with
+// more of them the partial sums (8 B a column and workgroup) and their addition take what the further waves gain (18912x768: 768 of them 37 us in
+// the place of 33).  fp32 throughout but for h - mu: mu is a double and is subtracted in two parts, since rows whose mean is far above their
+// deviation cancel there.  What is read here is read for the last time: large calls read past the caches (16384x2048 56.5 us, 51.2; 8192x768, 50 MB,
+// 16.9 and 17.6).  Wide rows on teams of more waves with fewer elements each: the sums' registers are what limits the waves.
+// 16384x2048 with dres 51.2 us, 5.2 TB/s (45 + 4.5 for the second launch); 18912x768 28.0, 50432x768 59.2, 8192x768 16.1; 257x1001 8.6, two launches.
 struct LnBwdArgs {
     const uint16_t *dy, *h, *gamma, *dres;
     const double *stats;
     uint16_t *dx;
-    float *partials;  // [groups][2][cols]
+    float *partials;  // [groups][2][cols rounded up to fours]
     float *sums;      // wide rows: mean(w), mean(w xhat) of each row
     int64_t rows;
     int cols;
@@ -273,71 +353,94 @@ __device__ __forceinline__ float dpp_sum(float v)
     return bits_to_f32((uint32_t)__builtin_amdgcn_readlane((int)f32_to_bits(v), 63));
 }
 
-__device__ __forceinline__ float element(uint4 v, int k)
-{
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    return k & 1 ? bf16hi_to_f32(w[k >> 1]) : bf16lo_to_f32(w[k >> 1]);
-}
-
 // SLAB: rows of more pieces than the teams hold; blockIdx.y is the slab of T * P * 64 pieces that this workgroup works on, and a
 // launch before has left the two means of each row.
-template <int T, int P, int WAVES, bool RES, bool RAGGED, bool SLAB>
+template <int T, int P, int V, int WAVES, bool RES, bool RAGGED, bool SLAB, bool ONCE>
 __global__ __launch_bounds__(WAVES *kWave) void ln_bwd_kernel(LnBwdArgs a)
 {
     constexpr int TEAMS = WAVES / T;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), team = wave / T;
     const int lane = (int)threadIdx.x - team * T * kWave, first = SLAB ? (int)blockIdx.y * T * P * kWave : 0;
-    const Row<RAGGED> row(a.cols);
+    const Row<V, RAGGED> row(a.cols);
     const float inv_n = 1.0f / (float)a.cols;
     __shared__ float2 red[2][WAVES];
-    uint4 gamma[P];
-    float dgamma[P][8], dbeta[P][8];
+    float gamma[P][V], dgamma[P][V], dbeta[P][V];
+    int turn = 0;
+    // the next row under way while one is worked on: where teams are small (16384x1536 47.6 -> 45.6 us; 2048 wide 56.4 -> 59.4) or fill a
+    // CU by themselves (4096x8192 61.7 -> 59.3)
+    constexpr bool AHEAD = !RAGGED && (T <= 2 || T == 16);
+    Piece<V> nh[P], ndy[P], ndres[RES ? P : 1];
+    double nmean, nrstd;
+    auto request = [&](int64_t r0) {
+        const int64_t r = r0 + team < a.rows ? r0 + team : a.rows - 1, at = r * a.cols;
+#pragma unroll
+        for (int u = 0; u < P; ++u) {
+            const int i = first + lane + u * T * kWave;
+            if (!RAGGED || row.count(i) == V) {
+                nh[u] = row.template whole<ONCE>(a.h + at, i);
+                ndy[u] = row.template whole<ONCE>(a.dy + at, i);
+                if constexpr (RES)
+                    ndres[u] = row.template whole<ONCE>(a.dres + at, i);
+            } else {
+                nh[u] = row.rest(a.h + at, i);
+                ndy[u] = row.rest(a.dy + at, i);
+                if constexpr (RES)
+                    ndres[u] = row.rest(a.dres + at, i);
+            }
+        }
+        nmean = a.stats[2 * r], nrstd = a.stats[2 * r + 1];
+    };
+    if (AHEAD && (int64_t)blockIdx.x * TEAMS < a.rows)
+        request((int64_t)blockIdx.x * TEAMS);
 #pragma unroll
     for (int u = 0; u < P; ++u) {
         const int i = first + lane + u * T * kWave;
-        // a gain of zero keeps a lane without a piece out of the row's sums (its column sums are not stored)
-        gamma[u] = row.load(a.gamma, i);
-        if (row.count(i) == 0)
-            gamma[u] = make_uint4(0u, 0u, 0u, 0u);
+        const Piece<V> g = row.load(a.gamma, i);
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
+        for (int k = 0; k < V; ++k) {
+            // a gain of zero keeps a lane without a piece out of the row's sums (its column sums are not stored)
+            gamma[u][k] = row.count(i) == 0 ? 0.0f : g.at(k);
             dgamma[u][k] = dbeta[u][k] = 0.0f;
+        }
     }
-    int turn = 0;
     for (int64_t r0 = (int64_t)blockIdx.x * TEAMS; r0 < a.rows; r0 += (int64_t)gridDim.x * TEAMS, turn ^= 1) {
         const bool mine = r0 + team < a.rows;
         const int64_t r = mine ? r0 + team : a.rows - 1, at = r * a.cols;
-        uint4 h[P], dy[P], dres[RES ? P : 1];
+        Piece<V> h[P], dy[P], dres[RES ? P : 1];
+        if constexpr (!AHEAD)
+            request(r0);
 #pragma unroll
         for (int u = 0; u < P; ++u) {
-            h[u] = row.load(a.h + at, first + lane + u * T * kWave);
-            dy[u] = row.load(a.dy + at, first + lane + u * T * kWave);
+            h[u] = nh[u], dy[u] = ndy[u];
             if constexpr (RES)
-                dres[u] = row.load(a.dres + at, first + lane + u * T * kWave);
+                dres[u] = ndres[u];
         }
-        const double mean = a.stats[2 * r];
-        const float mean_hi = (float)mean, mean_lo = (float)(mean - (double)mean_hi), rstd = (float)a.stats[2 * r + 1];
-        float c1 = 0.0f, c2 = 0.0f;  // mean(w xhat), mean(w)
-        if constexpr (SLAB) {
-            c2 = a.sums[2 * r];
-            c1 = a.sums[2 * r + 1];
-        }
+        const double mean = nmean;
+        const float mean_hi = (float)mean, rstd = (float)nrstd, shift = (float)(mean - (double)mean_hi) * -rstd;
+        if (AHEAD && r0 + (int64_t)gridDim.x * TEAMS < a.rows)
+            request(r0 + (int64_t)gridDim.x * TEAMS);
+        float c1 = 0.0f, c2 = 0.0f;  // sums of w xhat, w; then their means
+        float xhat[P][V], w[P][V];
 #pragma unroll
         for (int u = 0; u < P; ++u)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float xhat = ((element(h[u], k) - mean_hi) - mean_lo) * rstd, d = element(dy[u], k);
+            for (int k = 0; k < V; ++k) {
+                xhat[u][k] = __builtin_fmaf(h[u].at(k) - mean_hi, rstd, shift);
+                const float d = dy[u].at(k);
+                w[u][k] = d * gamma[u][k];
                 if constexpr (!SLAB) {
-                    const float w = d * element(gamma[u], k);
-                    c2 += w;
-                    c1 = __builtin_fmaf(w, xhat, c1);
+                    c2 += w[u][k];
+                    c1 = __builtin_fmaf(w[u][k], xhat[u][k], c1);
                 }
                 if (mine) {
-                    dgamma[u][k] = __builtin_fmaf(d, xhat, dgamma[u][k]);
+                    dgamma[u][k] = __builtin_fmaf(d, xhat[u][k], dgamma[u][k]);
                     dbeta[u][k] += d;
                 }
             }
-        if constexpr (!SLAB) {
+        if constexpr (SLAB) {
+            c2 = a.sums[2 * r];
+            c1 = a.sums[2 * r + 1];
+        } else {
             c1 = dpp_sum(c1);
             c2 = dpp_sum(c2);
             if constexpr (T > 1) {
@@ -346,8 +449,8 @@ __global__ __launch_bounds__(WAVES *kWave) void ln_bwd_kernel(LnBwdArgs a)
                 __syncthreads();
                 c1 = c2 = 0.0f;
 #pragma unroll
-                for (int w = 0; w < T; ++w) {
-                    const float2 v = red[turn][team * T + w];
+                for (int t = 0; t < T; ++t) {
+                    const float2 v = red[turn][team * T + t];
                     c1 += v.x;
                     c2 += v.y;
                 }
@@ -357,53 +460,54 @@ __global__ __launch_bounds__(WAVES *kWave) void ln_bwd_kernel(LnBwdArgs a)
         }
         if (!mine)
             continue;
+        const float k1 = -c1 * rstd, k2 = -c2 * rstd;
 #pragma unroll
         for (int u = 0; u < P; ++u) {
-            uint32_t out[4];
+            Piece<V> out;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < V / 2; ++k) {
                 float v[2];
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const float xhat = ((element(h[u], 2 * k + j) - mean_hi) - mean_lo) * rstd;
-                    const float w = element(dy[u], 2 * k + j) * element(gamma[u], 2 * k + j);
-                    v[j] = rstd * (w - c2 - xhat * c1);
+                    v[j] = __builtin_fmaf(xhat[u][2 * k + j], k1, __builtin_fmaf(w[u][2 * k + j], rstd, k2));
                     if constexpr (RES)
-                        v[j] += element(dres[u], 2 * k + j);
+                        v[j] += dres[u].at(2 * k + j);
                 }
-                out[k] = pack_bf16x2(v[0], v[1]);
+                out.w[k] = pack_bf16x2(v[0], v[1]);
             }
-            row.store(a.dx + at, first + lane + u * T * kWave, make_uint4(out[0], out[1], out[2], out[3]));
+            row.store(a.dx + at, first + lane + u * T * kWave, out);
         }
     }
-    // the teams' column sums, one team after the other
-    __shared__ float sums[TEAMS > 1 ? T * P * kWave * 8 : 1];
-    float *out = a.partials + (int64_t)blockIdx.x * 2 * a.cols;
+    // the teams' column sums through LDS, then added in the teams' order, four columns a thread
+    __shared__ float sums[TEAMS][P * V][T * kWave];
+    const int stride = (a.cols + 3) & ~3;
+    float *out = a.partials + (int64_t)blockIdx.x * 2 * stride;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
-        for (int t = 0; TEAMS > 1 && t < TEAMS; ++t) {
+        if (which)
             __syncthreads();
-            if (team == t)
 #pragma unroll
-                for (int u = 0; u < P; ++u)
+        for (int u = 0; u < P; ++u)
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        float *at = &sums[(u * 8 + k) * T * kWave + lane];
-                        float &v = which ? dbeta[u][k] : dgamma[u][k];
-                        if (t > 0)
-                            v += *at;
-                        *at = v;
-                    }
+            for (int k = 0; k < V; ++k)
+                sums[team][u * V + k][lane] = which ? dbeta[u][k] : dgamma[u][k];
+        __syncthreads();
+        constexpr int QUADS = T * P * kWave * V / 4;
+#pragma unroll
+        for (int q0 = 0; q0 < QUADS; q0 += WAVES * kWave) {
+            const int q = q0 + (int)threadIdx.x, l = q % (T * kWave), part = q / (T * kWave);
+            if (QUADS % (WAVES * kWave) != 0 && q >= QUADS)
+                break;
+            const int col = V * (first + l + part / (V / 4) * T * kWave) + part % (V / 4) * 4;
+            float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int t = 0; t < TEAMS; ++t)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    v[k] += sums[t][part * 4 + k][l];
+            if (col < a.cols)
+                *(float4 *)(out + (int64_t)which * stride + col) = make_float4(v[0], v[1], v[2], v[3]);
         }
-        if (team == TEAMS - 1)
-#pragma unroll
-            for (int u = 0; u < P; ++u) {
-                const int i = first + lane + u * T * kWave, n = row.count(i);
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (k < n)
-                        out[(int64_t)which * a.cols + 8 * (int64_t)i + k] = which ? dbeta[u][k] : dgamma[u][k];
-            }
     }
 }
 
@@ -413,17 +517,17 @@ __global__ __launch_bounds__(kWideThreads) void ln_bwd_sums_kernel(LnBwdArgs a)
 {
     constexpr int T = kWideThreads / kWave;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const Row<RAGGED> row(a.cols);
+    const Row<8, RAGGED> row(a.cols);
     __shared__ double red[2][T];
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const double mean = a.stats[2 * r];
-        const float mean_hi = (float)mean, mean_lo = (float)(mean - (double)mean_hi), rstd = (float)a.stats[2 * r + 1];
+        const float mean_hi = (float)mean, rstd = (float)a.stats[2 * r + 1], shift = (float)(mean - (double)mean_hi) * -rstd;
         float c1 = 0.0f, c2 = 0.0f;
         for (int i = threadIdx.x; i < row.pieces; i += kWideThreads) {
-            const uint4 h = row.load(a.h + r * a.cols, i), dy = row.load(a.dy + r * a.cols, i), g = row.load(a.gamma, i);
+            const Piece<8> h = row.load(a.h + r * a.cols, i), dy = row.load(a.dy + r * a.cols, i), g = row.load(a.gamma, i);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const float xhat = ((element(h, k) - mean_hi) - mean_lo) * rstd, w = element(dy, k) * element(g, k);
+                const float xhat = __builtin_fmaf(h.at(k) - mean_hi, rstd, shift), w = dy.at(k) * g.at(k);
                 c2 += w;
                 c1 = __builtin_fmaf(w, xhat, c1);
             }
@@ -436,67 +540,85 @@ __global__ __launch_bounds__(kWideThreads) void ln_bwd_sums_kernel(LnBwdArgs a)
     }
 }
 
-// Adds the workgroups' partial sums in their order: a wave takes 64 columns of one of the two gradients and every 16th row of
-// partials, then the 16 waves' sums are added, all in fp64.
-constexpr int kColsumWaves = 16;
+// Adds the workgroups' partial sums: a workgroup takes 4 * kFinLanes columns of one of the two gradients, four a lane, its groups of
+// lanes every 128th row of partials, whose sums are then added in their order, all in fp64.  (Lines of 128 B a workgroup, so that there are enough
+// workgroups: 512 rows of 768 columns 4.2 us, of 256 B 5.0; a wave 64 columns 10.8.)
+constexpr int kFinLanes = 8, kFinThreads = 1024, kFinRows = kFinThreads / kFinLanes;
 
-__global__ __launch_bounds__(kColsumWaves *kWave) void ln_bwd_finish_kernel(const float *__restrict__ partials, int groups, int cols,
-                                                                            float *__restrict__ dgamma, float *__restrict__ dbeta)
+__global__ __launch_bounds__(kFinThreads) void ln_bwd_finish_kernel(const float *__restrict__ partials, int groups, int cols,
+                                                                    float *__restrict__ dgamma, float *__restrict__ dbeta)
 {
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, which = blockIdx.y;
-    const int c = (int)blockIdx.x * kWave + lane;
-    double s = 0.0;
-    if (c < cols)
-        for (int g = wave; g < groups; g += kColsumWaves)
-            s += (double)partials[((int64_t)g * 2 + which) * cols + c];
-    __shared__ double red[kColsumWaves][kWave];
-    red[wave][lane] = s;
-    __syncthreads();
-    if (wave == 0 && c < cols) {
+    const int lane = threadIdx.x % kFinLanes, part = threadIdx.x / kFinLanes, which = blockIdx.y;
+    const int stride = (cols + 3) & ~3, c = ((int)blockIdx.x * kFinLanes + lane) * 4;
+    double s[4] = {0.0, 0.0, 0.0, 0.0};
+    if (c < cols) {
+        const float *p = partials + (int64_t)which * stride + c;
+#pragma unroll 8
+        for (int g = part; g < groups; g += kFinRows) {
+            const float4 v = *(const float4 *)(p + (int64_t)g * 2 * stride);
+            s[0] += (double)v.x, s[1] += (double)v.y, s[2] += (double)v.z, s[3] += (double)v.w;
+        }
+    }
+    __shared__ double red[kFinRows][kFinLanes * 4 + 1];
 #pragma unroll
-        for (int w = 1; w < kColsumWaves; ++w)
-            s += red[w][lane];
-        (which ? dbeta : dgamma)[c] = (float)s;
+    for (int k = 0; k < 4; ++k)
+        red[part][lane * 4 + k] = s[k];
+    __syncthreads();
+    const int col = (int)blockIdx.x * kFinLanes * 4 + (int)threadIdx.x;
+    if (threadIdx.x < kFinLanes * 4 && col < cols) {
+        double t = red[0][threadIdx.x];
+        for (int w = 1; w < kFinRows; ++w)
+            t += red[w][threadIdx.x];
+        (which ? dbeta : dgamma)[col] = (float)t;
     }
 }
 
-// what a backward call runs on
+// What a backward call runs on: T, P, V and WAVES of the kernel, the fewest lanes that hold a row.
 struct BwdShape {
-    int waves_a_row, pieces, waves;  // T, P, WAVES of the kernel
-    bool wide;                       // rows longer than T * P * 512 elements
+    int waves_a_row, pieces, elements, waves;
+    bool wide;
 };
 
 BwdShape bwd_shape(int64_t cols)
 {
-    const int64_t pieces = (cols + 7) / 8;
-    if (pieces <= kWave)
-        return {1, 1, 8, false};
-    if (pieces <= 2 * kWave)
-        return {1, 2, 8, false};
-    if (pieces <= 4 * kWave)
-        return {2, 2, 8, false};
-    if (pieces <= 8 * kWave)
-        return {4, 2, 8, false};
-    return {8, 2, 8, pieces > 16 * kWave};
+    if (cols <= 256)
+        return {1, 1, 4, 8, false};
+    if (cols <= 512)
+        return {1, 1, 8, 8, false};
+    if (cols <= 768)
+        return {1, 3, 4, 8, false};
+    if (cols <= 1024)
+        return {2, 1, 8, 8, false};
+    if (cols <= 1536)
+        return {2, 3, 4, 8, false};
+    if (cols <= 2048)
+        return {4, 1, 8, 8, false};
+    if (cols <= 4096)
+        return {8, 1, 8, 8, false};
+    return {16, 1, 8, 16, cols > 8192};
 }
 
 // workgroups, each of which leaves a row of partial sums; of wide rows so many for each slab of columns
 int bwd_groups(int64_t rows, int64_t cols, const BwdShape &b)
 {
-    const int64_t teams = b.waves / b.waves_a_row, slab = (int64_t)b.waves_a_row * b.pieces * kWave * 8;
-    const int64_t slabs = b.wide ? (cols + slab - 1) / slab : 1;
-    return (int)std::min<int64_t>((rows + teams - 1) / teams, std::max<int64_t>(1, 2 * kCus / slabs));
+    const int64_t teams = b.waves / b.waves_a_row, slab = (int64_t)b.waves_a_row * b.pieces * kWave * b.elements;
+    const int64_t slabs = b.wide ? (cols + slab - 1) / slab : 1, most = 16 * kCus / b.waves;
+    return (int)std::min<int64_t>((rows + teams - 1) / teams, std::max<int64_t>(1, most / slabs));
 }
 
-template <int T, int P, int WAVES, bool SLAB = false>
+size_t partial_floats(int64_t cols, int groups) { return (size_t)groups * 2 * (size_t)((cols + 3) / 4 * 4); }
+
+template <int T, int P, int V, int WAVES, bool SLAB = false>
 void launch_bwd(const LnBwdArgs &a, int groups, hipStream_t s)
 {
-    const unsigned slabs = SLAB ? (unsigned)((a.cols + T * P * kWave * 8 - 1) / (T * P * kWave * 8)) : 1u;
+    const unsigned slabs = SLAB ? (unsigned)((a.cols + T * P * kWave * V - 1) / (T * P * kWave * V)) : 1u;
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)groups, slabs), dim3(WAVES * kWave), 0, s, a); };
-    if (a.cols % 8 != 0)
-        a.dres ? go(ln_bwd_kernel<T, P, WAVES, true, true, SLAB>) : go(ln_bwd_kernel<T, P, WAVES, false, true, SLAB>);
+    if (a.cols % V != 0)
+        a.dres ? go(ln_bwd_kernel<T, P, V, WAVES, true, true, SLAB, false>) : go(ln_bwd_kernel<T, P, V, WAVES, false, true, SLAB, false>);
+    else if (a.rows * a.cols * (a.dres ? 8 : 6) > kKeptBytes)
+        a.dres ? go(ln_bwd_kernel<T, P, V, WAVES, true, false, SLAB, true>) : go(ln_bwd_kernel<T, P, V, WAVES, false, false, SLAB, true>);
     else
-        a.dres ? go(ln_bwd_kernel<T, P, WAVES, true, false, SLAB>) : go(ln_bwd_kernel<T, P, WAVES, false, false, SLAB>);
+        a.dres ? go(ln_bwd_kernel<T, P, V, WAVES, true, false, SLAB, false>) : go(ln_bwd_kernel<T, P, V, WAVES, false, false, SLAB, false>);
 }
 
 }  // namespace
@@ -506,19 +628,25 @@ hipError_t launch_layernorm_fwd(const void *x, const void *res, const void *gamm
 {
     const LnFwdArgs a{(const uint16_t *)x, (const uint16_t *)res, (const uint16_t *)gamma, (const uint16_t *)beta, (uint16_t *)h_out,
                       (uint16_t *)y, stats, rows, (int)cols, eps};
-    const int64_t pieces = (cols + 7) / 8;
-    if (pieces <= kWave)
-        launch_fwd<1, 1>(a, s);
-    else if (pieces <= 2 * kWave)
-        launch_fwd<1, 2>(a, s);
-    else if (pieces <= 4 * kWave)
-        launch_fwd<2, 2>(a, s);
-    else if (pieces <= 8 * kWave)
-        launch_fwd<4, 2>(a, s);
-    else if (pieces <= 16 * kWave)
-        launch_fwd<8, 2>(a, s);
-    else if (pieces <= 32 * kWave)
-        launch_fwd<8, 4>(a, s);
+    // the fewest lanes that hold a row with up to 16 elements each (two pieces of eight a lane are better than twice the waves: 2048 wide 53.9 us, 59.5)
+    if (cols <= 256)
+        launch_fwd<1, 1, 4, 4>(a, s);
+    else if (cols <= 512)
+        launch_fwd<1, 1, 8, 4>(a, s);
+    else if (cols <= 768)
+        launch_fwd<1, 3, 4, 4>(a, s);
+    else if (cols <= 1024)
+        launch_fwd<1, 2, 8, 4>(a, s);
+    else if (cols <= 1536)
+        launch_fwd<2, 3, 4, 4>(a, s);
+    else if (cols <= 2048)
+        launch_fwd<2, 2, 8, 4>(a, s);
+    else if (cols <= 4096)
+        launch_fwd<4, 2, 8, 4>(a, s);
+    else if (cols <= 8192)
+        launch_fwd<8, 2, 8, 8>(a, s);
+    else if (cols <= 16384)
+        launch_fwd<16, 2, 8, 16>(a, s);
     else {
         auto go = [&](auto kernel) {
             hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(rows, 4 * kCus)), dim3(kWideThreads), 0, s, a);
@@ -534,7 +662,7 @@ hipError_t launch_layernorm_fwd(const void *x, const void *res, const void *gamm
 size_t layernorm_bwd_bytes(int64_t rows, int64_t cols)
 {
     const BwdShape b = bwd_shape(cols);
-    return ((size_t)bwd_groups(rows, cols, b) * 2 * (size_t)cols + (b.wide ? 2 * (size_t)rows : 0)) * sizeof(float);
+    return (partial_floats(cols, bwd_groups(rows, cols, b)) + (b.wide ? 2 * (size_t)rows : 0)) * sizeof(float);
 }
 
 hipError_t launch_layernorm_bwd(const void *dy, const void *h, const void *gamma, const double *stats, const void *dres, int64_t rows,
@@ -542,7 +670,7 @@ hipError_t launch_layernorm_bwd(const void *dy, const void *h, const void *gamma
 {
     const BwdShape b = bwd_shape(cols);
     const int groups = bwd_groups(rows, cols, b);
-    float *partials = (float *)workspace, *sums = partials + (size_t)groups * 2 * (size_t)cols;
+    float *partials = (float *)workspace, *sums = partials + partial_floats(cols, groups);
     const LnBwdArgs a{(const uint16_t *)dy, (const uint16_t *)h, (const uint16_t *)gamma, (const uint16_t *)dres, stats,
                       (uint16_t *)dx, partials, sums, rows, (int)cols};
     if (b.wide) {
@@ -554,21 +682,24 @@ hipError_t launch_layernorm_bwd(const void *dy, const void *h, const void *gamma
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess)
             return e;
-        launch_bwd<8, 2, 8, true>(a, groups, s);
-    } else if (b.waves_a_row == 1) {
-        b.pieces == 1 ? launch_bwd<1, 1, 8>(a, groups, s) : launch_bwd<1, 2, 8>(a, groups, s);
-    } else if (b.waves_a_row == 2) {
-        launch_bwd<2, 2, 8>(a, groups, s);
-    } else if (b.waves_a_row == 4) {
-        launch_bwd<4, 2, 8>(a, groups, s);
+        launch_bwd<16, 1, 8, 16, true>(a, groups, s);
     } else {
-        launch_bwd<8, 2, 8>(a, groups, s);
+        switch (b.waves_a_row * 100 + b.pieces * 10 + b.elements) {
+        case 114: launch_bwd<1, 1, 4, 8>(a, groups, s); break;
+        case 118: launch_bwd<1, 1, 8, 8>(a, groups, s); break;
+        case 134: launch_bwd<1, 3, 4, 8>(a, groups, s); break;
+        case 218: launch_bwd<2, 1, 8, 8>(a, groups, s); break;
+        case 234: launch_bwd<2, 3, 4, 8>(a, groups, s); break;
+        case 418: launch_bwd<4, 1, 8, 8>(a, groups, s); break;
+        case 818: launch_bwd<8, 1, 8, 8>(a, groups, s); break;
+        default: launch_bwd<16, 1, 8, 16>(a, groups, s); break;
+        }
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess)
         return e;
-    hipLaunchKernelGGL(ln_bwd_finish_kernel, dim3((unsigned)((cols + kWave - 1) / kWave), dbeta != nullptr ? 2 : 1),
-                       dim3(kColsumWaves * kWave), 0, s, partials, groups, (int)cols, dgamma, dbeta);
+    hipLaunchKernelGGL(ln_bwd_finish_kernel, dim3((unsigned)((cols + 4 * kFinLanes - 1) / (4 * kFinLanes)), dbeta != nullptr ? 2 : 1),
+                       dim3(kFinThreads), 0, s, partials, groups, (int)cols, dgamma, dbeta);
     return hipGetLastError();
 }
 
