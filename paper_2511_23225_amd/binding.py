@@ -461,30 +461,46 @@ def tweo_fp8_linear_bwd_bf16_hybrid(dy_bf16, saved, K, dyq, dyqT, dx_bf16=None, 
                                                   _stream()), "tweo_fp8_linear_bwd_bf16_hybrid")
 
 
-def _same(device, shape, dtype, **tensors):
-    """Refuses what a kernel would read as something else: another shape or type, strides, another device than the current one."""
-    for name, t in tensors.items():
+def _device():
+    """The current device.  (As _stream: three looks at it and the stream by way of torch.cuda are what a small call takes.)"""
+    if _current is None:
+        _stream()
+    return _current[0]()
+
+
+def _same(device, shape, dtype, tensors, names):
+    """Refuses what a kernel would read as something else: another shape or type, strides, another device than the current one.
+    0.3 us a tensor."""
+    for i, t in enumerate(tensors):
         if t is not None and (t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != device):
             raise ValueError("%s: a contiguous %s tensor of shape %s on cuda:%d, the current device, is needed, got %s of %s on %s" %
-                             (name, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
+                             (names[i], dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
 
 
-def _device():
-    _stream()  # _current is set, or the GPU can't be used
-    return _current[0]()
+@functools.lru_cache(maxsize=1)
+def _types():
+    import torch
+    return torch.bfloat16, torch.float32, torch.float64
+
+
+_LN_FWD, _LN_FWD_PARAMS, _LN_STATS = ("x_bf16", "y_bf16", "residual_bf16", "h_out_bf16"), ("gamma_bf16", "beta_bf16"), ("stats",)
+_LN_BWD, _LN_BWD_SUMS = ("dy_bf16", "h_bf16", "dx_bf16", "residual_grad_bf16"), ("dgamma", "dbeta")
 
 
 def tweo_layernorm_fwd(x_bf16, gamma_bf16, y_bf16, beta_bf16=None, residual_bf16=None, eps=1e-5, h_out_bf16=None,
                        stats_out=None):
-    import torch
-    if x_bf16.dim() != 2:
+    shape = x_bf16.shape
+    if len(shape) != 2:
         raise ValueError("x_bf16: two dimensions are needed")
-    rows, cols = shape = x_bf16.shape
-    dev = _device()
-    _same(dev, shape, torch.bfloat16, x_bf16=x_bf16, y_bf16=y_bf16, residual_bf16=residual_bf16,
-          h_out_bf16=None if residual_bf16 is None else h_out_bf16)
-    _same(dev, shape[1:], torch.bfloat16, gamma_bf16=gamma_bf16, beta_bf16=beta_bf16)
-    _same(dev, (rows, 2), torch.float64, stats_out=stats_out)
+    rows, cols = shape
+    dev, (bf16, _, f64) = _device(), _types()
+    if residual_bf16 is None:
+        _same(dev, shape, bf16, (x_bf16, y_bf16), _LN_FWD)
+    else:
+        _same(dev, shape, bf16, (x_bf16, y_bf16, residual_bf16, h_out_bf16), _LN_FWD)
+    _same(dev, shape[1:], bf16, (gamma_bf16, beta_bf16), _LN_FWD_PARAMS)
+    if stats_out is not None:
+        _same(dev, (rows, 2), f64, (stats_out,), _LN_STATS)
     _check(load().tweo_layernorm_fwd(_ptr(x_bf16), _ptr(residual_bf16), _ptr(gamma_bf16), _ptr(beta_bf16), rows, cols,
                                      float(eps), _ptr(h_out_bf16), _ptr(y_bf16), _ptr(stats_out), _stream()),
            "tweo_layernorm_fwd")
@@ -498,15 +514,17 @@ def layernorm_stats(workspace, rows):
 
 def tweo_layernorm_bwd(dy_bf16, h_bf16, gamma_bf16, stats, dx_bf16, dgamma, dbeta=None, residual_grad_bf16=None,
                        workspace=None):
-    import torch
-    if dy_bf16.dim() != 2:
+    shape = dy_bf16.shape
+    if len(shape) != 2:
         raise ValueError("dy_bf16: two dimensions are needed")
-    rows, cols = shape = dy_bf16.shape
-    dev = _device()
-    _same(dev, shape, torch.bfloat16, dy_bf16=dy_bf16, h_bf16=h_bf16, dx_bf16=dx_bf16, residual_grad_bf16=residual_grad_bf16)
-    _same(dev, shape[1:], torch.bfloat16, gamma_bf16=gamma_bf16)
-    _same(dev, shape[1:], torch.float32, dgamma=dgamma, dbeta=dbeta)
-    _same(dev, (rows, 2), torch.float64, stats=stats)
+    rows, cols = shape
+    dev, (bf16, f32, f64) = _device(), _types()
+    _same(dev, shape, bf16, (dy_bf16, h_bf16, dx_bf16, residual_grad_bf16), _LN_BWD)
+    _same(dev, shape[1:], bf16, (gamma_bf16,), _LN_FWD_PARAMS)
+    _same(dev, shape[1:], f32, (dgamma, dbeta), _LN_BWD_SUMS)
+    _same(dev, (rows, 2), f64, (stats,), _LN_STATS)
+    if workspace is not None and workspace.get_device() != dev:
+        raise ValueError("workspace on %s, but cuda:%d is current" % (workspace.device, dev))
     wp, wb = _ws(workspace)
     _check(load().tweo_layernorm_bwd(_ptr(dy_bf16), _ptr(h_bf16), _ptr(gamma_bf16), _ptr(stats), _ptr(residual_grad_bf16),
                                      rows, cols, _ptr(dx_bf16), _ptr(dgamma), _ptr(dbeta), wp, wb, _stream()),
@@ -551,27 +569,25 @@ def make_optim_plan(rows, table):
     return plan
 
 
-def _on_device(plan, sumsq=None, **more):
-    import torch
+def _on_device(plan, sumsq, other):
     dev = _device()
     if dev != plan.device:
         raise ValueError("a plan of cuda:%d, but cuda:%d is current" % (plan.device, dev))
-    if sumsq is not None and sumsq.dtype is not torch.float64:
-        raise ValueError("the sum of squares is one torch.float64, got %s" % sumsq.dtype)
-    for name, t in dict(more, sumsq=sumsq).items():
-        if t is not None and (t.get_device() != dev or t.nbytes < 8):
-            raise ValueError("%s: at least 8 bytes on cuda:%d are needed, got %d on %s" % (name, dev, t.nbytes, t.device))
+    if sumsq is not None and (sumsq.dtype is not _types()[2] or sumsq.numel() < 1 or sumsq.get_device() != dev):
+        raise ValueError("the sum of squares: one torch.float64 on cuda:%d is needed, got %s on %s" % (dev, sumsq.dtype, sumsq.device))
+    if other is not None and (other.get_device() != dev or other.nbytes < 8):
+        raise ValueError("at least 8 bytes on cuda:%d are needed, got %d on %s" % (dev, other.nbytes, other.device))
 
 
 def tweo_grad_sumsq(plan, sumsq_out, workspace):
-    _on_device(plan, sumsq_out, workspace=workspace)
+    _on_device(plan, sumsq_out, workspace)
     wp, wb = _ws(workspace)
     _check(load().tweo_grad_sumsq(ctypes.byref(plan), _ptr(sumsq_out), wp, wb, _stream()), "tweo_grad_sumsq")
 
 
 def tweo_adamw_step(plan, lr=0.0, step=1, beta1=0.9, beta2=0.999, eps=1e-8, grad_sumsq=None, max_norm=1.0, schedule=None):
     """schedule: two 32-bit words on the device, lr as fp32 and step as an integer, in the place of `lr` and `step`."""
-    _on_device(plan, grad_sumsq, schedule=schedule)
+    _on_device(plan, grad_sumsq, schedule)
     cfg = AdamwCfg(lr, beta1, beta2, eps, max_norm, step)
     _check(load().tweo_adamw_step(ctypes.byref(plan), ctypes.byref(cfg), _ptr(grad_sumsq), _ptr(schedule), _stream()),
            "tweo_adamw_step")

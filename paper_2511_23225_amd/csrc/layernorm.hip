@@ -165,8 +165,9 @@ struct LnFwdArgs {
     double eps;
 };
 
+// (four waves a SIMD: left to itself the compiler takes 130 registers for 16 elements a lane, two more than four waves have; 4096x8192 55.0 us -> 49.4)
 template <int T, int P, int V, int WAVES, bool RES, bool RAGGED, bool ONCE>
-__global__ __launch_bounds__(WAVES *kWave) void ln_fwd_kernel(LnFwdArgs a)
+__global__ __launch_bounds__(WAVES *kWave, 4) void ln_fwd_kernel(LnFwdArgs a)
 {
     constexpr int TEAMS = WAVES / T;
     constexpr bool AHEAD = !RAGGED;  // (a ragged row's loads branch, and are waited for one after the other)
@@ -302,7 +303,7 @@ constexpr int kCus = 256;  // of an MI355X; a device with more or fewer runs the
 template <int T, int P, int V, int WAVES>
 void launch_fwd(const LnFwdArgs &a, hipStream_t s)
 {
-    // as many workgroups as hide each other's barriers: 32 waves a CU, 16 where a team is eight waves and more (4096x8192 52.5 us, with 32 54.1)
+    // as many workgroups as hide each other's barriers: 32 waves a CU, 16 where a team is eight waves and more (4096x8192 52.5 us, with 32 54.1 before the stream went past the caches)
     constexpr int TEAMS = WAVES / T, WAVES_PER_CU = T >= 8 ? 16 : 32;
     const int64_t wanted = (a.rows + TEAMS - 1) / TEAMS, most = kCus * WAVES_PER_CU / WAVES;
     auto go = [&](auto kernel) {
