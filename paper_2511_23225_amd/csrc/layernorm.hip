@@ -11,7 +11,7 @@ namespace {
 // ---------------------------------------------------------------------------
 // A row is worked on by a team of T waves; lane l of the team holds the pieces l, l + 64 T, ... of it, P of them, V elements (4 or 8:
 // 8 or 16 bytes) each, in registers.  RAGGED: cols is no multiple of V, so that rows start at any even address and their last piece is
-// short.  ONCE: past the caches.
+// short; what they cost is accesses that straddle lines (16384x2041 forward 63 us, 2048 wide 49; backward 66 and 51).  ONCE: past the caches.
 
 template <int V>
 struct Piece {
@@ -37,38 +37,49 @@ struct Row {
         const int left = cols - V * i;
         return left < 0 ? 0 : left < V ? left : V;
     }
-    // A lane without a piece gets the row's last one: with a branch around each load the compiler waits for one before it issues the
-    // next.  (Of a ragged row only pieces that are whole are loaded this way.)
-    template <bool ONCE>
-    __device__ __forceinline__ Piece<V> whole(const uint16_t *p, int i) const
+    // whether one of the 64 T pieces from i0 on is a ragged row's short one (the same for all lanes)
+    template <int T>
+    __device__ __forceinline__ bool ends(int i0) const
     {
-        const int last = pieces - 1, j = RAGGED || i < last ? i : last;
-        const vec *q = (const vec *)((const uint8_t *)p + (uint64_t)((uint32_t)j * (2u * V)));
-        const vec v = ONCE ? __builtin_nontemporal_load(q) : *q;
+        return RAGGED && pieces > i0 && pieces <= i0 + T * kWave;
+    }
+    // Piece i, zeros behind a ragged row's end.  Without branches, around which the compiler would wait for one load before it issues the
+    // next (4096x4093 backward 60.4 us, now 44.6): a lane without a piece gets the row's last one, and a short piece is taken from the row's last V elements and shifted down.
+    // `ending`: the pieces that ends() names.
+    template <bool ONCE = false>
+    __device__ __forceinline__ Piece<V> load(const uint16_t *p, int i, bool ending) const
+    {
         Piece<V> r;
+        if (RAGGED && cols < V) {
+            const int n = count(i);
+            uint32_t e[V];
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                e[k] = k < n ? p[k] : 0u;
+#pragma unroll
+            for (int k = 0; k < V / 2; ++k)
+                r.w[k] = e[2 * k] | e[2 * k + 1] << 16;
+            return r;
+        }
+        const int last = RAGGED ? cols - V : cols / V * V - V, at = V * i < last ? V * i : last;  // (elements)
+        const vec *q = (const vec *)((const uint8_t *)p + (uint64_t)((uint32_t)at * 2u));
+        const vec v = ONCE ? __builtin_nontemporal_load(q) : *q;
 #pragma unroll
         for (int k = 0; k < V / 2; ++k)
             r.w[k] = v[k];
-        return r;
-    }
-    // a ragged row's last piece, or none: zeros behind the end
-    __device__ __forceinline__ Piece<V> rest(const uint16_t *p, int i) const
-    {
-        const int n = count(i);
-        uint32_t e[V];
+        if (RAGGED && ending) {
+            const int by = i == pieces - 1 ? V * i - at : 0;
+            const uint32_t half = by & 1 ? 16 : 0;
 #pragma unroll
-        for (int k = 0; k < V; ++k)
-            e[k] = k < n ? p[V * (int64_t)i + k] : 0u;
-        Piece<V> r;
+            for (int k = 0; k < V / 2; ++k)
+                r.w[k] = __builtin_amdgcn_alignbit(k + 1 < V / 2 ? r.w[k + 1] : 0u, r.w[k], half);
 #pragma unroll
-        for (int k = 0; k < V / 2; ++k)
-            r.w[k] = e[2 * k] | e[2 * k + 1] << 16;
+            for (int step = 1; step < V / 2; step *= 2)
+#pragma unroll
+                for (int k = 0; k < V / 2; ++k)
+                    r.w[k] = by & (2 * step) ? (k + step < V / 2 ? r.w[k + step] : 0u) : r.w[k];
+        }
         return r;
-    }
-    template <bool ONCE = false>
-    __device__ __forceinline__ Piece<V> load(const uint16_t *p, int i) const
-    {
-        return !RAGGED || count(i) == V ? whole<ONCE>(p, i) : rest(p, i);
     }
     template <bool ONCE = false>
     __device__ __forceinline__ void store(uint16_t *p, int i, const Piece<V> &v) const
@@ -170,7 +181,7 @@ template <int T, int P, int V, int WAVES, bool RES, bool RAGGED, bool ONCE>
 __global__ __launch_bounds__(WAVES *kWave, 4) void ln_fwd_kernel(LnFwdArgs a)
 {
     constexpr int TEAMS = WAVES / T;
-    constexpr bool AHEAD = !RAGGED;  // (a ragged row's loads branch, and are waited for one after the other)
+    constexpr bool AHEAD = !RAGGED;  // (ragged rows: 16384x2041 80 us with it, 63 without)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), team = wave / T;
     const int lane = (int)threadIdx.x - team * T * kWave;
     const Row<V, RAGGED> row(a.cols);
@@ -182,9 +193,10 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void ln_fwd_kernel(LnFwdArgs a)
         const int64_t r = r0 + team < a.rows ? r0 + team : a.rows - 1, at = r * a.cols;
 #pragma unroll
         for (int u = 0; u < P; ++u) {
-            nx[u] = row.template load<ONCE>(a.x + at, lane + u * T * kWave);
+            const bool ending = row.template ends<T>(u * T * kWave);
+            nx[u] = row.template load<ONCE>(a.x + at, lane + u * T * kWave, ending);
             if constexpr (RES)
-                nr[u] = row.template load<ONCE>(a.res + at, lane + u * T * kWave);
+                nr[u] = row.template load<ONCE>(a.res + at, lane + u * T * kWave, ending);
         }
     };
     if (AHEAD && (int64_t)blockIdx.x * TEAMS < a.rows)
@@ -193,10 +205,11 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void ln_fwd_kernel(LnFwdArgs a)
 #pragma unroll
     for (int u = 0; u < P; ++u) {
         const int i = lane + u * T * kWave;
-        const Piece<V> g = row.load(a.gamma, i);
+        const bool ending = row.template ends<T>(u * T * kWave);
+        const Piece<V> g = row.load(a.gamma, i, ending);
         Piece<V> b{};
         if (a.beta != nullptr)
-            b = row.load(a.beta, i);
+            b = row.load(a.beta, i, ending);
 #pragma unroll
         for (int k = 0; k < V; ++k)
             gamma[u][k] = g.at(k), beta[u][k] = b.at(k);
@@ -265,9 +278,9 @@ __global__ __launch_bounds__(kWideThreads) void ln_fwd_wide_kernel(LnFwdArgs a)
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         double s = 0.0;
         for (int i = threadIdx.x; i < row.pieces; i += kWideThreads) {
-            Piece<8> v = row.load(a.x + r * a.cols, i);
+            Piece<8> v = row.load(a.x + r * a.cols, i, true);
             if constexpr (RES) {
-                v = sum_of(v, row.load(a.res + r * a.cols, i));
+                v = sum_of(v, row.load(a.res + r * a.cols, i, true));
                 row.store(a.h + r * a.cols, i, v);
             }
             s += sum64(v);
@@ -277,17 +290,17 @@ __global__ __launch_bounds__(kWideThreads) void ln_fwd_wide_kernel(LnFwdArgs a)
         const double mean = team_sum<T>(s, red[0], wave) / n;
         double ss = 0.0;
         for (int i = threadIdx.x; i < row.pieces; i += kWideThreads)
-            ss += squares64<8, RAGGED>(row.load(h, i), mean, row.count(i));
+            ss += squares64<8, RAGGED>(row.load(h, i, true), mean, row.count(i));
         const double rstd = 1.0 / __builtin_sqrt(team_sum<T>(ss, red[1], wave) / n + a.eps);
         if (a.stats != nullptr && threadIdx.x == 0) {
             a.stats[2 * r] = mean;
             a.stats[2 * r + 1] = rstd;
         }
         for (int i = threadIdx.x; i < row.pieces; i += kWideThreads) {
-            const Piece<8> x = row.load(h, i), g = row.load(a.gamma, i);
+            const Piece<8> x = row.load(h, i, true), g = row.load(a.gamma, i, true);
             Piece<8> b{}, y;
             if (a.beta != nullptr)
-                b = row.load(a.beta, i);
+                b = row.load(a.beta, i, true);
             float gamma[8], beta[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k)
@@ -377,17 +390,11 @@ __global__ __launch_bounds__(WAVES *kWave) void ln_bwd_kernel(LnBwdArgs a)
 #pragma unroll
         for (int u = 0; u < P; ++u) {
             const int i = first + lane + u * T * kWave;
-            if (!RAGGED || row.count(i) == V) {
-                nh[u] = row.template whole<ONCE>(a.h + at, i);
-                ndy[u] = row.template whole<ONCE>(a.dy + at, i);
-                if constexpr (RES)
-                    ndres[u] = row.template whole<ONCE>(a.dres + at, i);
-            } else {
-                nh[u] = row.rest(a.h + at, i);
-                ndy[u] = row.rest(a.dy + at, i);
-                if constexpr (RES)
-                    ndres[u] = row.rest(a.dres + at, i);
-            }
+            const bool ending = row.template ends<T>(first + u * T * kWave);
+            nh[u] = row.template load<ONCE>(a.h + at, i, ending);
+            ndy[u] = row.template load<ONCE>(a.dy + at, i, ending);
+            if constexpr (RES)
+                ndres[u] = row.template load<ONCE>(a.dres + at, i, ending);
         }
         nmean = a.stats[2 * r], nrstd = a.stats[2 * r + 1];
     };
@@ -396,11 +403,10 @@ __global__ __launch_bounds__(WAVES *kWave) void ln_bwd_kernel(LnBwdArgs a)
 #pragma unroll
     for (int u = 0; u < P; ++u) {
         const int i = first + lane + u * T * kWave;
-        const Piece<V> g = row.load(a.gamma, i);
+        const Piece<V> g = row.load(a.gamma, i, row.template ends<T>(first + u * T * kWave));
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            // a gain of zero keeps a lane without a piece out of the row's sums (its column sums are not stored)
-            gamma[u][k] = row.count(i) == 0 ? 0.0f : g.at(k);
+            gamma[u][k] = g.at(k);
             dgamma[u][k] = dbeta[u][k] = 0.0f;
         }
     }
@@ -423,21 +429,27 @@ __global__ __launch_bounds__(WAVES *kWave) void ln_bwd_kernel(LnBwdArgs a)
         float c1 = 0.0f, c2 = 0.0f;  // sums of w xhat, w; then their means
         float xhat[P][V], w[P][V];
 #pragma unroll
-        for (int u = 0; u < P; ++u)
+        for (int u = 0; u < P; ++u) {
+            float t1 = 0.0f, t2 = 0.0f;
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 xhat[u][k] = __builtin_fmaf(h[u].at(k) - mean_hi, rstd, shift);
                 const float d = dy[u].at(k);
                 w[u][k] = d * gamma[u][k];
                 if constexpr (!SLAB) {
-                    c2 += w[u][k];
-                    c1 = __builtin_fmaf(w[u][k], xhat[u][k], c1);
+                    t2 += w[u][k];
+                    t1 = __builtin_fmaf(w[u][k], xhat[u][k], t1);
                 }
                 if (mine) {
                     dgamma[u][k] = __builtin_fmaf(d, xhat[u][k], dgamma[u][k]);
                     dbeta[u][k] += d;
                 }
             }
+            // (a lane without a piece has another's; its column sums are not stored)
+            const bool some = row.count(first + lane + u * T * kWave) > 0;
+            c1 += some ? t1 : 0.0f;
+            c2 += some ? t2 : 0.0f;
+        }
         if constexpr (SLAB) {
             c2 = a.sums[2 * r];
             c1 = a.sums[2 * r + 1];
@@ -525,7 +537,7 @@ __global__ __launch_bounds__(kWideThreads) void ln_bwd_sums_kernel(LnBwdArgs a)
         const float mean_hi = (float)mean, rstd = (float)a.stats[2 * r + 1], shift = (float)(mean - (double)mean_hi) * -rstd;
         float c1 = 0.0f, c2 = 0.0f;
         for (int i = threadIdx.x; i < row.pieces; i += kWideThreads) {
-            const Piece<8> h = row.load(a.h + r * a.cols, i), dy = row.load(a.dy + r * a.cols, i), g = row.load(a.gamma, i);
+            const Piece<8> h = row.load(a.h + r * a.cols, i, true), dy = row.load(a.dy + r * a.cols, i, true), g = row.load(a.gamma, i, true);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 const float xhat = __builtin_fmaf(h.at(k) - mean_hi, rstd, shift), w = dy.at(k) * g.at(k);

@@ -53,7 +53,8 @@ def inputs(rows, cols, seed):
 # one token; widths on both sides of every change of the waves a row and the pieces a lane has; odd ones; the re-read paths
 SHAPES = [(1, 1), (3, 2), (2, 7), (5, 8), (4, 9), (1, 2048), (17, 64), (9, 255), (33, 512), (31, 513), (65, 768), (257, 1001), (12, 1024),
           (13, 1025), (40, 1536), (7, 2048), (6, 2049), (11, 4096), (5, 4104), (3, 8192), (4, 8193), (2, 8200), (3, 16384), (2, 16392), (2, 16385),
-          (3, 32776), (2, 33001), (5000, 24), (4099, 768)]
+          (3, 32776), (2, 33001), (5000, 24), (4099, 768), (3, 253), (3, 257),
+          (3, 509), (3, 767), (3, 769), (3, 1023), (3, 1531), (3, 1537), (3, 2047), (3, 4095), (3, 8191), (2, 16383), (300, 8200), (700, 5632)]
 
 
 def forward(t, cols, residual, beta, stats=True, eps=EPS):
@@ -207,6 +208,24 @@ def test_poisoned_rows_stay_by_themselves(cols):
     assert bool(torch.isnan(dgamma).all()) and torch.equal(dbeta, good[2])
 
 
+@pytest.mark.parametrize("cols", [3, 300, 768, 777, 1001, 2048, 4100, 8192, 16392])
+def test_gradients_that_are_not_finite(cols):
+    """Infinities and NaNs wherever they lie in a row: what fp64 arithmetic makes of them, in the same places, and the other rows' bits."""
+    rows = 9
+    t = inputs(rows, cols, 14)
+    stats = training.layernorm_stats(f64(t["x"]), EPS)
+    clean = backward(t, to_dev_bf16(t["x"]), torch.from_numpy(stats).to(DEV))
+    for r, (c, bits) in enumerate(((0, 0x7F80), (cols - 1, 0x7F80), (cols // 2, 0xFF80), (cols - 1, 0xFF80), (cols - 1, 0x7FC0), (0, 0x7FC0))):
+        t["dy"][r, c] = bits
+    t["dres"][6, cols - 1] = 0x7F80
+    got = backward(t, to_dev_bf16(t["x"]), torch.from_numpy(stats).to(DEV))
+    with np.errstate(all="ignore"):
+        want = training.layernorm_bwd(f64(t["dy"]), f64(t["x"]), f64(t["gamma"]), stats, f64(t["dres"]))
+    for g, ref in ((f64(bf16_bits(got[0])), want[0]), (got[1].cpu().numpy(), want[1]), (got[2].cpu().numpy(), want[2])):
+        assert np.array_equal(np.isnan(g), np.isnan(ref)) and np.array_equal(g[np.isinf(ref)], ref[np.isinf(ref)]) and np.array_equal(np.isinf(g), np.isinf(ref))
+    assert torch.equal(got[0][7:], clean[0][7:]) and torch.equal(got[0][6, :-1], clean[0][6, :-1])
+
+
 @pytest.mark.parametrize("shape", [(37, 768), (5, 4096), (6, 1001), (3, 33000)])
 def test_in_place(shape):
     rows, cols = shape
@@ -267,6 +286,36 @@ def test_another_stream_and_a_replayed_graph():
         assert all(torch.equal(a, b) for a, b in zip(results(), want[i])), i
         step()
         assert all(torch.equal(a, b) for a, b in zip(results(), want[i])), i
+
+
+def test_two_graphs_that_share_a_workspace():
+    """Replayed in turn, each leaves what its own eager call does: nothing is kept in the workspace between calls."""
+    ws = workspace(tw.TWEO_OP_LAYERNORM_BWD, 3000, 1024, 1)
+    cases = []
+    for rows, cols in ((3000, 1024), (70, 333)):
+        t = inputs(rows, cols, rows)
+        stats = torch.from_numpy(training.layernorm_stats(f64(t["x"]), EPS)).to(DEV)
+        bufs = [to_dev_bf16(t[k]) for k in ("dy", "x", "gamma", "dres")]
+        out = torch.empty_like(bufs[0]), torch.empty(cols, device=DEV), torch.empty(cols, device=DEV)
+        assert ws.nbytes >= tw.tweo_workspace_bytes(tw.TWEO_OP_LAYERNORM_BWD, rows, cols, 1)
+
+        def call(bufs=bufs, out=out, stats=stats):
+            tw.tweo_layernorm_bwd(bufs[0], bufs[1], bufs[2], stats, out[0], out[1], dbeta=out[2], residual_grad_bf16=bufs[3], workspace=ws)
+
+        call()
+        torch.cuda.synchronize()
+        want = [o.clone() for o in out]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call()
+        cases.append((graph, out, want, call))
+    for i in (0, 1, 1, 0, 0, 1):
+        graph, out, want, call = cases[i]
+        for o in out:
+            o.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, w) for o, w in zip(out, want)), i
 
 
 def test_offsets_beyond_32_bits():

@@ -291,6 +291,36 @@ def test_moments_in_8_bits_follow_those_in_32():
             assert abs(ratio.mean() - 1) <= 0.02 and ratio.std() < 0.29
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_offsets_beyond_32_bits(bits):
+    """A tensor of 2^32 elements and some more: the last ones as in a tensor of their own (whose elements have the same thresholds
+    2^32 elements earlier), and the norm."""
+    more, n = 5000, (1 << 32) + 5000
+    rng = np.random.default_rng(15)
+    if bits == 32:
+        n = (1 << 31) + 5000  # (what fp32 states leave room for; byte offsets pass 2^33)
+    small = Tensor(rng, more, ("bf16", False, "bf16"), bits)
+    small.weight_decay = 0.1
+    whole = {k: torch.zeros(n if not k.endswith("_step") else -(-n // 256), dtype=getattr(small, k).dtype, device=DEV)
+             for k in ("param", "grad", "m", "v") + (("m_step", "v_step") if bits == 8 else ())}
+    for k, v in whole.items():
+        v[-getattr(small, k).numel():] = getattr(small, k)
+    rows = [tw.optim_tensor(weight_decay=0.1, **whole)]
+    plan = tw.make_optim_plan(rows, torch.empty(tw.tweo_optim_table_bytes(1), dtype=torch.uint8, device=DEV))
+    total = sumsq(plan)
+    want = grad64([small])
+    assert abs(float(total) - want) <= 1e-13 * want
+    tw.tweo_adamw_step(plan, step=5, grad_sumsq=total, max_norm=0.1, **HYPER)
+    small_plan = plan_of([small])
+    assert abs(float(sumsq(small_plan)) - want) <= 1e-13 * want
+    tw.tweo_adamw_step(small_plan, step=5, grad_sumsq=total, max_norm=0.1, **HYPER)
+    torch.cuda.synchronize()
+    for k, v in whole.items():
+        mine = getattr(small, k)
+        assert torch.equal(v[-mine.numel():].view(torch.uint8), mine.contiguous().view(torch.uint8)), k
+    assert int(torch.count_nonzero(whole["param"][:1 << 20])) == 0 and int(torch.count_nonzero(whole["v"][n - more - (1 << 20):n - more])) == 0
+
+
 def test_schedule_and_replayed_graph():
     for bits in (32, 8):
         rng = np.random.default_rng(11)
