@@ -159,6 +159,21 @@ __device__ __forceinline__ double team_sum(double v, double *red, int wave)
     return v;
 }
 
+// 1 / sqrt(v), v >= 0, within a few ulp: v_rsq_f64's 2^-24 and one step of third order.  (A square root and a quotient in fp64 are 50
+// instructions; with two quotients by the row's length they were a fifth of what a row of 768 issued.)
+__device__ __forceinline__ double rsqrt64(double v)
+{
+    const double y = __builtin_amdgcn_rsq(v), e = __builtin_fma(-v * y, y, 1.0);
+    return v > 0.0 ? __builtin_fma(y * e, __builtin_fma(e, 0.375, 0.5), y) : y;  // 0: infinity; NaN
+}
+
+// s / n with 1 / n at hand, rounded once: a row of one value has exactly that value as its mean, and zeros for differences
+__device__ __forceinline__ double divided(double s, double n, double inv_n)
+{
+    const double q = s * inv_n;
+    return __builtin_fma(__builtin_fma(-q, n, s), inv_n, q);
+}
+
 // ---------------------------------------------------------------------------
 // Forward: y = (h - mu) / sqrt(var + eps) * gamma + beta, h = x or bf16(x + residual).  One read of a row (2 B an element, 4 with a
 // residual), one write (2, 4): mean and squared differences are taken of the registers, in fp64 as in the pass in front of the
@@ -166,7 +181,7 @@ __device__ __forceinline__ double team_sum(double v, double *red, int wave)
 // 19.2 and 15.8 at 16384x1024, which the caches hold).  The next row is under way while one is worked on.  With a residual x and it are
 // read for the last time, and h, the stream, is next read a whole layer later: large calls load and store them past the caches (16384x2048 52.4 us,
 // 48.3, the stores alone 53.7; 8192x768, 50 MB, 13.3 and 14.3).
-// 16384x2048 with a residual 48.3 us, 5.6 TB/s; 50432x768 56; 8192x768 13.3; one row of 2048 4.9 of which 3 run.
+// 16384x2048 with a residual 48.3 us, 5.6 TB/s; 50432x768 53; 8192x768 12.8, where issuing takes half of the time; one row of 2048 2.8.
 struct LnFwdArgs {
     const uint16_t *x, *res, *gamma, *beta;
     uint16_t *h, *y;
@@ -185,7 +200,7 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void ln_fwd_kernel(LnFwdArgs a)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), team = wave / T;
     const int lane = (int)threadIdx.x - team * T * kWave;
     const Row<V, RAGGED> row(a.cols);
-    const double n = (double)a.cols;
+    const double n = (double)a.cols, inv_n = 1.0 / n;
     __shared__ double red[2][WAVES];
     // a team without a row goes through the last one's sums with the others (barriers) and stores nothing
     Piece<V> nx[P], nr[RES ? P : 1];
@@ -240,14 +255,14 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void ln_fwd_kernel(LnFwdArgs a)
             const double t = sum64(c[u]);
             s += row.count(i) > 0 ? t : 0.0;
         }
-        const double mean = team_sum<T>(s, &red[0][team * T], wave - team * T) / n;
+        const double mean = divided(team_sum<T>(s, &red[0][team * T], wave - team * T), n, inv_n);
         double ss = 0.0;
 #pragma unroll
         for (int u = 0; u < P; ++u) {
             c[u].keep();
             ss += squares64<V, RAGGED>(c[u], mean, row.count(lane + u * T * kWave));
         }
-        const double rstd = 1.0 / __builtin_sqrt(team_sum<T>(ss, &red[1][team * T], wave - team * T) / n + a.eps);
+        const double rstd = rsqrt64(__builtin_fma(team_sum<T>(ss, &red[1][team * T], wave - team * T), inv_n, a.eps));
         if (!mine)
             continue;
         if (a.stats != nullptr && lane == 0) {
@@ -273,7 +288,7 @@ __global__ __launch_bounds__(kWideThreads) void ln_fwd_wide_kernel(LnFwdArgs a)
     constexpr int T = kWideThreads / kWave;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const Row<8, RAGGED> row(a.cols);
-    const double n = (double)a.cols;
+    const double n = (double)a.cols, inv_n = 1.0 / n;
     __shared__ double red[2][T];
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         double s = 0.0;
@@ -287,11 +302,11 @@ __global__ __launch_bounds__(kWideThreads) void ln_fwd_wide_kernel(LnFwdArgs a)
         }
         // h may be x or the residual itself: what this thread has stored is read back, not formed again
         const uint16_t *h = (RES ? a.h : a.x) + r * a.cols;
-        const double mean = team_sum<T>(s, red[0], wave) / n;
+        const double mean = divided(team_sum<T>(s, red[0], wave), n, inv_n);
         double ss = 0.0;
         for (int i = threadIdx.x; i < row.pieces; i += kWideThreads)
             ss += squares64<8, RAGGED>(row.load(h, i, true), mean, row.count(i));
-        const double rstd = 1.0 / __builtin_sqrt(team_sum<T>(ss, red[1], wave) / n + a.eps);
+        const double rstd = rsqrt64(__builtin_fma(team_sum<T>(ss, red[1], wave), inv_n, a.eps));
         if (a.stats != nullptr && threadIdx.x == 0) {
             a.stats[2 * r] = mean;
             a.stats[2 * r + 1] = rstd;

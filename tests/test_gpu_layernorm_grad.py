@@ -88,6 +88,20 @@ def test_forward(shape, residual, beta):
     assert torch.equal(y, again)
 
 
+@pytest.mark.parametrize("cols", [3, 48, 777, 768, 1000, 2048, 16392, 33001])
+def test_rows_of_one_value(cols):
+    """Variance 0: every difference is a zero, whatever 1 / cols rounds to, and y is beta, or a zero whose sign the gain decides."""
+    values = np.float32([5.5, -0.1, 3e38, 1e-39, 1 / 3, 0.0, 7.0, -1e30])
+    t = inputs(len(values), cols, 3)
+    t["x"] = synth.f32_to_bf16_bits(np.repeat(values[:, None], cols, 1))
+    t["gamma"][::3] ^= 0x8000
+    for beta in (True, False):
+        y, _, st = forward(t, cols, False, beta)
+        _, yb = oracle.layernorm(t["x"], t["gamma"], t["beta"] if beta else None, float(np.float32(EPS)))
+        assert np.array_equal(bf16_bits(y), yb)
+        assert np.array_equal(st.cpu().numpy()[:, 0], f64(t["x"])[:, 0])
+
+
 @pytest.mark.parametrize("shape", [(64, 768), (32, 4096)])
 def test_forward_equals_what_the_cast_stores(shape):
     rows, cols = shape
