@@ -248,6 +248,62 @@ def time_layernorm(tw, torch, dev, rows=16384, cols=2048, copies=6, iters=24):
     return out
 
 
+def time_training_rest(tw, torch, layers, dev, iters=12):
+    """What a training step runs around the block's linears, on the gradients that the timed steps have left: the norm in bf16 over the
+    residual stream and its gradients (cold: four streams in turn), the norm of all weight gradients, and the clipped AdamW step on
+    all weights with fp32 masters, moments in fp32 and in 8 bits.  Each with the bytes that it can not do without."""
+    g = torch.Generator(device=dev)
+    g.manual_seed(11)
+    rows, cols, sets = layers[0].M, layers[0].K, 4
+    bf = lambda *shape: torch.randn(shape, device=dev, generator=g).to(torch.bfloat16)
+    streams = [dict(x=bf(rows, cols), r=bf(rows, cols), dy=bf(rows, cols), h=bf(rows, cols), y=bf(rows, cols), dx=bf(rows, cols),
+                    stats=torch.empty((rows, 2), dtype=torch.float64, device=dev)) for _ in range(sets)]
+    gamma, beta = (1 + 0.1 * torch.randn(cols, device=dev, generator=g)).to(torch.bfloat16), bf(cols)
+    dgamma, dbeta = torch.empty(cols, device=dev), torch.empty(cols, device=dev)
+    ws = torch.empty(max(tw.tweo_workspace_bytes(tw.TWEO_OP_LAYERNORM_BWD, rows, cols, 1),
+                         tw.tweo_workspace_bytes(tw.TWEO_OP_GRAD_SUMSQ, 1, 1, 1)), dtype=torch.uint8, device=dev)
+    s, e = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+
+    def timed(fn, nbytes):
+        for k in range(sets):
+            fn(k)
+        s.record()
+        for k in range(iters):
+            fn(k % sets)
+        e.record()
+        torch.cuda.synchronize()
+        us = s.elapsed_time(e) / iters * 1e3
+        return {"us": round(us, 2), "GB/s": round(nbytes / us / 1e3, 1), "frac_of_hbm_peak": round(nbytes / us / 1e3 / HBM_PEAK_GBS, 3)}
+
+    def fwd(k):
+        t = streams[k]
+        tw.tweo_layernorm_fwd(t["x"], gamma, t["y"], beta_bf16=beta, residual_bf16=t["r"], h_out_bf16=t["h"], stats_out=t["stats"])
+
+    def bwd(k):
+        t = streams[k]
+        tw.tweo_layernorm_bwd(t["dy"], t["h"], gamma, t["stats"], t["dx"], dgamma, dbeta=dbeta, residual_grad_bf16=t["r"], workspace=ws)
+
+    out = {"stream": "%dx%d bf16" % (rows, cols), "layernorm_fwd": timed(fwd, 8 * rows * cols), "layernorm_bwd": timed(bwd, 8 * rows * cols)}
+    del streams
+    n = sum(L.w.numel() for L in layers)
+    weights = [L.w.clone() for L in layers]
+    masters = [w.float() for w in weights]
+    total = torch.zeros(1, dtype=torch.float64, device=dev)
+    for bits in (32, 8):
+        zeros = lambda count, dtype: torch.zeros(count, dtype=dtype, device=dev)
+        state = torch.float32 if bits == 32 else torch.uint8
+        rows_ = [tw.optim_tensor(L.dw, w, zeros(w.numel(), state), zeros(w.numel(), state), master=f, weight_decay=0.1,
+                                 **({} if bits == 32 else {k: zeros(-(-w.numel() // 256), torch.float32) for k in ("m_step", "v_step")}))
+                 for L, w, f in zip(layers, weights, masters)]
+        plan = tw.make_optim_plan(rows_, torch.empty(tw.tweo_optim_table_bytes(len(rows_)), dtype=torch.uint8, device=dev))
+        if bits == 32:
+            out["weights"] = "%d in %d tensors" % (n, len(layers))
+            out["grad_sumsq"] = timed(lambda k: tw.tweo_grad_sumsq(plan, total, ws), 2 * n)
+        out["adamw_%d_bit_moments" % bits] = timed(
+            lambda k: tw.tweo_adamw_step(plan, lr=1e-4, step=k + 1, grad_sumsq=total), (28 if bits == 32 else 16.0625) * n)
+    return out
+
+
 def vendor_library_context(torch, layers, reps=6):
     """Context, not a product path: the FP8 GEMM of the vendor's library (hipBLASLt behind
     torch._scaled_mm) on the same 15 GEMMs, fed with the codes the step above left in the layers'
@@ -711,6 +767,7 @@ def main():
         del peers
         out["penalty_cost"] = time_penalty_cost(tw, torch, layers[0])
         out["layernorm"] = time_layernorm(tw, torch, dev)
+        out["training_step_beside_the_linears"] = time_training_rest(tw, torch, layers, dev)
         del layers, big
         torch.cuda.empty_cache()
         out["w8a8_7b"] = time_w8a8(tw, torch, synth, dev)

@@ -605,7 +605,7 @@ tweo_status tweo_optim_plan_init(const tweo_optim_tensor *tensors, int count, vo
  * Sum of the squares of all gradients of a table, in fp64 (fp64 products, fixed order).  The sum
  * and not the norm: shards add theirs exactly, and tweo_adamw_step takes it as it is.  A gradient that
  * is not finite makes it infinite or NaN.
- *   sumsq_out one fp64 on the device.   workspace: tweo_workspace_bytes(TWEO_OP_GRAD_SUMSQ, 1, 1, 1).
+ *   sumsq_out one fp64 on the device, 8-byte aligned.   workspace: tweo_workspace_bytes(TWEO_OP_GRAD_SUMSQ, 1, 1, 1).
  * Errors: TWEO_ERR_INVALID_ARG, TWEO_ERR_WORKSPACE.
  */
 tweo_status tweo_grad_sumsq(const tweo_optim_plan *plan, double *sumsq_out, void *workspace,
@@ -646,7 +646,8 @@ typedef struct {
  * spread of 25 % (12 % of its root); to nearest 23 % above with 35 %.  A positive v never becomes 0.  An infinity or NaN in a block makes its step NaN and the
  * block NaN from then on.
  *   grad_sumsq: one fp64 on the device, or NULL.  schedule: device memory, or NULL; with it lr and step of cfg are not
- *   used (a step of 0 there gives NaN or infinite parameters).
+ *   used (a step of 0 there gives NaN or infinite parameters).  Both 8-byte aligned.
+ * With eps = 0 an element whose gradients have all been zero becomes NaN; a v below 2^-126 (gradients below 1e-18) counts as 0 under the root.
  * A plan's calls must not overlap in time with each other, on whatever streams.
  * Errors: TWEO_ERR_INVALID_ARG (null, cfg out of range, a plan for gradients alone).
  */

@@ -296,7 +296,7 @@ __global__ __launch_bounds__(kSumsqThreads) void grad_sumsq_finish_kernel(const 
 // ---------------------------------------------------------------------------
 // AdamW: with the clipped gradient g' = c g, c = min(1, max_norm / (sqrt(S) + 1e-6)),
 //   m = b1 m + (1 - b1) g',  v = b2 v + (1 - b2) g'^2,  p = p - lr wd p - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps).
-// Bound by memory: 28 B an element with fp32 states beside an fp32 copy, 22 without; 18 and 10 with 8-bit states.  A wave takes one chunk, all of
+// Bound by memory: 28 B an element with fp32 states beside an fp32 copy, 22 without; 16 and 10 with 8-bit states.  A wave takes one chunk, all of
 // whose loads (20 to 28 of 4 to 16 bytes a lane) are under way before the first is waited for, and workgroups walk the tensors in order: 51 M elements with
 // master, fp32 states 241 us (6.0 TB/s), 205 M with 8-bit states 580 (5.7), without master 374 (5.5, half of its time the SIMDs issue).  Persistent
 // waves, each on a run of chunks of its own, took 301, 703 and 450; persistent ones in turns, the streams of all side by side, 284 and 665.
@@ -549,9 +549,9 @@ constexpr int64_t kAdamwMostGroups = 1 << 20;
 
 // Whether buffers of so many bytes an element are more than the memory-side cache (256 MB) gives back to the next step.  One step after the
 // other, without and with accesses past the caches: fp32 states beside a master, 28 B an element, 3 M elements 15.3 us and 17.7, 5 M 24.7 and
-// 25.9, 7 M 36.9 and 34.8, 20 M 108 and 87; 8-bit ones, 18 B, 5 M 19.0 and 20.7, 10 M 32.8 and 30.9, 20 M 67 and 58.
+// 25.9, 7 M 36.9 and 34.8, 20 M 108 and 87; 8-bit ones, 16 B, 5 M 19.0 and 20.7, 10 M 32.8 and 30.9, 20 M 67 and 58.
 // (The norm, bf16 gradients: 103 MB 22.9 and 22.9, 411 MB 77 and 68.)
-constexpr int64_t kKeptBytes = 160 << 20;
+constexpr int64_t kKeptBytes = 150 << 20;
 bool past_caches(int64_t chunks, int64_t bytes) { return chunks * kChunk * bytes > kKeptBytes; }
 
 }  // namespace
@@ -596,7 +596,7 @@ hipError_t launch_adamw(const void *table, int count, int64_t chunks, bool eight
                       (float)c.eps, (float)c.lr, k.step_size, k.inv_sqrt_bc2, c.beta1, c.beta2, c.max_norm, c.step, c.grad_sumsq, c.schedule};
     const unsigned groups = (unsigned)std::min<int64_t>((chunks + 3) / 4, kAdamwMostGroups);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(groups), dim3(kAdamwThreads), 0, s, a); };
-    if (past_caches(chunks, eight_bits ? 18 : 28))
+    if (past_caches(chunks, eight_bits ? 16 : 28))
         eight_bits ? go(adamw_kernel<true, true>) : go(adamw_kernel<false, true>);
     else
         eight_bits ? go(adamw_kernel<true, false>) : go(adamw_kernel<false, false>);

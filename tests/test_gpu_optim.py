@@ -182,6 +182,29 @@ def test_large_tensors_beside_small_ones(bits):
         assert x.intact()
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_models_beyond_the_caches(bits):
+    """Buffers of more than 150 MB, which are read and stored past the caches: whole chunks, short ones, all kinds."""
+    rng = np.random.default_rng(16)
+    tensors = [Tensor(rng, n, kind, bits) for n, kind in zip((2_000_000, 1_999_997, 2_000_001, 1_234_567, 2_500_000, 999, 1_700_000), KINDS + [KINDS[2]])]
+    plan = plan_of(tensors)
+    total = sumsq(plan)
+    before = [x.state() for x in tensors]
+    tw.tweo_adamw_step(plan, step=9, grad_sumsq=total, max_norm=1.0, **HYPER)
+    for i, (x, b) in enumerate(zip(tensors, before)):
+        check(b, x.state(), 9, bits, x.weight_decay, HYPER, float(np.float32(training.clip_factor(float(total), 1.0))), i)
+        assert x.intact()
+
+
+def test_norm_of_many_gradients():
+    gen = torch.Generator(DEV).manual_seed(3)
+    grads = [torch.randn(n, device=DEV, generator=gen).to(d) for n, d in ((70_000_001, torch.bfloat16), (4096 * 5 + 3, torch.float32),
+                                                                          (9_000_000, torch.float32), (1, torch.bfloat16))]
+    plan = tw.make_optim_plan([tw.optim_tensor(g) for g in grads], torch.empty(tw.tweo_optim_table_bytes(4), dtype=torch.uint8, device=DEV))
+    want = sum(float(g.double().square().sum()) for g in grads)
+    assert abs(float(sumsq(plan)) - want) <= 1e-12 * want
+
+
 def test_many_tensors():
     """More than one launch's worth of table rows, and more tensors than waves would need."""
     rng = np.random.default_rng(4)
