@@ -118,6 +118,17 @@ __device__ __forceinline__ Piece<V> sum_of(const Piece<V> &a, const Piece<V> &b)
     return r;
 }
 
+// what stands for a beta that there is not: -0, which leaves a zero the sign that the product gives it
+template <int V>
+__device__ __forceinline__ Piece<V> nothing_added()
+{
+    Piece<V> r;
+#pragma unroll
+    for (int k = 0; k < V / 2; ++k)
+        r.w[k] = 0x80008000u;
+    return r;
+}
+
 template <int V>
 __device__ __forceinline__ double sum64(const Piece<V> &v)
 {
@@ -181,7 +192,7 @@ __device__ __forceinline__ double divided(double s, double n, double inv_n)
 // 19.2 and 15.8 at 16384x1024, which the caches hold).  The next row is under way while one is worked on.  With a residual x and it are
 // read for the last time, and h, the stream, is next read a whole layer later: large calls load and store them past the caches (16384x2048 52.4 us,
 // 48.3, the stores alone 53.7; 8192x768, 50 MB, 13.3 and 14.3).
-// 16384x2048 with a residual 48.3 us, 5.6 TB/s; 50432x768 53; 8192x768 12.8, where issuing takes half of the time; one row of 2048 2.8.
+// 16384x2048 with a residual 45.2 us, 5.9 TB/s; 50432x768 51; 8192x768 12.3, where issuing takes half of the time; one row of 2048 2.7.
 struct LnFwdArgs {
     const uint16_t *x, *res, *gamma, *beta;
     uint16_t *h, *y;
@@ -221,10 +232,7 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void ln_fwd_kernel(LnFwdArgs a)
     for (int u = 0; u < P; ++u) {
         const int i = lane + u * T * kWave;
         const bool ending = row.template ends<T>(u * T * kWave);
-        const Piece<V> g = row.load(a.gamma, i, ending);
-        Piece<V> b{};
-        if (a.beta != nullptr)
-            b = row.load(a.beta, i, ending);
+        const Piece<V> g = row.load(a.gamma, i, ending), b = a.beta != nullptr ? row.load(a.beta, i, ending) : nothing_added<V>();
 #pragma unroll
         for (int k = 0; k < V; ++k)
             gamma[u][k] = g.at(k), beta[u][k] = b.at(k);
@@ -273,7 +281,7 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void ln_fwd_kernel(LnFwdArgs a)
         for (int u = 0; u < P; ++u) {
             c[u].keep();
             Piece<V> y;
-            ln_pairs<V>(c[u].w, mean, rstd, gamma[u], beta[u], a.beta != nullptr, y.w);
+            ln_pairs<V, true>(c[u].w, mean, rstd, gamma[u], beta[u], true, y.w);
             row.store(a.y + at, lane + u * T * kWave, y);
         }
     }
@@ -313,14 +321,13 @@ __global__ __launch_bounds__(kWideThreads) void ln_fwd_wide_kernel(LnFwdArgs a)
         }
         for (int i = threadIdx.x; i < row.pieces; i += kWideThreads) {
             const Piece<8> x = row.load(h, i, true), g = row.load(a.gamma, i, true);
-            Piece<8> b{}, y;
-            if (a.beta != nullptr)
-                b = row.load(a.beta, i, true);
+            const Piece<8> b = a.beta != nullptr ? row.load(a.beta, i, true) : nothing_added<8>();
+            Piece<8> y;
             float gamma[8], beta[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k)
                 gamma[k] = g.at(k), beta[k] = b.at(k);
-            ln_pairs<8>(x.w, mean, rstd, gamma, beta, a.beta != nullptr, y.w);
+            ln_pairs<8, true>(x.w, mean, rstd, gamma, beta, true, y.w);
             row.store(a.y + r * a.cols, i, y);
         }
     }
