@@ -210,8 +210,9 @@ tweo_status tweo_layernorm_quantize_e4m3_delayed(const void *x_bf16, const void 
  * head, attention), and for one token as for many.
  *   h[r,c] = x[r,c]            or, with a residual, bf16( x[r,c] + residual[r,c] )
  *   y[r,c] = bf16( (h[r,c] - mu_r) / sqrt(var_r + eps) * gamma[c] + beta[c] )
- * mu and the biased var as in tweo_layernorm_quantize_e4m3; fp64, one rounding: y is
- * bit for bit what that call's y_out is.
+ * mu and the biased var as in tweo_layernorm_quantize_e4m3; fp64, one rounding: y has
+ * the bits of that call's y_out (the sums' order, 1e-16 of the value, can only show
+ * where that lies on a rounding boundary).
  *   x_bf16, y_bf16 [rows, cols], any rows >= 1 and cols >= 1 (cols that are no multiple
  *   of 8 start their rows at odd places and run slower).
  *   residual_bf16 [rows, cols] or NULL; with it h_out_bf16 is required, without it
@@ -641,13 +642,16 @@ typedef struct {
  *           a fraction of the distance to it, plus u is at least 1
  *   u     = top 20 (E4M3) or 21 (E5M2) bits of ( i * 0x6A09E667 + t * 0x9E3779B9 mod 2^32 ) as a fraction,
  *           i the element's index in its tensor
- * v moves by less than half a code step at a time, and rounded to nearest it would stay where it is; u runs evenly over
- * [0, 1) with t and with i.  Over 300 steps at beta2 = 0.99 the coded v is 1.5 % below the fp32 one on average with a
- * spread of 25 % (12 % of its root); to nearest 23 % above with 35 %.  A positive v never becomes 0.  An infinity or NaN in a block makes its step NaN and the
- * block NaN from then on.
- *   grad_sumsq: one fp64 on the device, or NULL.  schedule: device memory, or NULL; with it lr and step of cfg are not
- *   used (a step of 0 there gives NaN or infinite parameters).  Both 8-byte aligned.
- * With eps = 0 an element whose gradients have all been zero becomes NaN; a v below 2^-126 (gradients below 1e-18) counts as 0 under the root.
+ * v moves by less than half a code step at a time, and rounded to nearest it would stay
+ * where it is; u runs evenly over [0, 1) with t and with i.  Over 300 steps at beta2 =
+ * 0.99 the coded v is 1.5 % below the fp32 one on average with a spread of 25 % (12 % of
+ * its root); to nearest 23 % above with 35 %.  A positive v never becomes 0.  An infinity
+ * or NaN in a block makes its step NaN and the block NaN from then on.
+ *   grad_sumsq: one fp64 on the device, or NULL.  schedule: device memory, or NULL; with
+ *   it lr and step of cfg are not used (a step of 0 there gives NaN or infinite
+ *   parameters).  Both 8-byte aligned.
+ * With eps = 0 an element whose gradients have all been zero becomes NaN; a v below
+ * 2^-126 (gradients below 1e-18) counts as 0 under the root.
  * A plan's calls must not overlap in time with each other, on whatever streams.
  * Errors: TWEO_ERR_INVALID_ARG (null, cfg out of range, a plan for gradients alone).
  */

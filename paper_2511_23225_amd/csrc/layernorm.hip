@@ -175,7 +175,7 @@ __device__ __forceinline__ double team_sum(double v, double *red, int wave)
 __device__ __forceinline__ double rsqrt64(double v)
 {
     const double y = __builtin_amdgcn_rsq(v), e = __builtin_fma(-v * y, y, 1.0);
-    return v > 0.0 ? __builtin_fma(y * e, __builtin_fma(e, 0.375, 0.5), y) : y;  // 0: infinity; NaN
+    return v > 0.0 && v < __builtin_inf() ? __builtin_fma(y * e, __builtin_fma(e, 0.375, 0.5), y) : y;  // of 0 infinity, of infinity 0; NaN
 }
 
 // s / n with 1 / n at hand, rounded once: a row of one value has exactly that value as its mean, and zeros for differences

@@ -185,7 +185,6 @@ __device__ __forceinline__ void store4(GLOBAL uint8_t *p, uint32_t element, int 
 constexpr int kSumsqThreads = 256;
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-
 // whole chunks: 16 bytes a lane and load, all of them under way at once
 template <bool F32, bool ONCE, int CHUNKS>
 __device__ __forceinline__ double sumsq_whole(const GLOBAL uint8_t *grad)
@@ -310,9 +309,8 @@ __global__ __launch_bounds__(kSumsqThreads) void grad_sumsq_finish_kernel(const 
 // one element and along the elements i of one step: u = frac(i (sqrt(2) - 1) + t (sqrt(5) - 1) / 2), as 32-bit integers: a multiplication
 // and an addition, and any step can be recomputed.  Simulated over 300 steps at b2 = 0.99 (0.95, 0.999), the coded v over the exact one: mean
 // 0.985 (0.983, 0.987), spread 0.25 (0.18, 0.25); with independent random numbers 0.998, 0.29 (0.23, 0.30); to nearest 1.24 (1.08, 1.14), 0.35
-// (0.20, 0.36).  In bits: y, the
-// scaled value times the power of two that puts the code's exponent field where fp32 has its own (codes below the normal ones
-// becoming fp32's subnormals), plus the top of u below the code's last bit, shifted.
+// (0.20, 0.36).  In bits: y, the scaled value times the power of two that puts the code's exponent field where fp32 has its own (codes below
+// the normal ones becoming fp32's subnormals), plus the top of u below the code's last bit, shifted.
 struct AdamwArgs {
     const Entry *table;
     int count;

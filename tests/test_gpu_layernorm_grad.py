@@ -102,6 +102,17 @@ def test_rows_of_one_value(cols):
         assert np.array_equal(st.cpu().numpy()[:, 0], f64(t["x"])[:, 0])
 
 
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 0.5, 1e30, float("inf")])
+def test_every_eps(eps):
+    t = inputs(6, 300, 8)
+    y, _, st = forward(t, 300, False, True, eps=eps)
+    with np.errstate(all="ignore"):
+        want = training.layernorm_stats(f64(t["x"]), float(np.float32(eps)))
+    y64, yb = oracle.layernorm(t["x"], t["gamma"], t["beta"], float(np.float32(eps)))
+    check_y(bf16_bits(y), yb, y64, eps)
+    assert np.allclose(st.cpu().numpy(), want, rtol=1e-12, atol=0)
+
+
 @pytest.mark.parametrize("shape", [(64, 768), (32, 4096)])
 def test_forward_equals_what_the_cast_stores(shape):
     rows, cols = shape
