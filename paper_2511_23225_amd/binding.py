@@ -585,9 +585,14 @@ def tweo_grad_sumsq(plan, sumsq_out, workspace):
     _check(load().tweo_grad_sumsq(ctypes.byref(plan), _ptr(sumsq_out), wp, wb, _stream()), "tweo_grad_sumsq")
 
 
-def tweo_adamw_step(plan, lr=0.0, step=1, beta1=0.9, beta2=0.999, eps=1e-8, grad_sumsq=None, max_norm=1.0, schedule=None):
-    """schedule: two 32-bit words on the device, lr as fp32 and step as an integer, in the place of `lr` and `step`."""
+def tweo_adamw_step(plan, lr=None, step=None, beta1=0.9, beta2=0.999, eps=1e-8, grad_sumsq=None, max_norm=1.0, schedule=None):
+    """lr and step, or schedule: two 32-bit words on the device, lr as fp32 and step as an integer."""
     _on_device(plan, grad_sumsq, schedule)
-    cfg = AdamwCfg(lr, beta1, beta2, eps, max_norm, step)
+    if schedule is None:
+        if lr is None or step is None:
+            raise ValueError("lr and step are needed without a schedule")
+        cfg = AdamwCfg(lr, beta1, beta2, eps, max_norm, step)
+    else:
+        cfg = AdamwCfg(0.0, beta1, beta2, eps, max_norm, 1)
     _check(load().tweo_adamw_step(ctypes.byref(plan), ctypes.byref(cfg), _ptr(grad_sumsq), _ptr(schedule), _stream()),
            "tweo_adamw_step")

@@ -170,6 +170,26 @@ def test_backward(shape, residual, beta):
     assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
 
 
+def test_backward_of_the_norm_in_front_of_a_cast():
+    """The statistics that the LayerNorm -> cast calls leave in their workspace are what the backward pass takes."""
+    rows, cols = 320, 2048
+    t = inputs(rows, cols, 23)
+    x, r, gamma, beta = (to_dev_bf16(t[k]) for k in ("x", "r", "gamma", "beta"))
+    ws = workspace(tw.TWEO_OP_LAYERNORM_QUANTIZE, rows, 1, 1)
+    q, h = torch.empty((rows, cols), dtype=torch.uint8, device=DEV), torch.empty_like(x)
+    state = torch.zeros(tw.DELAYED_STATE_WORDS, dtype=torch.float32, device=DEV)
+    tw.tweo_delayed_state_init(state)
+    hb = oracle.residual_add_bf16(t["x"], t["r"])
+    stats = training.layernorm_stats(f64(hb), float(np.float32(EPS)))
+    for delayed in (False, True):
+        ws.fill_(0)
+        if delayed:
+            tw.tweo_layernorm_quantize_e4m3_delayed(x, gamma, state, q, ws, bootstrap=True, beta_bf16=beta, residual_bf16=r, eps=EPS, h_out_bf16=h)
+        else:
+            tw.tweo_layernorm_quantize_e4m3(x, gamma, q, ws, beta_bf16=beta, residual_bf16=r, eps=EPS, h_out_bf16=h)
+        check_backward(t, hb, stats, backward(t, h, tw.layernorm_stats(ws, rows)))
+
+
 @pytest.mark.parametrize("shape", [(17501, 768), (3301, 4096), (52000, 256), (1601, 8200)])
 def test_streams_beyond_the_caches(shape):
     """Calls of more than 100 MB, which read and store past the caches; the second in place."""

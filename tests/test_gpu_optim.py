@@ -218,6 +218,39 @@ def test_many_tensors():
         check(b, x.state(), 3, 32, x.weight_decay, HYPER, 1.0, i)
 
 
+def test_a_table_of_thousands():
+    """More tensors than two looks at 64 entries tell apart, in one buffer each kind, with one gradient that two of them share."""
+    rng = np.random.default_rng(17)
+    sizes = [int(n) for n in rng.integers(1, 1500, 5000)]
+    places = np.concatenate([[0], np.cumsum([(n + 7) // 8 * 8 for n in sizes])])  # multiples of 16 bytes, also of bf16
+    total = int(places[-1])
+    g, p, m, v = (torch.from_numpy((rng.standard_normal(total) * s).astype(np.float32)).to(DEV) for s in (0.01, 0.02, 0.003, 0.01))
+    g, v = g.bfloat16(), v.square() + 2e-5
+    view = lambda x, i: x[int(places[i]):int(places[i]) + sizes[i]]  # noqa: E731
+    sizes[4999] = min(sizes[4999], sizes[17])
+    grads = [view(g, i) for i in range(4999)] + [view(g, 17)[:sizes[4999]]]
+    used = torch.zeros(total, dtype=torch.bool, device=DEV)
+    for i in range(5000):
+        view(used, i).fill_(True)
+    before = [x.cpu().double().numpy() for x in (p, m, v)]
+    gd = np.zeros(total)
+    for i in range(5000):
+        gd[int(places[i]):int(places[i]) + sizes[i]] = grads[i].float().cpu().numpy()
+    rows = [tw.optim_tensor(grads[i], view(p, i), view(m, i), view(v, i), weight_decay=0.1) for i in range(5000)]
+    plan = tw.make_optim_plan(rows, torch.empty(tw.tweo_optim_table_bytes(5000), dtype=torch.uint8, device=DEV))
+    want = math.fsum((gd ** 2).tolist())
+    got = sumsq(plan)
+    assert abs(float(got) - want) <= 1e-13 * want
+    tw.tweo_adamw_step(plan, step=3, grad_sumsq=got, max_norm=0.1, **HYPER)
+    clip = float(np.float32(training.clip_factor(want, 0.1)))
+    p1, m1, v1, m_size, change = training.adamw(before[0], gd, before[1], before[2], 3, HYPER["lr"], HYPER["beta1"], HYPER["beta2"], HYPER["eps"],
+                                                float(np.float32(0.1)), clip)
+    u = used.cpu().numpy()
+    for x, ref, old, tol in ((p, p1, before[0], 24 * E * change + 2 * E * np.abs(p1)), (m, m1, before[1], 6 * E * m_size + 1e-44), (v, v1, before[2], 9 * E * v1)):
+        x = x.cpu().double().numpy()
+        assert np.all(np.abs(x - ref)[u] <= tol[u]) and np.array_equal(x[~u], old[~u])
+
+
 def test_norm_of_gradients_alone():
     rng = np.random.default_rng(5)
     grads = [torch.from_numpy((rng.standard_normal(n) * s).astype(np.float32)).to(DEV).to(d)
@@ -403,6 +436,15 @@ def test_a_plan_of_another_device_is_refused():
         tw.tweo_adamw_step(plan, step=1, grad_sumsq=torch.zeros(1, dtype=torch.float64), **HYPER)
     with pytest.raises(ValueError):
         tw.tweo_adamw_step(plan, schedule=torch.zeros(1, dtype=torch.int32, device=DEV), **HYPER)
+    for missing in (dict(step=1), dict(lr=1e-3)):
+        with pytest.raises(ValueError):
+            tw.tweo_adamw_step(plan, **missing)
+    with pytest.raises(tw.TweoError):
+        tw.make_optim_plan([x.row(), x.row()], torch.empty(256, dtype=torch.uint8, device=DEV))  # the same buffers twice
+    with pytest.raises(tw.TweoError):
+        tw.make_optim_plan([], torch.empty(256, dtype=torch.uint8, device=DEV))
+    with pytest.raises(ValueError):
+        tw.make_optim_plan([tw.optim_tensor(torch.zeros(8))], torch.empty(256, dtype=torch.uint8, device=DEV))
     plan.device = 1
     with pytest.raises(ValueError):
         tw.tweo_adamw_step(plan, step=1, **HYPER)
