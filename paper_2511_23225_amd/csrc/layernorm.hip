@@ -362,7 +362,7 @@ void launch_fwd(const LnFwdArgs &a, hipStream_t s)
 // the place of 33).  fp32 throughout but for h - mu: mu is a double and is subtracted in two parts, since rows whose mean is far above their
 // deviation cancel there.  What is read here is read for the last time: large calls read past the caches (16384x2048 56.5 us, 51.2; 8192x768, 50 MB,
 // 16.9 and 17.6).  Wide rows on teams of more waves with fewer elements each: the sums' registers are what limits the waves.
-// 16384x2048 with dres 51.2 us, 5.2 TB/s (45 + 4.5 for the second launch); 18912x768 28.0, 50432x768 59.2, 8192x768 16.1; 257x1001 8.6, two launches.
+// 16384x2048 with dres 51.2 us, 5.2 TB/s (45 + 4.5 for the second launch); 18912x768 28.0, 50432x768 59.2, 8192x768 16.1; 257x1001 7.0, one launch.
 struct LnBwdArgs {
     const uint16_t *dy, *h, *gamma, *dres;
     const double *stats;
@@ -371,6 +371,9 @@ struct LnBwdArgs {
     float *sums;      // wide rows: mean(w), mean(w xhat) of each row
     int64_t rows;
     int cols;
+    // ALONE: workgroups from this one on take the column sums
+    int row_groups;
+    float *dgamma, *dbeta;
 };
 
 __device__ __forceinline__ float dpp_sum(float v)
@@ -389,12 +392,63 @@ __device__ __forceinline__ float dpp_sum(float v)
     return bits_to_f32((uint32_t)__builtin_amdgcn_readlane((int)f32_to_bits(v), 63));
 }
 
-// SLAB: rows of more pieces than the teams hold; blockIdx.y is the slab of T * P * 64 pieces that this workgroup works on, and a
+// Column sums of a call of few rows (ALONE): this workgroup's 64 columns over all rows.  They need the statistics only and not the two means of
+// each row, so that other workgroups of the same launch work on dx meanwhile and nothing has to be added afterwards; h and dy are read twice, the
+// second time from the caches.  257x768 8.6 us in two launches, 6.0 in one; 512x768 8.7, 6.8; 512x4096 15.6, 10.5; 1024x768 9.0, 9.7.
+template <int V, int THREADS, bool RAGGED>
+__device__ __forceinline__ void column_sums(const LnBwdArgs &a, int group)
+{
+    constexpr int LANES = 64 / V, PARTS = THREADS / LANES;
+    const Row<V, RAGGED> row(a.cols);
+    const int lane = threadIdx.x % LANES, part = threadIdx.x / LANES, i = group * LANES + lane;
+    float dgamma[V], dbeta[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+        dgamma[k] = dbeta[k] = 0.0f;
+#pragma unroll 4
+    for (int64_t r = part; r < a.rows; r += PARTS) {
+        const Piece<V> h = row.load(a.h + r * a.cols, i, true), dy = row.load(a.dy + r * a.cols, i, true);
+        const double mean = a.stats[2 * r];
+        const float mean_hi = (float)mean, rstd = (float)a.stats[2 * r + 1], shift = (float)(mean - (double)mean_hi) * -rstd;
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            dgamma[k] = __builtin_fmaf(dy.at(k), __builtin_fmaf(h.at(k) - mean_hi, rstd, shift), dgamma[k]);
+            dbeta[k] += dy.at(k);
+        }
+    }
+    __shared__ float sums[PARTS][64 + 1];
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        if (which) {
+            if (a.dbeta == nullptr)
+                return;
+            __syncthreads();
+        }
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            sums[part][lane * V + k] = which ? dbeta[k] : dgamma[k];
+        __syncthreads();
+        const int col = group * 64 + (int)threadIdx.x;
+        if (threadIdx.x < 64 && col < a.cols) {
+            double s = 0.0;
+#pragma unroll 8
+            for (int p = 0; p < PARTS; ++p)
+                s += (double)sums[p][threadIdx.x];
+            (which ? a.dbeta : a.dgamma)[col] = (float)s;
+        }
+    }
+}
+
+// ALONE: the row sums and dx only; column_sums has the rest.  SLAB: rows of more pieces than the teams hold; blockIdx.y is the slab of T * P * 64 pieces that this workgroup works on, and a
 // launch before has left the two means of each row.
-template <int T, int P, int V, int WAVES, bool RES, bool RAGGED, bool SLAB, bool ONCE>
+template <int T, int P, int V, int WAVES, bool RES, bool RAGGED, bool SLAB, bool ONCE, bool ALONE = false>
 __global__ __launch_bounds__(WAVES *kWave) void ln_bwd_kernel(LnBwdArgs a)
 {
     constexpr int TEAMS = WAVES / T;
+    if constexpr (ALONE)
+        if ((int)blockIdx.x >= a.row_groups)
+            return column_sums<V, WAVES * kWave, RAGGED>(a, (int)blockIdx.x - a.row_groups);
+    const int64_t stride_rows = (int64_t)(ALONE ? a.row_groups : (int)gridDim.x) * TEAMS;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), team = wave / T;
     const int lane = (int)threadIdx.x - team * T * kWave, first = SLAB ? (int)blockIdx.y * T * P * kWave : 0;
     const Row<V, RAGGED> row(a.cols);
@@ -432,7 +486,7 @@ __global__ __launch_bounds__(WAVES *kWave) void ln_bwd_kernel(LnBwdArgs a)
             dgamma[u][k] = dbeta[u][k] = 0.0f;
         }
     }
-    for (int64_t r0 = (int64_t)blockIdx.x * TEAMS; r0 < a.rows; r0 += (int64_t)gridDim.x * TEAMS, turn ^= 1) {
+    for (int64_t r0 = (int64_t)blockIdx.x * TEAMS; r0 < a.rows; r0 += stride_rows, turn ^= 1) {
         const bool mine = r0 + team < a.rows;
         const int64_t r = mine ? r0 + team : a.rows - 1, at = r * a.cols;
         Piece<V> h[P], dy[P], dres[RES ? P : 1];
@@ -446,8 +500,8 @@ __global__ __launch_bounds__(WAVES *kWave) void ln_bwd_kernel(LnBwdArgs a)
         }
         const double mean = nmean;
         const float mean_hi = (float)mean, rstd = (float)nrstd, shift = (float)(mean - (double)mean_hi) * -rstd;
-        if (AHEAD && r0 + (int64_t)gridDim.x * TEAMS < a.rows)
-            request(r0 + (int64_t)gridDim.x * TEAMS);
+        if (AHEAD && r0 + stride_rows < a.rows)
+            request(r0 + stride_rows);
         float c1 = 0.0f, c2 = 0.0f;  // sums of w xhat, w; then their means
         float xhat[P][V], w[P][V];
 #pragma unroll
@@ -462,7 +516,7 @@ __global__ __launch_bounds__(WAVES *kWave) void ln_bwd_kernel(LnBwdArgs a)
                     t2 += w[u][k];
                     t1 = __builtin_fmaf(w[u][k], xhat[u][k], t1);
                 }
-                if (mine) {
+                if (!ALONE && mine) {
                     dgamma[u][k] = __builtin_fmaf(d, xhat[u][k], dgamma[u][k]);
                     dbeta[u][k] += d;
                 }
@@ -513,6 +567,8 @@ __global__ __launch_bounds__(WAVES *kWave) void ln_bwd_kernel(LnBwdArgs a)
             row.store(a.dx + at, first + lane + u * T * kWave, out);
         }
     }
+    if constexpr (ALONE)
+        return;
     // the teams' column sums through LDS, then added in the teams' order, four columns a thread
     __shared__ float sums[TEAMS][P * V][T * kWave];
     const int stride = (a.cols + 3) & ~3;
@@ -608,6 +664,9 @@ __global__ __launch_bounds__(kFinThreads) void ln_bwd_finish_kernel(const float 
     }
 }
 
+// few rows, of which a workgroup can take 64 columns as fast as others the rows
+bool bwd_alone(int64_t rows, int64_t cols) { return rows <= 512 && cols <= 8192; }
+
 // What a backward call runs on: T, P, V and WAVES of the kernel, the fewest lanes that hold a row.
 struct BwdShape {
     int waves_a_row, pieces, elements, waves;
@@ -648,6 +707,23 @@ void launch_bwd(const LnBwdArgs &a, int groups, hipStream_t s)
 {
     const unsigned slabs = SLAB ? (unsigned)((a.cols + T * P * kWave * V - 1) / (T * P * kWave * V)) : 1u;
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)groups, slabs), dim3(WAVES * kWave), 0, s, a); };
+    if constexpr (!SLAB)
+        if (bwd_alone(a.rows, a.cols)) {
+            auto alone = [&](int row_groups, int grid) {
+                LnBwdArgs b = a;
+                b.row_groups = row_groups;
+                auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(WAVES * kWave), 0, s, b); };
+                if (a.cols % V != 0)
+                    a.dres ? run(ln_bwd_kernel<T, P, V, WAVES, true, true, false, false, true>) : run(ln_bwd_kernel<T, P, V, WAVES, false, true, false, false, true>);
+                else
+                    a.dres ? run(ln_bwd_kernel<T, P, V, WAVES, true, false, false, false, true>) : run(ln_bwd_kernel<T, P, V, WAVES, false, false, false, false, true>);
+            };
+            const int column_groups = (a.cols + 63) / 64;
+            if ((const void *)a.dx != (const void *)a.dy)
+                return alone(groups, groups + column_groups);
+            alone(0, column_groups);  // in place of dy: the sums first
+            return alone(groups, groups);
+        }
     if (a.cols % V != 0)
         a.dres ? go(ln_bwd_kernel<T, P, V, WAVES, true, true, SLAB, false>) : go(ln_bwd_kernel<T, P, V, WAVES, false, true, SLAB, false>);
     else if (a.rows * a.cols * (a.dres ? 8 : 6) > kKeptBytes)
@@ -707,7 +783,7 @@ hipError_t launch_layernorm_bwd(const void *dy, const void *h, const void *gamma
     const int groups = bwd_groups(rows, cols, b);
     float *partials = (float *)workspace, *sums = partials + partial_floats(cols, groups);
     const LnBwdArgs a{(const uint16_t *)dy, (const uint16_t *)h, (const uint16_t *)gamma, (const uint16_t *)dres, stats,
-                      (uint16_t *)dx, partials, sums, rows, (int)cols};
+                      (uint16_t *)dx, partials, sums, rows, (int)cols, 0, dgamma, dbeta};
     if (b.wide) {
         const dim3 grid((unsigned)std::min<int64_t>(rows, 4 * kCus));
         if (cols % 8 != 0)
@@ -731,7 +807,7 @@ hipError_t launch_layernorm_bwd(const void *dy, const void *h, const void *gamma
         }
     }
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess)
+    if (e != hipSuccess || bwd_alone(rows, cols))
         return e;
     hipLaunchKernelGGL(ln_bwd_finish_kernel, dim3((unsigned)((cols + 4 * kFinLanes - 1) / (4 * kFinLanes)), dbeta != nullptr ? 2 : 1),
                        dim3(kFinThreads), 0, s, partials, groups, (int)cols, dgamma, dbeta);

@@ -54,7 +54,8 @@ def inputs(rows, cols, seed):
 SHAPES = [(1, 1), (3, 2), (2, 7), (5, 8), (4, 9), (1, 2048), (17, 64), (9, 255), (33, 512), (31, 513), (65, 768), (257, 1001), (12, 1024),
           (13, 1025), (40, 1536), (7, 2048), (6, 2049), (11, 4096), (5, 4104), (3, 8192), (4, 8193), (2, 8200), (3, 16384), (2, 16392), (2, 16385),
           (3, 32776), (2, 33001), (5000, 24), (4099, 768), (3, 253), (3, 257),
-          (3, 509), (3, 767), (3, 769), (3, 1023), (3, 1531), (3, 1537), (3, 2047), (3, 4095), (3, 8191), (2, 16383), (300, 8200), (700, 5632)]
+          (3, 509), (3, 767), (3, 769), (3, 1023), (3, 1531), (3, 1537), (3, 2047), (3, 4095), (3, 8191), (2, 16383), (300, 8200), (700, 5632),
+          (512, 768), (513, 768), (512, 1001), (511, 8192), (512, 250), (65, 61)]
 
 
 def forward(t, cols, residual, beta, stats=True, eps=EPS):
@@ -294,7 +295,7 @@ def test_gradients_that_are_not_finite(cols):
     assert torch.equal(got[0][7:], clean[0][7:]) and torch.equal(got[0][6, :-1], clean[0][6, :-1])
 
 
-@pytest.mark.parametrize("shape", [(37, 768), (5, 4096), (6, 1001), (3, 33000)])
+@pytest.mark.parametrize("shape", [(37, 768), (5, 4096), (6, 1001), (3, 33000), (512, 768), (700, 768), (300, 1001)])
 def test_in_place(shape):
     rows, cols = shape
     t = inputs(rows, cols, 9)
