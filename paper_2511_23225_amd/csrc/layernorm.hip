@@ -43,9 +43,9 @@ struct Row {
     {
         return RAGGED && pieces > i0 && pieces <= i0 + T * kWave;
     }
-    // Piece i, zeros behind a ragged row's end.  Without branches, around which the compiler would wait for one load before it issues the
-    // next (4096x4093 backward 60.4 us, now 44.6): a lane without a piece gets the row's last one, and a short piece is taken from the row's last V elements and shifted down.
-    // `ending`: the pieces that ends() names.
+    // Piece i, zeros behind a ragged row's end.  Without branches, around which the compiler would wait for one load before it
+    // issues the next (4096x4093 backward 60.4 us, now 44.6): a lane without a piece gets the row's last one, and a short piece
+    // is taken from the row's last V elements and shifted down. `ending`: the pieces that ends() names.
     template <bool ONCE = false>
     __device__ __forceinline__ Piece<V> load(const uint16_t *p, int i, bool ending) const
     {
@@ -186,13 +186,13 @@ __device__ __forceinline__ double divided(double s, double n, double inv_n)
 }
 
 // ---------------------------------------------------------------------------
-// Forward: y = (h - mu) / sqrt(var + eps) * gamma + beta, h = x or bf16(x + residual).  One read of a row (2 B an element, 4 with a
-// residual), one write (2, 4): mean and squared differences are taken of the registers, in fp64 as in the pass in front of the
-// FP8 cast, whose stored activation this one's equals bit for bit (fp32 in its place: no faster where memory bounds it, 54.4 us and 54.1 at 16384x2048;
-// 19.2 and 15.8 at 16384x1024, which the caches hold).  The next row is under way while one is worked on.  With a residual x and it are
-// read for the last time, and h, the stream, is next read a whole layer later: large calls load and store them past the caches (16384x2048 52.4 us,
-// 48.3, the stores alone 53.7; 8192x768, 50 MB, 13.3 and 14.3).
-// 16384x2048 with a residual 45.2 us, 5.9 TB/s; 50432x768 51; 8192x768 12.3, where issuing takes half of the time; one row of 2048 2.7.
+// Forward: y = (h - mu) / sqrt(var + eps) * gamma + beta, h = x or bf16(x + residual).  One read of a row (2 B an element, 4 with
+// a residual), one write (2, 4): mean and squared differences are taken of the registers, in fp64 as in the pass in front of the
+// FP8 cast, whose stored activation this one's equals bit for bit (fp32 in its place: no faster where memory bounds it, 54.4 us
+// and 54.1 at 16384x2048; 19.2 and 15.8 at 16384x1024, which the caches hold).  The next row is under way while one is worked on.
+// With a residual x and it are read for the last time, and h, the stream, is next read a whole layer later: large calls load and
+// store them past the caches (16384x2048 52.4 us, 48.3, the stores alone 53.7; 8192x768, 50 MB, 13.3 and 14.3). 16384x2048 with a
+// residual 45.2 us, 5.9 TB/s; 50432x768 51; 8192x768 12.3, where issuing takes half of the time; one row of 2048 2.7.
 struct LnFwdArgs {
     const uint16_t *x, *res, *gamma, *beta;
     uint16_t *h, *y;
@@ -202,7 +202,8 @@ struct LnFwdArgs {
     double eps;
 };
 
-// (four waves a SIMD: left to itself the compiler takes 130 registers for 16 elements a lane, two more than four waves have; 4096x8192 55.0 us -> 49.4)
+// (four waves a SIMD: left to itself the compiler takes 130 registers for 16 elements a lane, two more than four waves have;
+// 4096x8192 55.0 us -> 49.4)
 template <int T, int P, int V, int WAVES, bool RES, bool RAGGED, bool ONCE>
 __global__ __launch_bounds__(WAVES *kWave, 4) void ln_fwd_kernel(LnFwdArgs a)
 {
@@ -338,7 +339,8 @@ constexpr int kCus = 256;  // of an MI355X; a device with more or fewer runs the
 template <int T, int P, int V, int WAVES>
 void launch_fwd(const LnFwdArgs &a, hipStream_t s)
 {
-    // as many workgroups as hide each other's barriers: 32 waves a CU, 16 where a team is eight waves and more (4096x8192 52.5 us, with 32 54.1 before the stream went past the caches)
+    // as many workgroups as hide each other's barriers: 32 waves a CU, 16 where a team is eight waves and more (4096x8192 52.5
+    // us, with 32 54.1 before the stream went past the caches)
     constexpr int TEAMS = WAVES / T, WAVES_PER_CU = T >= 8 ? 16 : 32;
     const int64_t wanted = (a.rows + TEAMS - 1) / TEAMS, most = kCus * WAVES_PER_CU / WAVES;
     auto go = [&](auto kernel) {
@@ -355,14 +357,15 @@ void launch_fwd(const LnFwdArgs &a, hipStream_t s)
 // ---------------------------------------------------------------------------
 // Backward.  With xhat = (h - mu) rstd and w = dy gamma of a row:
 //   dx = rstd (w - mean(w) - xhat mean(w xhat)) + dres,   dgamma = sum over rows of dy xhat,   dbeta = sum over rows of dy.
-// One read of h, dy and dres, one write of dx (6 B an element, 8 with dres).  The column sums stay in registers over the rows that a
-// team works on, are added over a workgroup's teams through LDS, and leave the workgroup as one row of partial sums in the
-// workspace, which a second launch adds in their order (no atomics: the same bits on every run).  512 workgroups of eight waves, two a CU: with
-// more of them the partial sums (8 B a column and workgroup) and their addition take what the further waves gain (18912x768: 768 of them 37 us in
-// the place of 33).  fp32 throughout but for h - mu: mu is a double and is subtracted in two parts, since rows whose mean is far above their
-// deviation cancel there.  What is read here is read for the last time: large calls read past the caches (16384x2048 56.5 us, 51.2; 8192x768, 50 MB,
-// 16.9 and 17.6).  Wide rows on teams of more waves with fewer elements each: the sums' registers are what limits the waves.
-// 16384x2048 with dres 51.2 us, 5.2 TB/s (45 + 4.5 for the second launch); 18912x768 28.0, 50432x768 59.2, 8192x768 16.1; 257x1001 7.0, one launch.
+// One read of h, dy and dres, one write of dx (6 B an element, 8 with dres).  The column sums stay in registers over the rows
+// that a team works on, are added over a workgroup's teams through LDS, and leave the workgroup as one row of partial sums in the
+// workspace, which a second launch adds in their order (no atomics: the same bits on every run).  512 workgroups of eight waves,
+// two a CU: with more of them the partial sums (8 B a column and workgroup) and their addition take what the further waves gain
+// (18912x768: 768 of them 37 us in the place of 33).  fp32 throughout but for h - mu: mu is a double and is subtracted in two
+// parts, since rows whose mean is far above their deviation cancel there.  What is read here is read for the last time: large
+// calls read past the caches (16384x2048 56.5 us, 51.2; 8192x768, 50 MB, 16.9 and 17.6).  Wide rows on teams of more waves with
+// fewer elements each: the sums' registers are what limits the waves. 16384x2048 with dres 51.2 us, 5.2 TB/s (45 + 4.5 for the
+// second launch); 18912x768 28.0, 50432x768 59.2, 8192x768 16.1; 257x1001 7.0, one launch.
 struct LnBwdArgs {
     const uint16_t *dy, *h, *gamma, *dres;
     const double *stats;
@@ -392,9 +395,10 @@ __device__ __forceinline__ float dpp_sum(float v)
     return bits_to_f32((uint32_t)__builtin_amdgcn_readlane((int)f32_to_bits(v), 63));
 }
 
-// Column sums of a call of few rows (ALONE): this workgroup's 64 columns over all rows.  They need the statistics only and not the two means of
-// each row, so that other workgroups of the same launch work on dx meanwhile and nothing has to be added afterwards; h and dy are read twice, the
-// second time from the caches.  257x768 8.6 us in two launches, 6.0 in one; 512x768 8.7, 6.8; 512x4096 15.6, 10.5; 1024x768 9.0, 9.7.
+// Column sums of a call of few rows (ALONE): this workgroup's 64 columns over all rows.  They need the statistics only and not
+// the two means of each row, so that other workgroups of the same launch work on dx meanwhile and nothing has to be added
+// afterwards; h and dy are read twice, the second time from the caches.  257x768 8.6 us in two launches, 6.0 in one; 512x768 8.7,
+// 6.8; 512x4096 15.6, 10.5; 1024x768 9.0, 9.7.
 template <int V, int THREADS, bool RAGGED>
 __device__ __forceinline__ void column_sums(const LnBwdArgs &a, int group)
 {
@@ -439,8 +443,8 @@ __device__ __forceinline__ void column_sums(const LnBwdArgs &a, int group)
     }
 }
 
-// ALONE: the row sums and dx only; column_sums has the rest.  SLAB: rows of more pieces than the teams hold; blockIdx.y is the slab of T * P * 64 pieces that this workgroup works on, and a
-// launch before has left the two means of each row.
+// ALONE: the row sums and dx only; column_sums has the rest.  SLAB: rows of more pieces than the teams hold; blockIdx.y is the
+// slab of T * P * 64 pieces that this workgroup works on, and a launch before has left the two means of each row.
 template <int T, int P, int V, int WAVES, bool RES, bool RAGGED, bool SLAB, bool ONCE, bool ALONE = false>
 __global__ __launch_bounds__(WAVES *kWave) void ln_bwd_kernel(LnBwdArgs a)
 {
@@ -631,9 +635,9 @@ __global__ __launch_bounds__(kWideThreads) void ln_bwd_sums_kernel(LnBwdArgs a)
     }
 }
 
-// Adds the workgroups' partial sums: a workgroup takes 4 * kFinLanes columns of one of the two gradients, four a lane, its groups of
-// lanes every 128th row of partials, whose sums are then added in their order, all in fp64.  (Lines of 128 B a workgroup, so that there are enough
-// workgroups: 512 rows of 768 columns 4.2 us, of 256 B 5.0; a wave 64 columns 10.8.)
+// Adds the workgroups' partial sums: a workgroup takes 4 * kFinLanes columns of one of the two gradients, four a lane, its groups
+// of lanes every 128th row of partials, whose sums are then added in their order, all in fp64.  (Lines of 128 B a workgroup, so
+// that there are enough workgroups: 512 rows of 768 columns 4.2 us, of 256 B 5.0; a wave 64 columns 10.8.)
 constexpr int kFinLanes = 8, kFinThreads = 1024, kFinRows = kFinThreads / kFinLanes;
 
 __global__ __launch_bounds__(kFinThreads) void ln_bwd_finish_kernel(const float *__restrict__ partials, int groups, int cols,
@@ -739,7 +743,8 @@ hipError_t launch_layernorm_fwd(const void *x, const void *res, const void *gamm
 {
     const LnFwdArgs a{(const uint16_t *)x, (const uint16_t *)res, (const uint16_t *)gamma, (const uint16_t *)beta, (uint16_t *)h_out,
                       (uint16_t *)y, stats, rows, (int)cols, eps};
-    // the fewest lanes that hold a row with up to 16 elements each (two pieces of eight a lane are better than twice the waves: 2048 wide 53.9 us, 59.5)
+    // the fewest lanes that hold a row with up to 16 elements each (two pieces of eight a lane are better than twice the waves:
+    // 2048 wide 53.9 us, 59.5)
     if (cols <= 256)
         launch_fwd<1, 1, 4, 4>(a, s);
     else if (cols <= 512)

@@ -295,22 +295,24 @@ __global__ __launch_bounds__(kSumsqThreads) void grad_sumsq_finish_kernel(const 
 // ---------------------------------------------------------------------------
 // AdamW: with the clipped gradient g' = c g, c = min(1, max_norm / (sqrt(S) + 1e-6)),
 //   m = b1 m + (1 - b1) g',  v = b2 v + (1 - b2) g'^2,  p = p - lr wd p - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps).
-// Bound by memory: 28 B an element with fp32 states beside an fp32 copy, 22 without; 16 and 10 with 8-bit states.  A wave takes one chunk, all of
-// whose loads (20 to 28 of 4 to 16 bytes a lane) are under way before the first is waited for, and workgroups walk the tensors in order: 51 M elements with
-// master, fp32 states 241 us (6.0 TB/s), 205 M with 8-bit states 580 (5.7), without master 374 (5.5, half of its time the SIMDs issue).  Persistent
-// waves, each on a run of chunks of its own, took 301, 703 and 450; persistent ones in turns, the streams of all side by side, 284 and 665.
+// Bound by memory: 28 B an element with fp32 states beside an fp32 copy, 22 without; 16 and 10 with 8-bit states.  A wave takes
+// one chunk, all of whose loads (20 to 28 of 4 to 16 bytes a lane) are under way before the first is waited for, and workgroups
+// walk the tensors in order: 51 M elements with master, fp32 states 241 us (6.0 TB/s), 205 M with 8-bit states 580 (5.7), without
+// master 374 (5.5, half of its time the SIMDs issue).  Persistent waves, each on a run of chunks of its own, took 301, 703 and
+// 450; persistent ones in turns, the streams of all side by side, 284 and 665.
 //
 // 8-bit states: a block of 256 elements shares an fp32 step for m (E4M3 codes) and one for v (E5M2: no square root is taken on the way,
 // and 2^32 between the largest and the smallest).  A block is 16 lanes of a wave with 16 elements each, four at a time 64 apart, so that its
 // maxima are four DPP steps and the lanes' loads lie side by side.
 //
-// Rounding to codes: an E4M3 or E5M2 step is 6-25 % of the value, a moment moves by 1 - b2 (0.1-5 %) a step.  Rounded to nearest, v would stay
-// where it is for ever.  So the part that is cut off decides with a threshold that is spread evenly over [0, 1) along the steps t of
-// one element and along the elements i of one step: u = frac(i (sqrt(2) - 1) + t (sqrt(5) - 1) / 2), as 32-bit integers: a multiplication
-// and an addition, and any step can be recomputed.  Simulated over 300 steps at b2 = 0.99 (0.95, 0.999), the coded v over the exact one: mean
-// 0.985 (0.983, 0.987), spread 0.25 (0.18, 0.25); with independent random numbers 0.998, 0.29 (0.23, 0.30); to nearest 1.24 (1.08, 1.14), 0.35
-// (0.20, 0.36).  In bits: y, the scaled value times the power of two that puts the code's exponent field where fp32 has its own (codes below
-// the normal ones becoming fp32's subnormals), plus the top of u below the code's last bit, shifted.
+// Rounding to codes: an E4M3 or E5M2 step is 6-25 % of the value, a moment moves by 1 - b2 (0.1-5 %) a step.  Rounded to nearest,
+// v would stay where it is for ever.  So the part that is cut off decides with a threshold that is spread evenly over [0, 1)
+// along the steps t of one element and along the elements i of one step: u = frac(i (sqrt(2) - 1) + t (sqrt(5) - 1) / 2), as
+// 32-bit integers: a multiplication and an addition, and any step can be recomputed.  Simulated over 300 steps at b2 = 0.99
+// (0.95, 0.999), the coded v over the exact one: mean 0.985 (0.983, 0.987), spread 0.25 (0.18, 0.25); with independent random
+// numbers 0.998, 0.29 (0.23, 0.30); to nearest 1.24 (1.08, 1.14), 0.35 (0.20, 0.36).  In bits: y, the scaled value times the
+// power of two that puts the code's exponent field where fp32 has its own (codes below the normal ones becoming fp32's
+// subnormals), plus the top of u below the code's last bit, shifted.
 struct AdamwArgs {
     const Entry *table;
     int count;
