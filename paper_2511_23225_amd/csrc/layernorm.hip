@@ -9,9 +9,15 @@ namespace tweo {
 namespace {
 
 // ---------------------------------------------------------------------------
-// A row is worked on by a team of T waves; lane l of the team holds the pieces l, l + 64 T, ... of it, P of them, V elements (4 or 8:
-// 8 or 16 bytes) each, in registers.  RAGGED: cols is no multiple of V, so that rows start at any even address and their last piece is
-// short; what they cost is accesses that straddle lines (16384x2041 forward 63 us, 2048 wide 49; backward 66 and 51).  ONCE: past the caches.
+// A row is worked on by a team of T waves or, if it is narrow (a norm over the dimensions of a head), of 16 or 8 lanes of a wave
+// that has four or eight rows at once (524288x64 forward 140 us with a wave a row, 33; backward 130, 46); lane l of the team
+// holds the pieces l, l + 64 T, ... of it, P of them, V elements (4 or 8: 8 or 16 bytes) each, in registers.  RAGGED: cols is no
+// multiple of V, so that rows start at any even address and their last piece is short; what they cost is accesses that straddle
+// lines (16384x2041 forward 63 us, 2048 wide 49; backward 66 and 51).  ONCE: past the caches.
+
+// T = 0 and -1: 16 and 8 lanes
+template <int T>
+constexpr int kLanes = T < 0 ? 8 : T == 0 ? 16 : T * kWave;
 
 template <int V>
 struct Piece {
@@ -37,11 +43,11 @@ struct Row {
         const int left = cols - V * i;
         return left < 0 ? 0 : left < V ? left : V;
     }
-    // whether one of the 64 T pieces from i0 on is a ragged row's short one (the same for all lanes)
+    // whether one of the team's pieces from i0 on is a ragged row's short one (the same for all lanes)
     template <int T>
     __device__ __forceinline__ bool ends(int i0) const
     {
-        return RAGGED && pieces > i0 && pieces <= i0 + T * kWave;
+        return RAGGED && pieces > i0 && pieces <= i0 + kLanes<T>;
     }
     // Piece i, zeros behind a ragged row's end.  Without branches, around which the compiler would wait for one load before it
     // issues the next (4096x4093 backward 60.4 us, now 44.6): a lane without a piece gets the row's last one, and a short piece
@@ -152,11 +158,37 @@ __device__ __forceinline__ double squares64(const Piece<V> &v, double mean, int 
     return n > 0 ? s : 0.0;
 }
 
+// Sum over the lanes of a narrow row's team: its lanes are in one DPP row, and other teams of the wave may have returned.
+template <int CTRL>
+__device__ __forceinline__ double dpp_add_within(double v)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, 0xF, 0xF, false),
+                   hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, 0xF, 0xF, false);
+    return v + __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
+}
+template <int CTRL>
+__device__ __forceinline__ float dpp_add_within(float v)
+{
+    return v + bits_to_f32((uint32_t)__builtin_amdgcn_update_dpp(0, (int)f32_to_bits(v), CTRL, 0xF, 0xF, false));
+}
+// sum over 8 or 16 lanes (a DPP row), in all of them
+template <int LANES, typename F>
+__device__ __forceinline__ F row_sum(F v)
+{
+    v = dpp_add_within<0xB1>(v);   // quad_perm: 1 0 3 2
+    v = dpp_add_within<0x4E>(v);   // quad_perm: 2 3 0 1
+    v = dpp_add_within<0x141>(v);  // row_half_mirror
+    return LANES == 8 ? v : dpp_add_within<0x140>(v);  // row_mirror
+}
+
 // Sum over the T waves of a team: of each wave through DPP, then through LDS, added in the waves' order by all of them.  `red`: the
 // T words of this team for this sum, which are free again two barriers later.
 template <int T>
 __device__ __forceinline__ double team_sum(double v, double *red, int wave)
 {
+    if constexpr (T <= 0)
+        return row_sum<kLanes<T>>(v);
     v = wave_sum_f64(v);
     if constexpr (T > 1) {
         if ((threadIdx.x & (kWave - 1)) == 0)
@@ -207,10 +239,10 @@ struct LnFwdArgs {
 template <int T, int P, int V, int WAVES, bool RES, bool RAGGED, bool ONCE>
 __global__ __launch_bounds__(WAVES *kWave, 4) void ln_fwd_kernel(LnFwdArgs a)
 {
-    constexpr int TEAMS = WAVES / T;
+    constexpr int TEAMS = WAVES * kWave / kLanes<T>;
     constexpr bool AHEAD = !RAGGED;  // (ragged rows: 16384x2041 80 us with it, 63 without)
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), team = wave / T;
-    const int lane = (int)threadIdx.x - team * T * kWave;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), team = T <= 0 ? (int)threadIdx.x / kLanes<T> : wave / std::max(T, 1);
+    const int lane = (int)threadIdx.x - team * kLanes<T>;
     const Row<V, RAGGED> row(a.cols);
     const double n = (double)a.cols, inv_n = 1.0 / n;
     __shared__ double red[2][WAVES];
@@ -220,10 +252,10 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void ln_fwd_kernel(LnFwdArgs a)
         const int64_t r = r0 + team < a.rows ? r0 + team : a.rows - 1, at = r * a.cols;
 #pragma unroll
         for (int u = 0; u < P; ++u) {
-            const bool ending = row.template ends<T>(u * T * kWave);
-            nx[u] = row.template load<ONCE>(a.x + at, lane + u * T * kWave, ending);
+            const bool ending = row.template ends<T>(u * kLanes<T>);
+            nx[u] = row.template load<ONCE>(a.x + at, lane + u * kLanes<T>, ending);
             if constexpr (RES)
-                nr[u] = row.template load<ONCE>(a.res + at, lane + u * T * kWave, ending);
+                nr[u] = row.template load<ONCE>(a.res + at, lane + u * kLanes<T>, ending);
         }
     };
     if (AHEAD && (int64_t)blockIdx.x * TEAMS < a.rows)
@@ -231,8 +263,8 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void ln_fwd_kernel(LnFwdArgs a)
     float gamma[P][V], beta[P][V];
 #pragma unroll
     for (int u = 0; u < P; ++u) {
-        const int i = lane + u * T * kWave;
-        const bool ending = row.template ends<T>(u * T * kWave);
+        const int i = lane + u * kLanes<T>;
+        const bool ending = row.template ends<T>(u * kLanes<T>);
         const Piece<V> g = row.load(a.gamma, i, ending), b = a.beta != nullptr ? row.load(a.beta, i, ending) : nothing_added<V>();
 #pragma unroll
         for (int k = 0; k < V; ++k)
@@ -241,7 +273,7 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void ln_fwd_kernel(LnFwdArgs a)
     for (int64_t r0 = (int64_t)blockIdx.x * TEAMS; r0 < a.rows; r0 += (int64_t)gridDim.x * TEAMS) {
         const bool mine = r0 + team < a.rows;
         const int64_t r = mine ? r0 + team : a.rows - 1, at = r * a.cols;
-        if (T == 1 && !mine)
+        if (T <= 1 && !mine)
             return;
         if (!AHEAD)
             request(r0);
@@ -258,20 +290,20 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void ln_fwd_kernel(LnFwdArgs a)
         double s = 0.0;
 #pragma unroll
         for (int u = 0; u < P; ++u) {
-            const int i = lane + u * T * kWave;
+            const int i = lane + u * kLanes<T>;
             if (RES && mine)
                 row.template store<ONCE>(a.h + at, i, c[u]);
             const double t = sum64(c[u]);
             s += row.count(i) > 0 ? t : 0.0;
         }
-        const double mean = divided(team_sum<T>(s, &red[0][team * T], wave - team * T), n, inv_n);
+        const double mean = divided(team_sum<T>(s, red[0] + team * std::max(T, 0), wave - team * T), n, inv_n);
         double ss = 0.0;
 #pragma unroll
         for (int u = 0; u < P; ++u) {
             c[u].keep();
-            ss += squares64<V, RAGGED>(c[u], mean, row.count(lane + u * T * kWave));
+            ss += squares64<V, RAGGED>(c[u], mean, row.count(lane + u * kLanes<T>));
         }
-        const double rstd = rsqrt64(__builtin_fma(team_sum<T>(ss, &red[1][team * T], wave - team * T), inv_n, a.eps));
+        const double rstd = rsqrt64(__builtin_fma(team_sum<T>(ss, red[1] + team * std::max(T, 0), wave - team * T), inv_n, a.eps));
         if (!mine)
             continue;
         if (a.stats != nullptr && lane == 0) {
@@ -283,7 +315,7 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void ln_fwd_kernel(LnFwdArgs a)
             c[u].keep();
             Piece<V> y;
             ln_pairs<V, true>(c[u].w, mean, rstd, gamma[u], beta[u], true, y.w);
-            row.store(a.y + at, lane + u * T * kWave, y);
+            row.store(a.y + at, lane + u * kLanes<T>, y);
         }
     }
 }
@@ -341,7 +373,7 @@ void launch_fwd(const LnFwdArgs &a, hipStream_t s)
 {
     // as many workgroups as hide each other's barriers: 32 waves a CU, 16 where a team is eight waves and more (4096x8192 52.5
     // us, with 32 54.1 before the stream went past the caches)
-    constexpr int TEAMS = WAVES / T, WAVES_PER_CU = T >= 8 ? 16 : 32;
+    constexpr int TEAMS = WAVES * kWave / kLanes<T>, WAVES_PER_CU = T >= 8 ? 16 : 32;
     const int64_t wanted = (a.rows + TEAMS - 1) / TEAMS, most = kCus * WAVES_PER_CU / WAVES;
     auto go = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(wanted, most)), dim3(WAVES * kWave), 0, s, a);
@@ -448,13 +480,13 @@ __device__ __forceinline__ void column_sums(const LnBwdArgs &a, int group)
 template <int T, int P, int V, int WAVES, bool RES, bool RAGGED, bool SLAB, bool ONCE, bool ALONE = false>
 __global__ __launch_bounds__(WAVES *kWave) void ln_bwd_kernel(LnBwdArgs a)
 {
-    constexpr int TEAMS = WAVES / T;
+    constexpr int TEAMS = WAVES * kWave / kLanes<T>;
     if constexpr (ALONE)
         if ((int)blockIdx.x >= a.row_groups)
             return column_sums<V, WAVES * kWave, RAGGED>(a, (int)blockIdx.x - a.row_groups);
     const int64_t stride_rows = (int64_t)(ALONE ? a.row_groups : (int)gridDim.x) * TEAMS;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), team = wave / T;
-    const int lane = (int)threadIdx.x - team * T * kWave, first = SLAB ? (int)blockIdx.y * T * P * kWave : 0;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), team = T <= 0 ? (int)threadIdx.x / kLanes<T> : wave / std::max(T, 1);
+    const int lane = (int)threadIdx.x - team * kLanes<T>, first = SLAB ? (int)blockIdx.y * P * kLanes<T> : 0;
     const Row<V, RAGGED> row(a.cols);
     const float inv_n = 1.0f / (float)a.cols;
     __shared__ float2 red[2][WAVES];
@@ -469,8 +501,8 @@ __global__ __launch_bounds__(WAVES *kWave) void ln_bwd_kernel(LnBwdArgs a)
         const int64_t r = r0 + team < a.rows ? r0 + team : a.rows - 1, at = r * a.cols;
 #pragma unroll
         for (int u = 0; u < P; ++u) {
-            const int i = first + lane + u * T * kWave;
-            const bool ending = row.template ends<T>(first + u * T * kWave);
+            const int i = first + lane + u * kLanes<T>;
+            const bool ending = row.template ends<T>(first + u * kLanes<T>);
             nh[u] = row.template load<ONCE>(a.h + at, i, ending);
             ndy[u] = row.template load<ONCE>(a.dy + at, i, ending);
             if constexpr (RES)
@@ -482,8 +514,8 @@ __global__ __launch_bounds__(WAVES *kWave) void ln_bwd_kernel(LnBwdArgs a)
         request((int64_t)blockIdx.x * TEAMS);
 #pragma unroll
     for (int u = 0; u < P; ++u) {
-        const int i = first + lane + u * T * kWave;
-        const Piece<V> g = row.load(a.gamma, i, row.template ends<T>(first + u * T * kWave));
+        const int i = first + lane + u * kLanes<T>;
+        const Piece<V> g = row.load(a.gamma, i, row.template ends<T>(first + u * kLanes<T>));
 #pragma unroll
         for (int k = 0; k < V; ++k) {
             gamma[u][k] = g.at(k);
@@ -526,7 +558,7 @@ __global__ __launch_bounds__(WAVES *kWave) void ln_bwd_kernel(LnBwdArgs a)
                 }
             }
             // (a lane without a piece has another's; its column sums are not stored)
-            const bool some = row.count(first + lane + u * T * kWave) > 0;
+            const bool some = row.count(first + lane + u * kLanes<T>) > 0;
             c1 += some ? t1 : 0.0f;
             c2 += some ? t2 : 0.0f;
         }
@@ -534,8 +566,8 @@ __global__ __launch_bounds__(WAVES *kWave) void ln_bwd_kernel(LnBwdArgs a)
             c2 = a.sums[2 * r];
             c1 = a.sums[2 * r + 1];
         } else {
-            c1 = dpp_sum(c1);
-            c2 = dpp_sum(c2);
+            c1 = T <= 0 ? row_sum<kLanes<T>>(c1) : dpp_sum(c1);
+            c2 = T <= 0 ? row_sum<kLanes<T>>(c2) : dpp_sum(c2);
             if constexpr (T > 1) {
                 if ((threadIdx.x & (kWave - 1)) == 0)
                     red[turn][wave] = make_float2(c1, c2);
@@ -568,13 +600,13 @@ __global__ __launch_bounds__(WAVES *kWave) void ln_bwd_kernel(LnBwdArgs a)
                 }
                 out.w[k] = pack_bf16x2(v[0], v[1]);
             }
-            row.store(a.dx + at, first + lane + u * T * kWave, out);
+            row.store(a.dx + at, first + lane + u * kLanes<T>, out);
         }
     }
     if constexpr (ALONE)
         return;
     // the teams' column sums through LDS, then added in the teams' order, four columns a thread
-    __shared__ float sums[TEAMS][P * V][T * kWave];
+    __shared__ float sums[TEAMS][P * V][kLanes<T>];
     const int stride = (a.cols + 3) & ~3;
     float *out = a.partials + (int64_t)blockIdx.x * 2 * stride;
 #pragma unroll
@@ -587,13 +619,13 @@ __global__ __launch_bounds__(WAVES *kWave) void ln_bwd_kernel(LnBwdArgs a)
             for (int k = 0; k < V; ++k)
                 sums[team][u * V + k][lane] = which ? dbeta[u][k] : dgamma[u][k];
         __syncthreads();
-        constexpr int QUADS = T * P * kWave * V / 4;
+        constexpr int QUADS = kLanes<T> * P * V / 4;
 #pragma unroll
         for (int q0 = 0; q0 < QUADS; q0 += WAVES * kWave) {
-            const int q = q0 + (int)threadIdx.x, l = q % (T * kWave), part = q / (T * kWave);
+            const int q = q0 + (int)threadIdx.x, l = q % kLanes<T>, part = q / kLanes<T>;
             if (QUADS % (WAVES * kWave) != 0 && q >= QUADS)
                 break;
-            const int col = V * (first + l + part / (V / 4) * T * kWave) + part % (V / 4) * 4;
+            const int col = V * (first + l + part / (V / 4) * kLanes<T>) + part % (V / 4) * 4;
             float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int t = 0; t < TEAMS; ++t)
@@ -671,7 +703,9 @@ __global__ __launch_bounds__(kFinThreads) void ln_bwd_finish_kernel(const float 
 // few rows, of which a workgroup can take 64 columns as fast as others the rows
 bool bwd_alone(int64_t rows, int64_t cols) { return rows <= 512 && cols <= 8192; }
 
-// What a backward call runs on: T, P, V and WAVES of the kernel, the fewest lanes that hold a row.
+// What a backward call runs on: T, P, V and WAVES of the kernel, the fewest lanes that hold a row with 4 to 16 elements each, but
+// 64 for the widths to 256: 16 elements on each of 16 lanes are better on long calls (131072x256 42.3 us, 46.6) and worse
+// on others (20000x200 16.2, 13.4; 65536x256 33.5, 32.0).  64 columns on 8 lanes: 65536x64 15.5, on 16 13.7; 524288x64 42.0, 45.9.
 struct BwdShape {
     int waves_a_row, pieces, elements, waves;
     bool wide;
@@ -679,6 +713,10 @@ struct BwdShape {
 
 BwdShape bwd_shape(int64_t cols)
 {
+    if (cols <= 64)
+        return {0, 1, 4, 8, false};
+    if (cols <= 128)
+        return {0, 1, 8, 8, false};
     if (cols <= 256)
         return {1, 1, 4, 8, false};
     if (cols <= 512)
@@ -699,7 +737,8 @@ BwdShape bwd_shape(int64_t cols)
 // workgroups, each of which leaves a row of partial sums; of wide rows so many for each slab of columns
 int bwd_groups(int64_t rows, int64_t cols, const BwdShape &b)
 {
-    const int64_t teams = b.waves / b.waves_a_row, slab = (int64_t)b.waves_a_row * b.pieces * kWave * b.elements;
+    const int64_t lanes = b.waves_a_row == 0 ? kLanes<0> : b.waves_a_row * kWave,
+                   teams = b.waves * kWave / lanes, slab = lanes * b.pieces * b.elements;
     const int64_t slabs = b.wide ? (cols + slab - 1) / slab : 1, most = 16 * kCus / b.waves;
     return (int)std::min<int64_t>((rows + teams - 1) / teams, std::max<int64_t>(1, most / slabs));
 }
@@ -709,7 +748,7 @@ size_t partial_floats(int64_t cols, int groups) { return (size_t)groups * 2 * (s
 template <int T, int P, int V, int WAVES, bool SLAB = false>
 void launch_bwd(const LnBwdArgs &a, int groups, hipStream_t s)
 {
-    const unsigned slabs = SLAB ? (unsigned)((a.cols + T * P * kWave * V - 1) / (T * P * kWave * V)) : 1u;
+    const unsigned slabs = SLAB ? (unsigned)((a.cols + kLanes<T> * P * V - 1) / (kLanes<T> * P * V)) : 1u;
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)groups, slabs), dim3(WAVES * kWave), 0, s, a); };
     if constexpr (!SLAB)
         if (bwd_alone(a.rows, a.cols)) {
@@ -743,10 +782,14 @@ hipError_t launch_layernorm_fwd(const void *x, const void *res, const void *gamm
 {
     const LnFwdArgs a{(const uint16_t *)x, (const uint16_t *)res, (const uint16_t *)gamma, (const uint16_t *)beta, (uint16_t *)h_out,
                       (uint16_t *)y, stats, rows, (int)cols, eps};
-    // the fewest lanes that hold a row with up to 16 elements each (two pieces of eight a lane are better than twice the waves:
-    // 2048 wide 53.9 us, 59.5)
-    if (cols <= 256)
-        launch_fwd<1, 1, 4, 4>(a, s);
+    // the fewest lanes that hold a row with 8 to 16 elements each (131072x256 on 16 lanes 29.9 us, on 64 41.0; two pieces of
+    // eight a lane are better than twice the waves: 2048 wide 53.9 us, 59.5)
+    if (cols <= 64)
+        launch_fwd<-1, 1, 8, 4>(a, s);
+    else if (cols <= 128)
+        launch_fwd<0, 1, 8, 4>(a, s);
+    else if (cols <= 256)
+        launch_fwd<0, 2, 8, 4>(a, s);
     else if (cols <= 512)
         launch_fwd<1, 1, 8, 4>(a, s);
     else if (cols <= 768)
@@ -801,6 +844,8 @@ hipError_t launch_layernorm_bwd(const void *dy, const void *h, const void *gamma
         launch_bwd<16, 1, 8, 16, true>(a, groups, s);
     } else {
         switch (b.waves_a_row * 100 + b.pieces * 10 + b.elements) {
+        case 14: launch_bwd<0, 1, 4, 8>(a, groups, s); break;
+        case 18: launch_bwd<0, 1, 8, 8>(a, groups, s); break;
         case 114: launch_bwd<1, 1, 4, 8>(a, groups, s); break;
         case 118: launch_bwd<1, 1, 8, 8>(a, groups, s); break;
         case 134: launch_bwd<1, 3, 4, 8>(a, groups, s); break;

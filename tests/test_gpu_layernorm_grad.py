@@ -4,8 +4,9 @@ Forward: the kernel normalises in fp64 like the oracle in another summation orde
 the fp64 value lies within 1e-10 of a rounding boundary, and the statistics agree to 1e-12.
 Backward: fp32, one rounding to bf16 (half a step, 2^-8 of the value).  The fp32 part: with S the sum of the magnitudes of a
 result's terms, a sum over a lane's 16 elements, a wave's 6 levels and 8 waves, and the 10 roundings of each term, are within
-64 * 2^-24 S.  Column sums: a team's rows one after the other, 8 teams after each other, fp64 then, one rounding to fp32 and 6
-roundings in each term: (rows a team + 16) * 2^-24 S."""
+64 * 2^-24 S.  Column sums: a team's rows one after the other, then a workgroup's teams (8, or 32 where a row has 16 lanes), fp64
+then, one rounding to fp32 and 6 roundings in each term; of up to 512 rows 16 one after the other, and the same 7: (rows a team
++ 24) * 2^-24 S, + 40 of up to 128 columns."""
 import numpy as np
 import pytest
 import torch
@@ -55,6 +56,7 @@ SHAPES = [(1, 1), (3, 2), (2, 7), (5, 8), (4, 9), (1, 2048), (17, 64), (9, 255),
           (13, 1025), (40, 1536), (7, 2048), (6, 2049), (11, 4096), (5, 4104), (3, 8192), (4, 8193), (2, 8200), (3, 16384), (2, 16392), (2, 16385),
           (3, 32776), (2, 33001), (5000, 24), (4099, 768), (3, 253), (3, 257),
           (3, 509), (3, 767), (3, 769), (3, 1023), (3, 1531), (3, 1537), (3, 2047), (3, 4095), (3, 8191), (2, 16383), (300, 8200), (700, 5632),
+          (1500, 64), (3001, 61), (1500, 128), (1403, 100), (700, 65), (2001, 129), (999, 256), (1301, 200), (600, 8), (601, 5), (777, 16), (515, 1),
           (512, 768), (513, 768), (512, 1001), (511, 8192), (512, 250), (65, 61)]
 
 
@@ -89,7 +91,7 @@ def test_forward(shape, residual, beta):
     assert torch.equal(y, again)
 
 
-@pytest.mark.parametrize("cols", [3, 48, 777, 768, 1000, 2048, 16392, 33001])
+@pytest.mark.parametrize("cols", [3, 48, 100, 256, 777, 768, 1000, 2048, 16392, 33001])
 def test_rows_of_one_value(cols):
     """Variance 0: every difference is a zero, whatever 1 / cols rounds to, and y is beta, or a zero whose sign the gain decides."""
     values = np.float32([5.5, -0.1, 3e38, 1e-39, 1 / 3, 0.0, 7.0, -1e30])
@@ -151,8 +153,9 @@ def check_backward(t, hb, stats, got, residual=True, beta=True, rows_ok=slice(No
     dx, dgamma, dbeta, size, sg, sb = training.layernorm_bwd(f64(t["dy"]), f64(hb), f64(t["gamma"]), stats, f64(t["dres"]) if residual else None)
     far = np.abs(f64(bf16_bits(got[0])) - dx)
     assert np.all((far <= 2.0 ** -8 * np.abs(dx) + 64 * 2.0 ** -24 * size)[rows_ok]), np.nanmax(far / (size + 1e-300))
-    # 512 workgroups of one team of eight waves, 256 of sixteen
-    chain = (-(-rows // (512 if t["dy"].shape[1] <= 4096 else 256)) + 16) * 2.0 ** -24
+    # 512 workgroups of one team of eight waves, 256 of sixteen; of narrow rows 512 workgroups of 32 teams
+    cols = t["dy"].shape[1]
+    chain = (-(-rows // 16384) + 40 if cols <= 128 else -(-rows // (512 if cols <= 4096 else 256)) + 24) * 2.0 ** -24
     for name, g, ref, s in (("dgamma", got[1], dgamma, sg),) + ((("dbeta", got[2], dbeta, sb),) if beta else ()):
         far = np.abs(g.cpu().numpy().astype(np.float64) - ref)
         assert np.all(far <= chain * s + 1e-30), (name, (far / (s + 1e-300)).max(), chain)
@@ -191,7 +194,7 @@ def test_backward_of_the_norm_in_front_of_a_cast():
         check_backward(t, hb, stats, backward(t, h, tw.layernorm_stats(ws, rows)))
 
 
-@pytest.mark.parametrize("shape", [(17501, 768), (3301, 4096), (52000, 256), (1601, 8200)])
+@pytest.mark.parametrize("shape", [(17501, 768), (3301, 4096), (52000, 256), (1601, 8200), (230001, 64), (110003, 128)])
 def test_streams_beyond_the_caches(shape):
     """Calls of more than 100 MB, which read and store past the caches; the second in place."""
     rows, cols = shape
@@ -257,7 +260,7 @@ def test_rows_whose_mean_is_far_above_their_deviation():
     check_backward(t, t["x"], st.cpu().numpy(), backward(t, to_dev_bf16(t["x"]), st))
 
 
-@pytest.mark.parametrize("cols", [768, 1001, 4096, 16392])
+@pytest.mark.parametrize("cols", [64, 100, 200, 768, 1001, 4096, 16392])
 def test_poisoned_rows_stay_by_themselves(cols):
     rows = 24
     t = inputs(rows, cols, 4)
@@ -277,7 +280,7 @@ def test_poisoned_rows_stay_by_themselves(cols):
     assert bool(torch.isnan(dgamma).all()) and torch.equal(dbeta, good[2])
 
 
-@pytest.mark.parametrize("cols", [3, 300, 768, 777, 1001, 2048, 4100, 8192, 16392])
+@pytest.mark.parametrize("cols", [3, 64, 61, 128, 250, 300, 768, 777, 1001, 2048, 4100, 8192, 16392])
 def test_gradients_that_are_not_finite(cols):
     """Infinities and NaNs wherever they lie in a row: what fp64 arithmetic makes of them, in the same places, and the other rows' bits."""
     rows = 9
@@ -295,7 +298,7 @@ def test_gradients_that_are_not_finite(cols):
     assert torch.equal(got[0][7:], clean[0][7:]) and torch.equal(got[0][6, :-1], clean[0][6, :-1])
 
 
-@pytest.mark.parametrize("shape", [(37, 768), (5, 4096), (6, 1001), (3, 33000), (512, 768), (700, 768), (300, 1001)])
+@pytest.mark.parametrize("shape", [(37, 768), (5, 4096), (6, 1001), (3, 33000), (512, 768), (700, 768), (300, 1001), (701, 64), (603, 121)])
 def test_in_place(shape):
     rows, cols = shape
     t = inputs(rows, cols, 9)
