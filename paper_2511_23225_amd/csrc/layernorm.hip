@@ -543,9 +543,13 @@ __global__ __launch_bounds__(WAVES *kWave) void ln_bwd_kernel(LnBwdArgs a)
 #pragma unroll
         for (int u = 0; u < P; ++u) {
             float t1 = 0.0f, t2 = 0.0f;
+            const int count = row.count(first + lane + u * kLanes<T>);
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 xhat[u][k] = __builtin_fmaf(h[u].at(k) - mean_hi, rstd, shift);
+                // behind a ragged row's end (0 - mean) * rstd may be infinite, and w is 0 there
+                if (RAGGED && k > 0)
+                    xhat[u][k] = k < count ? xhat[u][k] : 0.0f;
                 const float d = dy[u].at(k);
                 w[u][k] = d * gamma[u][k];
                 if constexpr (!SLAB) {
@@ -558,9 +562,8 @@ __global__ __launch_bounds__(WAVES *kWave) void ln_bwd_kernel(LnBwdArgs a)
                 }
             }
             // (a lane without a piece has another's; its column sums are not stored)
-            const bool some = row.count(first + lane + u * kLanes<T>) > 0;
-            c1 += some ? t1 : 0.0f;
-            c2 += some ? t2 : 0.0f;
+            c1 += count > 0 ? t1 : 0.0f;
+            c2 += count > 0 ? t2 : 0.0f;
         }
         if constexpr (SLAB) {
             c2 = a.sums[2 * r];
@@ -652,9 +655,11 @@ __global__ __launch_bounds__(kWideThreads) void ln_bwd_sums_kernel(LnBwdArgs a)
         float c1 = 0.0f, c2 = 0.0f;
         for (int i = threadIdx.x; i < row.pieces; i += kWideThreads) {
             const Piece<8> h = row.load(a.h + r * a.cols, i, true), dy = row.load(a.dy + r * a.cols, i, true), g = row.load(a.gamma, i, true);
+            const int count = row.count(i);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const float xhat = __builtin_fmaf(h.at(k) - mean_hi, rstd, shift), w = dy.at(k) * g.at(k);
+                // (behind a ragged row's end as in ln_bwd_kernel)
+                const float xhat = !RAGGED || k < count ? __builtin_fmaf(h.at(k) - mean_hi, rstd, shift) : 0.0f, w = dy.at(k) * g.at(k);
                 c2 += w;
                 c1 = __builtin_fmaf(w, xhat, c1);
             }
