@@ -411,6 +411,21 @@ struct LnBwdArgs {
     float *dgamma, *dbeta;
 };
 
+// xhat = (h - mu) rstd in fp32.  Where rstd is below 1 both factors are taken by halves and twice, which changes no bit but where h - mu
+// itself, of values near bf16's largest, is beyond fp32.
+struct Normalizer {
+    float scale, mean, rstd, shift;
+    __device__ __forceinline__ Normalizer(double mean_d, double rstd_d)
+    {
+        const float mean_hi = (float)mean_d, r = (float)rstd_d;
+        scale = r < 1.0f ? 0.5f : 1.0f;
+        mean = mean_hi * scale;
+        rstd = r < 1.0f ? 2.0f * r : r;
+        shift = (float)(mean_d - (double)mean_hi) * -r;
+    }
+    __device__ __forceinline__ float operator()(float h) const { return __builtin_fmaf(__builtin_fmaf(h, scale, -mean), rstd, shift); }
+};
+
 __device__ __forceinline__ float dpp_sum(float v)
 {
     auto add = [](float x, auto ctrl, auto mask) {
@@ -444,11 +459,10 @@ __device__ __forceinline__ void column_sums(const LnBwdArgs &a, int group)
 #pragma unroll 4
     for (int64_t r = part; r < a.rows; r += PARTS) {
         const Piece<V> h = row.load(a.h + r * a.cols, i, true), dy = row.load(a.dy + r * a.cols, i, true);
-        const double mean = a.stats[2 * r];
-        const float mean_hi = (float)mean, rstd = (float)a.stats[2 * r + 1], shift = (float)(mean - (double)mean_hi) * -rstd;
+        const Normalizer normalized(a.stats[2 * r], a.stats[2 * r + 1]);
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            dgamma[k] = __builtin_fmaf(dy.at(k), __builtin_fmaf(h.at(k) - mean_hi, rstd, shift), dgamma[k]);
+            dgamma[k] = __builtin_fmaf(dy.at(k), normalized(h.at(k)), dgamma[k]);
             dbeta[k] += dy.at(k);
         }
     }
@@ -534,8 +548,8 @@ __global__ __launch_bounds__(WAVES *kWave) void ln_bwd_kernel(LnBwdArgs a)
             if constexpr (RES)
                 dres[u] = ndres[u];
         }
-        const double mean = nmean;
-        const float mean_hi = (float)mean, rstd = (float)nrstd, shift = (float)(mean - (double)mean_hi) * -rstd;
+        const Normalizer normalized(nmean, nrstd);
+        const float rstd = (float)nrstd;
         if (AHEAD && r0 + stride_rows < a.rows)
             request(r0 + stride_rows);
         float c1 = 0.0f, c2 = 0.0f;  // sums of w xhat, w; then their means
@@ -546,7 +560,7 @@ __global__ __launch_bounds__(WAVES *kWave) void ln_bwd_kernel(LnBwdArgs a)
             const int count = row.count(first + lane + u * kLanes<T>);
 #pragma unroll
             for (int k = 0; k < V; ++k) {
-                xhat[u][k] = __builtin_fmaf(h[u].at(k) - mean_hi, rstd, shift);
+                xhat[u][k] = normalized(h[u].at(k));
                 // behind a ragged row's end (0 - mean) * rstd may be infinite, and w is 0 there
                 if (RAGGED && k > 0)
                     xhat[u][k] = k < count ? xhat[u][k] : 0.0f;
@@ -650,8 +664,7 @@ __global__ __launch_bounds__(kWideThreads) void ln_bwd_sums_kernel(LnBwdArgs a)
     const Row<8, RAGGED> row(a.cols);
     __shared__ double red[2][T];
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        const double mean = a.stats[2 * r];
-        const float mean_hi = (float)mean, rstd = (float)a.stats[2 * r + 1], shift = (float)(mean - (double)mean_hi) * -rstd;
+        const Normalizer normalized(a.stats[2 * r], a.stats[2 * r + 1]);
         float c1 = 0.0f, c2 = 0.0f;
         for (int i = threadIdx.x; i < row.pieces; i += kWideThreads) {
             const Piece<8> h = row.load(a.h + r * a.cols, i, true), dy = row.load(a.dy + r * a.cols, i, true), g = row.load(a.gamma, i, true);
@@ -659,7 +672,7 @@ __global__ __launch_bounds__(kWideThreads) void ln_bwd_sums_kernel(LnBwdArgs a)
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 // (behind a ragged row's end as in ln_bwd_kernel)
-                const float xhat = !RAGGED || k < count ? __builtin_fmaf(h.at(k) - mean_hi, rstd, shift) : 0.0f, w = dy.at(k) * g.at(k);
+                const float xhat = !RAGGED || k < count ? normalized(h.at(k)) : 0.0f, w = dy.at(k) * g.at(k);
                 c2 += w;
                 c1 = __builtin_fmaf(w, xhat, c1);
             }

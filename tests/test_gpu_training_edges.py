@@ -27,3 +27,28 @@ def test_backward_of_rows_of_one_value(rows, cols):
         got = backward(t, to_dev_bf16(t["x"]), st, residual)
         assert bool(torch.isfinite(got[0].float()).all()) and not bool(got[1].any())
         check_backward(t, t["x"], st.cpu().numpy(), got, residual)
+
+
+@pytest.mark.parametrize("cols", [8, 61, 64, 250, 768, 1001, 4096, 8192, 8200])
+def test_backward_of_values_near_the_largest(cols):
+    """h - mean has no place in fp32 where values of 3e38 have both signs, xhat has.  rstd is about 2^-128 there, a subnormal with 21 bits: 4 of
+    the roundings that `check_backward` counts 64 and 24 of.  The gradients are scaled so that dx (1e-36) is a normal bf16 number; terms of
+    it that cancel are off by fp32's least step."""
+    rows = 11
+    say("largest values", cols)
+    rng = np.random.default_rng(cols)
+    t = inputs(rows, cols, 32)
+    x = np.where(rng.random((rows, cols)) < 0.5, 3e38, -3e38) * rng.uniform(0.7, 1.0, (rows, cols))
+    x[0], x[1] = -3.3e38, 3.3e38
+    x[0, cols // 2], x[1, cols - 1] = 3.3e38, -3.3e38  # the mean at one end, one value at the other
+    t["x"] = synth.f32_to_bf16_bits(x.astype(np.float32))
+    t["dy"] = synth.f32_to_bf16_bits((rng.standard_normal((rows, cols)) * 4096).astype(np.float32))
+    _, _, st = forward(t, cols, False, True)
+    stats = training.layernorm_stats(f64(t["x"]), float(np.float32(EPS)))
+    assert np.allclose(st.cpu().numpy(), stats, rtol=1e-12, atol=0)
+    dx, dgamma, dbeta = backward(t, to_dev_bf16(t["x"]), st, residual=False)
+    want = training.layernorm_bwd(f64(t["dy"]), f64(t["x"]), f64(t["gamma"]), stats)
+    far = np.abs(f64(bf16_bits(dx)) - want[0])
+    assert np.all(far <= 2.0 ** -8 * np.abs(want[0]) + 64 * 2.0 ** -24 * want[3] + 2.0 ** -134 + 8 * 2.0 ** -149)
+    for g, ref, s in ((dgamma, want[1], want[4]), (dbeta, want[2], want[5])):
+        assert np.all(np.abs(g.cpu().numpy().astype(np.float64) - ref) <= 25 * 2.0 ** -24 * s)
