@@ -574,7 +574,7 @@ tweo_status tweo_layernorm_bwd(const void *dy_bf16, const void *h_bf16, const vo
         return TWEO_ERR_INVALID_ARG;
     if (rows > kMaxDim || cols > kMaxCols)
         return TWEO_ERR_UNSUPPORTED;
-    if (!workspace || !aligned16(workspace) || workspace_bytes < layernorm_bwd_bytes(rows, cols))
+    if (!workspace || !aligned16(workspace) || workspace_bytes < std::max<size_t>(256, layernorm_bwd_bytes(rows, cols)))
         return TWEO_ERR_WORKSPACE;
     return hip_status(launch_layernorm_bwd(dy_bf16, h_bf16, gamma_bf16, stats, residual_grad_bf16, rows, cols, dx_bf16, dgamma,
                                            dbeta, workspace, (hipStream_t)stream));

@@ -838,6 +838,8 @@ hipError_t launch_layernorm_fwd(const void *x, const void *res, const void *gamm
 
 size_t layernorm_bwd_bytes(int64_t rows, int64_t cols)
 {
+    if (bwd_alone(rows, cols))
+        return 0;
     const BwdShape b = bwd_shape(cols);
     return (partial_floats(cols, bwd_groups(rows, cols, b)) + (b.wide ? 2 * (size_t)rows : 0)) * sizeof(float);
 }
