@@ -222,7 +222,7 @@ tweo_status tweo_layernorm_quantize_e4m3_delayed(const void *x_bf16, const void 
  *   stats_out NULL or fp64 [rows][2]: (mu, 1 / sqrt(var + eps)), as the LayerNorm -> cast
  *   calls leave them in their workspace from byte 2304 on.
  * Needs no workspace.  Errors: TWEO_ERR_INVALID_ARG (null, misaligned, negative or NaN
- * eps, residual without h_out, h_out == y), TWEO_ERR_UNSUPPORTED (rows above 2^30 or
+ * eps, residual without h_out, any other overlap), TWEO_ERR_UNSUPPORTED (rows above 2^30 or
  * cols above 2^24).
  */
 tweo_status tweo_layernorm_fwd(const void *x_bf16, const void *residual_bf16, const void *gamma_bf16,
@@ -244,8 +244,9 @@ tweo_status tweo_layernorm_fwd(const void *x_bf16, const void *residual_bf16, co
  *   after tweo_layernorm_quantize_e4m3 / _delayed.
  *   gamma_bf16 [cols]; dgamma fp32 [cols]; dbeta fp32 [cols] or NULL.
  *   workspace: tweo_workspace_bytes(TWEO_OP_LAYERNORM_BWD, rows, cols, 1); 256 bytes up to
- *   512 rows of up to 8192 columns, which leave nothing there.
- * Errors: TWEO_ERR_INVALID_ARG (null, misaligned), TWEO_ERR_UNSUPPORTED (as above),
+ *   512 rows of up to 8192 columns, which leave nothing there.  The LayerNorm -> cast
+ *   call's workspace can not be this one while its statistics are read here.
+ * Errors: TWEO_ERR_INVALID_ARG (null, misaligned, any other overlap), TWEO_ERR_UNSUPPORTED (as above),
  * TWEO_ERR_WORKSPACE.
  */
 tweo_status tweo_layernorm_bwd(const void *dy_bf16, const void *h_bf16, const void *gamma_bf16,

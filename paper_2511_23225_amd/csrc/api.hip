@@ -549,41 +549,8 @@ tweo_status tweo_layernorm_quantize_e4m3_delayed(const void *x_bf16, const void 
                                    stream);
 }
 
-tweo_status tweo_layernorm_fwd(const void *x_bf16, const void *residual_bf16, const void *gamma_bf16,
-                               const void *beta_bf16, int64_t rows, int64_t cols, float eps, void *h_out_bf16,
-                               void *y_bf16, double *stats_out, void *stream)
-{
-    if (!x_bf16 || !gamma_bf16 || !y_bf16 || rows <= 0 || cols <= 0 || !aligned16(x_bf16) || !aligned16(gamma_bf16) ||
-        !aligned16(y_bf16) || (beta_bf16 && !aligned16(beta_bf16)) || (stats_out && !aligned16(stats_out)) || !(eps >= 0.0f))
-        return TWEO_ERR_INVALID_ARG;
-    if (residual_bf16 && (!h_out_bf16 || !aligned16(residual_bf16) || !aligned16(h_out_bf16) || h_out_bf16 == y_bf16))
-        return TWEO_ERR_INVALID_ARG;
-    if (rows > kMaxDim || cols > kMaxCols)
-        return TWEO_ERR_UNSUPPORTED;
-    return hip_status(launch_layernorm_fwd(x_bf16, residual_bf16, gamma_bf16, beta_bf16, rows, cols, (double)eps, h_out_bf16,
-                                           y_bf16, stats_out, (hipStream_t)stream));
-}
-
-tweo_status tweo_layernorm_bwd(const void *dy_bf16, const void *h_bf16, const void *gamma_bf16, const double *stats,
-                               const void *residual_grad_bf16, int64_t rows, int64_t cols, void *dx_bf16, float *dgamma,
-                               float *dbeta, void *workspace, size_t workspace_bytes, void *stream)
-{
-    if (!dy_bf16 || !h_bf16 || !gamma_bf16 || !stats || !dx_bf16 || !dgamma || rows <= 0 || cols <= 0 || !aligned16(dy_bf16) ||
-        !aligned16(h_bf16) || !aligned16(gamma_bf16) || !aligned16(stats) || !aligned16(dx_bf16) || !aligned16(dgamma) ||
-        (residual_grad_bf16 && !aligned16(residual_grad_bf16)) || (dbeta && !aligned16(dbeta)))
-        return TWEO_ERR_INVALID_ARG;
-    if (rows > kMaxDim || cols > kMaxCols)
-        return TWEO_ERR_UNSUPPORTED;
-    if (!workspace || !aligned16(workspace) || workspace_bytes < std::max<size_t>(256, layernorm_bwd_bytes(rows, cols)))
-        return TWEO_ERR_WORKSPACE;
-    return hip_status(launch_layernorm_bwd(dy_bf16, h_bf16, gamma_bf16, stats, residual_grad_bf16, rows, cols, dx_bf16, dgamma,
-                                           dbeta, workspace, (hipStream_t)stream));
-}
-
 namespace {
-constexpr int kMaxOptimTensors = 1 << 16;
-
-// the buffers of a table: what a step writes overlaps nothing
+// a call's buffers: what it writes overlaps nothing
 struct Range {
     uintptr_t from, to;
     bool written;
@@ -602,6 +569,84 @@ bool ranges_clash(Range *r, size_t n)
     }
     return false;
 }
+
+// the buffers of a LayerNorm call
+struct Ranges {
+    Range r[9];
+    size_t n = 0;
+    void add(const void *p, size_t bytes, bool written)
+    {
+        if (p && bytes)
+            r[n++] = {(uintptr_t)p, (uintptr_t)p + bytes, written};
+    }
+    // one that may be `out` or `other`, in place: as what is written it is in the list already
+    void add_read(const void *p, size_t bytes, const void *out, const void *other)
+    {
+        if (p != out && p != other)
+            add(p, bytes, false);
+    }
+    bool clash() { return ranges_clash(r, n); }
+};
+}  // namespace
+
+tweo_status tweo_layernorm_fwd(const void *x_bf16, const void *residual_bf16, const void *gamma_bf16,
+                               const void *beta_bf16, int64_t rows, int64_t cols, float eps, void *h_out_bf16,
+                               void *y_bf16, double *stats_out, void *stream)
+{
+    if (!x_bf16 || !gamma_bf16 || !y_bf16 || rows <= 0 || cols <= 0 || !aligned16(x_bf16) || !aligned16(gamma_bf16) ||
+        !aligned16(y_bf16) || (beta_bf16 && !aligned16(beta_bf16)) || (stats_out && !aligned16(stats_out)) || !(eps >= 0.0f))
+        return TWEO_ERR_INVALID_ARG;
+    if (residual_bf16 && (!h_out_bf16 || !aligned16(residual_bf16) || !aligned16(h_out_bf16) || h_out_bf16 == y_bf16))
+        return TWEO_ERR_INVALID_ARG;
+    if (rows > kMaxDim || cols > kMaxCols)
+        return TWEO_ERR_UNSUPPORTED;
+    const size_t bytes = 2 * (size_t)rows * (size_t)cols;
+    const void *h_out = residual_bf16 ? h_out_bf16 : nullptr;
+    Ranges all;
+    all.add(y_bf16, bytes, true);
+    all.add(h_out, bytes, true);
+    all.add(stats_out, 16 * (size_t)rows, true);
+    all.add_read(x_bf16, bytes, y_bf16, h_out);
+    all.add_read(residual_bf16, bytes, y_bf16, h_out);
+    all.add(gamma_bf16, 2 * (size_t)cols, false);
+    all.add(beta_bf16, 2 * (size_t)cols, false);
+    if (all.clash())
+        return TWEO_ERR_INVALID_ARG;
+    return hip_status(launch_layernorm_fwd(x_bf16, residual_bf16, gamma_bf16, beta_bf16, rows, cols, (double)eps, h_out_bf16,
+                                           y_bf16, stats_out, (hipStream_t)stream));
+}
+
+tweo_status tweo_layernorm_bwd(const void *dy_bf16, const void *h_bf16, const void *gamma_bf16, const double *stats,
+                               const void *residual_grad_bf16, int64_t rows, int64_t cols, void *dx_bf16, float *dgamma,
+                               float *dbeta, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!dy_bf16 || !h_bf16 || !gamma_bf16 || !stats || !dx_bf16 || !dgamma || rows <= 0 || cols <= 0 || !aligned16(dy_bf16) ||
+        !aligned16(h_bf16) || !aligned16(gamma_bf16) || !aligned16(stats) || !aligned16(dx_bf16) || !aligned16(dgamma) ||
+        (residual_grad_bf16 && !aligned16(residual_grad_bf16)) || (dbeta && !aligned16(dbeta)))
+        return TWEO_ERR_INVALID_ARG;
+    if (rows > kMaxDim || cols > kMaxCols)
+        return TWEO_ERR_UNSUPPORTED;
+    const size_t need = layernorm_bwd_bytes(rows, cols), bytes = 2 * (size_t)rows * (size_t)cols;
+    if (!workspace || !aligned16(workspace) || workspace_bytes < std::max<size_t>(256, need))
+        return TWEO_ERR_WORKSPACE;
+    Ranges all;
+    all.add(dx_bf16, bytes, true);
+    all.add(dgamma, 4 * (size_t)cols, true);
+    all.add(dbeta, 4 * (size_t)cols, true);
+    all.add(workspace, need, true);
+    all.add_read(dy_bf16, bytes, dx_bf16, nullptr);
+    all.add_read(residual_grad_bf16, bytes, dx_bf16, nullptr);
+    all.add(h_bf16, bytes, false);
+    all.add(stats, 16 * (size_t)rows, false);
+    all.add(gamma_bf16, 2 * (size_t)cols, false);
+    if (all.clash())
+        return TWEO_ERR_INVALID_ARG;
+    return hip_status(launch_layernorm_bwd(dy_bf16, h_bf16, gamma_bf16, stats, residual_grad_bf16, rows, cols, dx_bf16, dgamma,
+                                           dbeta, workspace, (hipStream_t)stream));
+}
+
+namespace {
+constexpr int kMaxOptimTensors = 1 << 16;
 
 int optim_state_bits(const tweo_optim_tensor &t) { return !t.param ? 0 : t.m_step ? 8 : 32; }
 

@@ -28,3 +28,38 @@ def test_workspace_of_a_backward_pass_of_few_rows(lib):
         assert need(rows, cols) == 256, (rows, cols)
     # of more, a row of partial sums of both gradients a workgroup
     assert need(513, 8192) >= 256 * 2 * 8192 * 4 and need(512, 8200) >= 2 * 8200 * 4 and need(513, 64) >= 2 * 64 * 4
+
+
+def test_layernorm_buffers_that_overlap(lib, memory):
+    """What a call writes may be one of the tensors that the header names, exactly, and touches nothing else that the call reads or writes.
+    The statistics in the backward pass's own workspace among them: its partial sums would go over them while they are read."""
+    x, r, g, b, h, y, st, far = memory[:8]
+    size = 4 * 16 * 2
+    good = dict(x=x, r=r, g=g, b=b, rows=4, cols=16, h=h, y=y, st=st)
+
+    def fwd(**k):
+        a = {**good, **k}
+        return lib.tweo_layernorm_fwd(a["x"], a["r"], a["g"], a["b"], a["rows"], a["cols"], 1e-5, a["h"], a["y"], a["st"], None)
+
+    bad = [dict(y=x + 16), dict(y=x - size + 16), dict(y=r + 32), dict(h=x + 16), dict(h=r - 16), dict(h=y), dict(h=y + 16), dict(y=h - 16), dict(y=g), dict(y=b),
+           dict(h=g - size + 16), dict(st=x), dict(st=r + 16), dict(st=y + size - 16), dict(st=h), dict(st=g), dict(st=b + 16),
+           dict(h=x, y=x), dict(h=r, y=r), dict(r=x, h=x, y=x), dict(r=None, y=x + 16), dict(r=None, y=x, st=x), dict(r=None, y=g)]
+    for k in bad:
+        assert fwd(**k) == tw.TWEO_ERR_INVALID_ARG, k
+    good = dict(dy=x, h=h, g=g, st=st, dres=r, rows=600, cols=16, dx=y, dg=b, db=b + 64, ws=far, n=1 << 15)
+    size = 600 * 16 * 2
+
+    def bwd(**k):
+        a = {**good, **k}
+        return lib.tweo_layernorm_bwd(a["dy"], a["h"], a["g"], a["st"], a["dres"], a["rows"], a["cols"], a["dx"], a["dg"], a["db"], a["ws"], a["n"], None)
+
+    need = tw.tweo_workspace_bytes(tw.TWEO_OP_LAYERNORM_BWD, 600, 16, 1)
+    assert 256 < need < 1 << 15
+    bad = [dict(st=far), dict(st=far + 256), dict(st=far + 2304), dict(st=far - 600 * 16 + 16), dict(h=far), dict(dx=far), dict(dg=far), dict(g=far + 16),
+           dict(dx=h), dict(dx=h + 16), dict(dx=x + 16), dict(dx=r - 16), dict(dx=st), dict(dx=g), dict(dg=b + 16, db=b), dict(db=b), dict(dg=h + size - 16),
+           dict(db=st), dict(dg=g), dict(dg=y), dict(db=x), dict(dy=h, dx=h), dict(dres=h, dx=h)]
+    for k in bad:
+        assert bwd(**k) == tw.TWEO_ERR_INVALID_ARG, k
+    # few rows in one launch: other workgroups read h while dx is written
+    for k in (dict(dx=h), dict(dx=h + 16), dict(dx=st), dict(dg=b, db=b)):
+        assert bwd(rows=12, **k) == tw.TWEO_ERR_INVALID_ARG, k
