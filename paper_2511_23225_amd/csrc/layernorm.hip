@@ -655,7 +655,8 @@ __global__ __launch_bounds__(WAVES *kWave) void ln_bwd_kernel(LnBwdArgs a)
     }
 }
 
-// mean(w) and mean(w xhat) of wide rows, a workgroup a row
+// mean(w) and mean(w xhat) of wide rows, a workgroup a row: eight elements in fp32, then fp64 (a thread of rows of 2^20 columns adds
+// 2048 of them; equal ones in fp32 throughout were off by 2e-5, of 2^22 columns by 7e-5)
 template <bool RAGGED>
 __global__ __launch_bounds__(kWideThreads) void ln_bwd_sums_kernel(LnBwdArgs a)
 {
@@ -665,19 +666,22 @@ __global__ __launch_bounds__(kWideThreads) void ln_bwd_sums_kernel(LnBwdArgs a)
     __shared__ double red[2][T];
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const Normalizer normalized(a.stats[2 * r], a.stats[2 * r + 1]);
-        float c1 = 0.0f, c2 = 0.0f;
+        double c1 = 0.0, c2 = 0.0;
         for (int i = threadIdx.x; i < row.pieces; i += kWideThreads) {
             const Piece<8> h = row.load(a.h + r * a.cols, i, true), dy = row.load(a.dy + r * a.cols, i, true), g = row.load(a.gamma, i, true);
             const int count = row.count(i);
+            float t1 = 0.0f, t2 = 0.0f;
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 // (behind a ragged row's end as in ln_bwd_kernel)
                 const float xhat = !RAGGED || k < count ? normalized(h.at(k)) : 0.0f, w = dy.at(k) * g.at(k);
-                c2 += w;
-                c1 = __builtin_fmaf(w, xhat, c1);
+                t2 += w;
+                t1 = __builtin_fmaf(w, xhat, t1);
             }
+            c1 += (double)t1;
+            c2 += (double)t2;
         }
-        const double s2 = team_sum<T>((double)c2, red[0], wave), s1 = team_sum<T>((double)c1, red[1], wave);
+        const double s2 = team_sum<T>(c2, red[0], wave), s1 = team_sum<T>(c1, red[1], wave);
         if (threadIdx.x == 0) {
             a.sums[2 * r] = (float)(s2 / (double)a.cols);
             a.sums[2 * r + 1] = (float)(s1 / (double)a.cols);

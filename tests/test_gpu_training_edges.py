@@ -52,3 +52,25 @@ def test_backward_of_values_near_the_largest(cols):
     assert np.all(far <= 2.0 ** -8 * np.abs(want[0]) + 64 * 2.0 ** -24 * want[3] + 2.0 ** -134 + 8 * 2.0 ** -149)
     for g, ref, s in ((dgamma, want[1], want[4]), (dbeta, want[2], want[5])):
         assert np.all(np.abs(g.cpu().numpy().astype(np.float64) - ref) <= 25 * 2.0 ** -24 * s)
+
+
+@pytest.mark.parametrize("cols", [1 << 20, (1 << 20) + 3, 1 << 22])
+def test_row_sums_of_a_million_columns(cols):
+    """w xhat is the same number almost everywhere, so that every addition to a sum in fp32 rounds alike, and a few places where
+    w - xhat mean(w xhat) is 0 show what the mean has lost: 64 * 2^-24 of the terms' magnitudes is allowed."""
+    say("row sums", cols)
+    rows, w, ws, wide = 2, 0.30078125, 0.400390625, 2.0
+    sign = np.where(np.arange(cols) % 2, -1.0, 1.0).astype(np.float32)
+    h, dy = np.tile(sign, (rows, 1)), np.tile(np.float32(w) * sign, (rows, 1))
+    places = np.linspace(5, cols - 1, 7).astype(np.int64)
+    h[:, places], dy[:, places] = wide, ws
+    t = dict(dy=synth.f32_to_bf16_bits(dy), gamma=np.full(cols, 0x3F80, np.uint16), dres=None)
+    hb = synth.f32_to_bf16_bits(h)
+    stats = np.tile(np.float64([0.0, np.sqrt(ws / (wide * w))]), (rows, 1))
+    dx, dgamma, dbeta = backward(t, to_dev_bf16(hb), torch.from_numpy(stats).to(DEV), residual=False)
+    ref = training.layernorm_bwd(f64(t["dy"]), f64(hb), f64(t["gamma"]), stats)
+    far = np.abs(f64(bf16_bits(dx)) - ref[0])
+    bound = 2.0 ** -8 * np.abs(ref[0]) + 64 * 2.0 ** -24 * ref[3]
+    say("worst of the bound", (far / bound).max())
+    assert np.all(far <= bound)
+    assert np.all(np.abs(dgamma.cpu().numpy() - ref[1]) <= 24 * 2.0 ** -24 * ref[4]) and np.all(np.abs(dbeta.cpu().numpy() - ref[2]) <= 24 * 2.0 ** -24 * ref[5])
