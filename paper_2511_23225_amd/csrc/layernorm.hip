@@ -536,6 +536,22 @@ __global__ __launch_bounds__(WAVES *kWave) void ln_bwd_kernel(LnBwdArgs a)
             dgamma[u][k] = dbeta[u][k] = 0.0f;
         }
     }
+    // Slabs of wide rows leave few workgroups to a column: the sums of 64 rows are added to others, so that 4096 rows are two sums of
+    // 64 terms one after the other.
+    constexpr int kHeld = 64;
+    float held[2][SLAB ? P : 1][V] = {};
+    int rows_held = 0;
+    auto hold = [&] {
+#pragma unroll
+        for (int u = 0; u < (SLAB ? P : 1); ++u)
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                held[0][u][k] += dgamma[u][k];
+                held[1][u][k] += dbeta[u][k];
+                dgamma[u][k] = dbeta[u][k] = 0.0f;
+            }
+        rows_held = 0;
+    };
     for (int64_t r0 = (int64_t)blockIdx.x * TEAMS; r0 < a.rows; r0 += stride_rows, turn ^= 1) {
         const bool mine = r0 + team < a.rows;
         const int64_t r = mine ? r0 + team : a.rows - 1, at = r * a.cols;
@@ -619,9 +635,19 @@ __global__ __launch_bounds__(WAVES *kWave) void ln_bwd_kernel(LnBwdArgs a)
             }
             row.store(a.dx + at, first + lane + u * kLanes<T>, out);
         }
+        if (SLAB && ++rows_held == kHeld)
+            hold();
     }
     if constexpr (ALONE)
         return;
+    if constexpr (SLAB) {
+        hold();
+#pragma unroll
+        for (int u = 0; u < P; ++u)
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                dgamma[u][k] = held[0][u][k], dbeta[u][k] = held[1][u][k];
+    }
     // the teams' column sums through LDS, then added in the teams' order, four columns a thread
     __shared__ float sums[TEAMS][P * V][kLanes<T>];
     const int stride = (a.cols + 3) & ~3;

@@ -74,3 +74,23 @@ def test_row_sums_of_a_million_columns(cols):
     say("worst of the bound", (far / bound).max())
     assert np.all(far <= bound)
     assert np.all(np.abs(dgamma.cpu().numpy() - ref[1]) <= 24 * 2.0 ** -24 * ref[4]) and np.all(np.abs(dbeta.cpu().numpy() - ref[2]) <= 24 * 2.0 ** -24 * ref[5])
+
+
+@pytest.mark.parametrize("rows,cols", [(1 << 19, 8200), (8192, 1 << 20)])
+def test_column_sums_of_long_wide_tensors(rows, cols):
+    """4096 rows to a workgroup, the same term in each, so that all additions to a sum in fp32 round alike.  Sums of 64 rows, then
+    sums of those: (64 + 4096 / 64 + 24) * 2^-24 of the terms' magnitudes, as in the shorter calls' bound."""
+    say("column sums", rows, cols)
+    w, rstd = 0.30078125, 0.9173
+    dy = torch.full((rows, cols), w, dtype=torch.bfloat16, device=DEV)
+    h = torch.ones((rows, cols), dtype=torch.bfloat16, device=DEV)
+    h[:, 1::2] = -1
+    stats = torch.tensor([0.0, rstd], dtype=torch.float64, device=DEV).repeat(rows, 1)
+    gamma = torch.ones(cols, dtype=torch.bfloat16, device=DEV)
+    dgamma, dbeta = torch.empty(cols, device=DEV), torch.empty(cols, device=DEV)
+    tw.tweo_layernorm_bwd(dy, h, gamma, stats, dy, dgamma, dbeta=dbeta, workspace=workspace(tw.TWEO_OP_LAYERNORM_BWD, rows, cols, 1))
+    sign = np.where(np.arange(cols) % 2, -1.0, 1.0)
+    for name, got, want in (("dgamma", dgamma, rows * w * rstd * sign), ("dbeta", dbeta, np.full(cols, rows * w))):
+        far = np.abs(got.cpu().numpy().astype(np.float64) / want - 1).max()
+        say(name, far * 2.0 ** 24)
+        assert far <= (64 + 4096 // 64 + 24) * 2.0 ** -24, name
