@@ -638,6 +638,8 @@ typedef struct {
  *   p = p - lr * weight_decay * p - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
  * in fp32.  If *grad_sumsq is not finite nothing is changed (one bad gradient must not reach every
  * parameter through the clip): the caller sees it there, and decides whether t counts the step.
+ * A finite g beyond 2^63 (9.2e18) counts as 2^63 with its sign, in both moments: its square is
+ * beyond fp32, and an infinite v would stop its parameter, or in 8 bits its block, for good.
  * 8-bit states: p takes the moments before they are rounded to codes.  Of a block of 256 elements
  *   scale = 448 / max|m| (E4M3) or 57344 / max v (E5M2), guards as tweo_quantize_e4m3;  step = 1 / scale
  *   code  = the magnitude's code at or below |m| * scale, or the next one if what is cut off, as

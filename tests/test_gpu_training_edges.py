@@ -9,6 +9,7 @@ from oracle import training
 from paper_2511_23225_amd import synth
 from gpu_util import DEV, bf16_bits, to_dev_bf16, workspace
 from test_gpu_layernorm_grad import EPS, backward, check_backward, f64, forward, inputs, say
+from test_gpu_optim import HYPER, KINDS, Tensor, check, moments, plan_of
 
 pytestmark = pytest.mark.gpu
 
@@ -94,3 +95,36 @@ def test_column_sums_of_long_wide_tensors(rows, cols):
         far = np.abs(got.cpu().numpy().astype(np.float64) / want - 1).max()
         say(name, far * 2.0 ** 24)
         assert far <= (64 + 4096 // 64 + 24) * 2.0 ** -24, name
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("kind", KINDS)
+def test_finite_gradients_whose_square_is_beyond_fp32(bits, kind):
+    """They count as 2^63 or -2^63, in both moments, so that the step is of lr's size as for any other gradient and the next ones find finite
+    moments; infinities and NaN stay what they are."""
+    n = 3000
+    t = Tensor(np.random.default_rng(41), n, kind, bits, fresh=True)
+    big = {100: 1e20, 101: -3e38, 777: 2.0 ** 63, 1500: -1e25, 2050: 9e18, 2999: 3.3e38}
+    for i, g in big.items():
+        t.grad[i] = g
+    plan = plan_of([t])
+    at = torch.tensor(sorted(big))
+    held = lambda s: dict(s, grad=s["grad"].clamp(-2.0 ** 63, 2.0 ** 63))  # noqa: E731
+    for step in (1, 2, 3):
+        before = t.state()
+        tw.tweo_adamw_step(plan, step=step, **HYPER)
+        after = t.state()
+        assert torch.equal(before["grad"], after["grad"])
+        check(held(before), held(after), step, bits, t.weight_decay, HYPER, 1.0, (kind, step))
+        m, v = moments(after, bits)
+        assert np.isfinite(m).all() and np.isfinite(v).all() and bool((after["param"].float()[at].abs() < 1).all())
+    t.grad[5], t.grad[600], t.grad[1999] = float("inf"), float("-inf"), float("nan")
+    tw.tweo_adamw_step(plan, step=4, **HYPER)
+    after = t.state()
+    bad = torch.zeros(n, dtype=torch.bool)
+    bad[[5, 600, 1999]] = True
+    assert torch.equal(torch.isnan(after["param"]), bad)
+    if bits == 32:
+        assert torch.equal(~torch.isfinite(after["m"]), bad) and torch.equal(~torch.isfinite(after["v"]), bad)
+    else:
+        assert torch.isnan(after["m_step"]).nonzero().flatten().tolist() == torch.isnan(after["v_step"]).nonzero().flatten().tolist() == [0, 2, 7]
