@@ -626,7 +626,7 @@ typedef struct {
     double lr;       /* >= 0 */
     double beta1;    /* 0 <= beta < 1 */
     double beta2;
-    double eps;      /* >= 0 */
+    double eps;      /* 0, or at least 2^-126: below it fp32 has no reciprocal */
     double max_norm; /* > 0; used with grad_sumsq */
     int64_t step;    /* t of this step, 1 .. 2^32 - 1 */
 } tweo_adamw_cfg;

@@ -733,6 +733,7 @@ tweo_status tweo_adamw_step(const tweo_optim_plan *plan, const tweo_adamw_cfg *c
     auto beta_ok = [](double b) { return b >= 0.0 && b < 1.0; };
     auto positive = [](double v, double least) { return v >= least && v <= 3.4028234663852886e+38; };
     if (!beta_ok(cfg->beta1) || !beta_ok(cfg->beta2) || !positive(cfg->eps, 0.0) || (grad_sumsq && !(cfg->max_norm > 0.0)) ||
+        (cfg->eps > 0.0 && (float)cfg->eps < 0x1p-126f) ||
         (!schedule && (!positive(cfg->lr, 0.0) || cfg->step < 1 || cfg->step > 0xFFFFFFFFll)))
         return TWEO_ERR_INVALID_ARG;
     const AdamwCall call{cfg->lr, cfg->beta1, cfg->beta2, cfg->eps, cfg->max_norm, schedule ? 1u : (uint32_t)cfg->step, grad_sumsq,

@@ -128,3 +128,14 @@ def test_finite_gradients_whose_square_is_beyond_fp32(bits, kind):
         assert torch.equal(~torch.isfinite(after["m"]), bad) and torch.equal(~torch.isfinite(after["v"]), bad)
     else:
         assert torch.isnan(after["m_step"]).nonzero().flatten().tolist() == torch.isnan(after["v_step"]).nonzero().flatten().tolist() == [0, 2, 7]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_the_least_eps_keeps_what_has_no_gradient(bits):
+    t = Tensor(np.random.default_rng(43), 700, ("fp32", False, "fp32"), bits, fresh=True)
+    t.grad[:300] = 0
+    before = t.state()
+    tw.tweo_adamw_step(plan_of([t]), step=1, **dict(HYPER, eps=2.0 ** -126))
+    after = t.state()
+    assert torch.equal(after["param"][:300], before["param"][:300]) and bool(torch.isfinite(after["param"]).all())
+    check(before, after, 1, bits, t.weight_decay, dict(HYPER, eps=2.0 ** -126), 1.0, bits)

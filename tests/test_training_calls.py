@@ -63,3 +63,11 @@ def test_layernorm_buffers_that_overlap(lib, memory):
     # few rows in one launch: other workgroups read h while dx is written
     for k in (dict(dx=h), dict(dx=h + 16), dict(dx=st), dict(dg=b, db=b)):
         assert bwd(rows=12, **k) == tw.TWEO_ERR_INVALID_ARG, k
+
+
+def test_an_eps_without_a_reciprocal(lib, memory):
+    """Below 2^-126 1 / eps is beyond fp32 (or eps is 0 there), and 0 times it would make NaN of a parameter whose gradients have been zero."""
+    plan = tw.binding.OptimPlan(memory[0], 4, 1, 32)
+    for eps in (1e-40, 1e-60, 5e-324, 2.0 ** -127, 2.0 ** -126 * (1 - 2.0 ** -23)):
+        cfg = tw.binding.AdamwCfg(1e-3, 0.9, 0.999, eps, 1.0, 1)
+        assert lib.tweo_adamw_step(ctypes.byref(plan), ctypes.byref(cfg), None, None, None) == tw.TWEO_ERR_INVALID_ARG, eps
