@@ -480,7 +480,7 @@ def _same(device, shape, dtype, tensors, names):
 @functools.lru_cache(maxsize=1)
 def _types():
     import torch
-    return torch.bfloat16, torch.float32, torch.float64
+    return torch.bfloat16, torch.float32, torch.float64, torch.int32, torch.uint32
 
 
 _LN_FWD, _LN_FWD_PARAMS, _LN_STATS = ("x_bf16", "y_bf16", "residual_bf16", "h_out_bf16"), ("gamma_bf16", "beta_bf16"), ("stats",)
@@ -493,7 +493,7 @@ def tweo_layernorm_fwd(x_bf16, gamma_bf16, y_bf16, beta_bf16=None, residual_bf16
     if len(shape) != 2:
         raise ValueError("x_bf16: two dimensions are needed")
     rows, cols = shape
-    dev, (bf16, _, f64) = _device(), _types()
+    dev, (bf16, _, f64) = _device(), _types()[:3]
     if residual_bf16 is None:
         _same(dev, shape, bf16, (x_bf16, y_bf16), _LN_FWD)
     else:
@@ -518,7 +518,7 @@ def tweo_layernorm_bwd(dy_bf16, h_bf16, gamma_bf16, stats, dx_bf16, dgamma, dbet
     if len(shape) != 2:
         raise ValueError("dy_bf16: two dimensions are needed")
     rows, cols = shape
-    dev, (bf16, f32, f64) = _device(), _types()
+    dev, (bf16, f32, f64) = _device(), _types()[:3]
     _same(dev, shape, bf16, (dy_bf16, h_bf16, dx_bf16, residual_grad_bf16), _LN_BWD)
     _same(dev, shape[1:], bf16, (gamma_bf16,), _LN_FWD_PARAMS)
     _same(dev, shape[1:], f32, (dgamma, dbeta), _LN_BWD_SUMS)
@@ -586,8 +586,11 @@ def tweo_grad_sumsq(plan, sumsq_out, workspace):
 
 
 def tweo_adamw_step(plan, lr=None, step=None, beta1=0.9, beta2=0.999, eps=1e-8, grad_sumsq=None, max_norm=1.0, schedule=None):
-    """lr and step, or schedule: two 32-bit words on the device, lr as fp32 and step as an integer."""
+    """lr and step, or schedule: a torch.int32 (or uint32) tensor of two words on the device, the bits of lr as fp32 and step
+    (schedule[:1].view(torch.float32).fill_(lr); schedule[1:].fill_(step))."""
     _on_device(plan, grad_sumsq, schedule)
+    if schedule is not None and (schedule.dtype not in _types()[3:] or not schedule.is_contiguous()):
+        raise ValueError("schedule: contiguous 32-bit integers are needed, got %s of strides %s" % (schedule.dtype, schedule.stride()))
     if schedule is None:
         if lr is None or step is None:
             raise ValueError("lr and step are needed without a schedule")

@@ -3,6 +3,7 @@ before anything is launched."""
 import ctypes
 
 import pytest
+import torch
 
 import paper_2511_23225_amd as tw
 
@@ -71,3 +72,47 @@ def test_an_eps_without_a_reciprocal(lib, memory):
     for eps in (1e-40, 1e-60, 5e-324, 2.0 ** -127, 2.0 ** -126 * (1 - 2.0 ** -23)):
         cfg = tw.binding.AdamwCfg(1e-3, 0.9, 0.999, eps, 1.0, 1)
         assert lib.tweo_adamw_step(ctypes.byref(plan), ctypes.byref(cfg), None, None, None) == tw.TWEO_ERR_INVALID_ARG, eps
+
+
+class Elsewhere:
+    """A tensor that says it is on the device it is asked for, for checks that come before any launch."""
+
+    def __init__(self, t, device=0):
+        self.t, self.device = t, device
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+    def get_device(self):
+        return self.device
+
+
+@pytest.fixture
+def on_device(monkeypatch):
+    """A current device without a GPU, and entry points that note that they were reached."""
+    reached = []
+
+    class Reached:
+        def __getattr__(self, name):
+            return lambda *a: reached.append(name) or tw.TWEO_OK
+
+    monkeypatch.setattr(tw.binding, "_current", (lambda: 0, lambda device: None))
+    monkeypatch.setattr(tw.binding, "_lib", Reached())
+    plan = tw.binding.OptimPlan()
+    plan.device = 0
+    return plan, reached
+
+
+def test_a_schedule_is_two_integer_words(on_device):
+    plan, reached = on_device
+    words = torch.zeros(8, dtype=torch.int32)
+    for bad in (torch.tensor([1e-3, 1000.0]), torch.zeros(2, dtype=torch.int64), torch.zeros(4, dtype=torch.int16), torch.zeros(2, dtype=torch.float64),
+                words[::2], words[:1], torch.zeros(1, dtype=torch.int32).expand(2)):
+        with pytest.raises(ValueError):
+            tw.tweo_adamw_step(plan, schedule=Elsewhere(bad))
+    with pytest.raises(ValueError):
+        tw.tweo_adamw_step(plan, schedule=Elsewhere(words[:2], -1))
+    assert not reached
+    tw.tweo_adamw_step(plan, schedule=Elsewhere(words[:2]))
+    tw.tweo_adamw_step(plan, schedule=Elsewhere(words[4:].view(torch.uint32)))
+    assert reached == ["tweo_adamw_step"] * 2
