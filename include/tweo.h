@@ -205,6 +205,9 @@ tweo_status tweo_layernorm_quantize_e4m3_delayed(const void *x_bf16, const void 
                                                  uint8_t *q, uint8_t *qT, void *workspace,
                                                  size_t workspace_bytes, void *stream);
 
+/* Where the LayerNorm -> cast calls leave the rows' statistics in their workspace, fp64 [rows][2]. */
+#define TWEO_LAYERNORM_STATS_OFFSET 2304
+
 /*
  * LayerNorm to bf16 without a cast: in front of what is not an FP8 linear (a bf16
  * head, attention), and for one token as for many.

@@ -506,10 +506,18 @@ def tweo_layernorm_fwd(x_bf16, gamma_bf16, y_bf16, beta_bf16=None, residual_bf16
            "tweo_layernorm_fwd")
 
 
+LAYERNORM_STATS_OFFSET = 2304  # TWEO_LAYERNORM_STATS_OFFSET
+
+
 def layernorm_stats(workspace, rows):
-    """The row statistics (mean, 1 / sqrt(var + eps)), fp64 [rows, 2], that a LayerNorm -> cast call left in its workspace."""
+    """The row statistics (mean, 1 / sqrt(var + eps)), fp64 [rows, 2], that a LayerNorm -> cast call left in its workspace, a contiguous
+    tensor of any type."""
     import torch
-    return workspace[2304:2304 + 16 * rows].view(torch.float64).view(rows, 2)
+    end = LAYERNORM_STATS_OFFSET + 16 * rows
+    if rows < 1 or not workspace.is_contiguous() or workspace.nbytes < end:
+        raise ValueError("the workspace of a LayerNorm -> cast of %d rows has at least %d contiguous bytes, got %d of strides %s" %
+                         (rows, end, workspace.nbytes, workspace.stride()))
+    return workspace.view(-1).view(torch.uint8)[LAYERNORM_STATS_OFFSET:end].view(torch.float64).view(rows, 2)
 
 
 def tweo_layernorm_bwd(dy_bf16, h_bf16, gamma_bf16, stats, dx_bf16, dgamma, dbeta=None, residual_grad_bf16=None,

@@ -496,6 +496,7 @@ namespace {
 // workspace of the LayerNorm entry points: the amax launch's workgroup maxima, one spare fp32 slot
 // for the amax when the caller wants none, then two doubles per row
 constexpr size_t kLnHeadBytes = kAmaxPartialsMax * sizeof(uint32_t) + 256;
+static_assert(kLnHeadBytes == TWEO_LAYERNORM_STATS_OFFSET, "what callers are told");
 inline size_t layernorm_bytes(int64_t rows) { return kLnHeadBytes + round256((size_t)rows * 2 * sizeof(double)); }
 
 tweo_status layernorm_quantize_impl(const void *x_bf16, const void *residual_bf16, const void *gamma_bf16,

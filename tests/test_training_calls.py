@@ -1,6 +1,8 @@
 """Without a GPU: calls of the norm and optimizer entry points that would read or write the wrong memory, or count it wrongly, are refused
 before anything is launched."""
 import ctypes
+import os
+import re
 
 import pytest
 import torch
@@ -116,3 +118,21 @@ def test_a_schedule_is_two_integer_words(on_device):
     tw.tweo_adamw_step(plan, schedule=Elsewhere(words[:2]))
     tw.tweo_adamw_step(plan, schedule=Elsewhere(words[4:].view(torch.uint32)))
     assert reached == ["tweo_adamw_step"] * 2
+
+
+def test_statistics_in_a_workspace_of_any_type():
+    """The offset is in bytes, whatever the workspace's type; what is too short, or does not lie in one piece, is refused."""
+    header = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "tweo.h")).read()
+    assert int(re.search(r"#define TWEO_LAYERNORM_STATS_OFFSET (\d+)", header).group(1)) == tw.binding.LAYERNORM_STATS_OFFSET
+    rows, offset = 48, tw.binding.LAYERNORM_STATS_OFFSET
+    need = tw.tweo_workspace_bytes(tw.TWEO_OP_LAYERNORM_QUANTIZE, rows, 1, 1)
+    whole = torch.zeros(need + 64, dtype=torch.uint8)
+    want = torch.arange(2 * rows, dtype=torch.float64)
+    whole[offset:offset + 16 * rows] = want.view(torch.uint8)
+    for kind in (torch.uint8, torch.int8, torch.int32, torch.float32, torch.float64, torch.bfloat16):
+        got = tw.layernorm_stats(whole[:need].view(kind), rows)
+        assert torch.equal(got, want.view(rows, 2)) and got.data_ptr() == whole.data_ptr() + offset, kind
+    assert torch.equal(tw.layernorm_stats(whole[:need].view(4, -1), rows), want.view(rows, 2))
+    for bad, count in ((whole[:need:2], rows), (whole[:offset + 16 * rows - 1], rows), (whole[:offset], 1), (whole, 0), (whole, -1), (whole[:need], 1 << 20)):
+        with pytest.raises(ValueError):
+            tw.layernorm_stats(bad, count)
