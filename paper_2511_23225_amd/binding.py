@@ -483,6 +483,13 @@ def _types():
     return torch.bfloat16, torch.float32, torch.float64, torch.int32, torch.uint32
 
 
+def _scratch(device, t, name):
+    """Address and bytes of a workspace or table, which has to lie in one piece on the current device."""
+    if t is not None and (t.get_device() != device or not t.is_contiguous()):
+        raise ValueError("%s: a contiguous tensor on cuda:%d, the current device, is needed, got strides %s on %s" % (name, device, t.stride(), t.device))
+    return _ws(t)
+
+
 _LN_FWD, _LN_FWD_PARAMS, _LN_STATS = ("x_bf16", "y_bf16", "residual_bf16", "h_out_bf16"), ("gamma_bf16", "beta_bf16"), ("stats",)
 _LN_BWD, _LN_BWD_SUMS = ("dy_bf16", "h_bf16", "dx_bf16", "residual_grad_bf16"), ("dgamma", "dbeta")
 
@@ -531,9 +538,7 @@ def tweo_layernorm_bwd(dy_bf16, h_bf16, gamma_bf16, stats, dx_bf16, dgamma, dbet
     _same(dev, shape[1:], bf16, (gamma_bf16,), _LN_FWD_PARAMS)
     _same(dev, shape[1:], f32, (dgamma, dbeta), _LN_BWD_SUMS)
     _same(dev, (rows, 2), f64, (stats,), _LN_STATS)
-    if workspace is not None and workspace.get_device() != dev:
-        raise ValueError("workspace on %s, but cuda:%d is current" % (workspace.device, dev))
-    wp, wb = _ws(workspace)
+    wp, wb = _scratch(dev, workspace, "workspace")
     _check(load().tweo_layernorm_bwd(_ptr(dy_bf16), _ptr(h_bf16), _ptr(gamma_bf16), _ptr(stats), _ptr(residual_grad_bf16),
                                      rows, cols, _ptr(dx_bf16), _ptr(dgamma), _ptr(dbeta), wp, wb, _stream()),
            "tweo_layernorm_bwd")
@@ -570,35 +575,34 @@ def make_optim_plan(rows, table):
         if t.get_device() != dev:
             raise ValueError("a tensor on %s, but cuda:%d is current" % (t.device, dev))
     plan = OptimPlan()
-    wp, wb = _ws(table)
+    wp, wb = _scratch(dev, table, "table")
     _check(load().tweo_optim_plan_init((OptimTensor * len(rows))(*rows), len(rows), wp, wb, ctypes.byref(plan), _stream()),
            "tweo_optim_plan_init")
     plan.device, plan.tensors = dev, [table] + [t for r in rows for t in r.tensors]
     return plan
 
 
-def _on_device(plan, sumsq, other):
+def _on_device(plan, sumsq):
     dev = _device()
     if dev != plan.device:
         raise ValueError("a plan of cuda:%d, but cuda:%d is current" % (plan.device, dev))
     if sumsq is not None and (sumsq.dtype is not _types()[2] or sumsq.numel() < 1 or sumsq.get_device() != dev):
         raise ValueError("the sum of squares: one torch.float64 on cuda:%d is needed, got %s on %s" % (dev, sumsq.dtype, sumsq.device))
-    if other is not None and (other.get_device() != dev or other.nbytes < 8):
-        raise ValueError("at least 8 bytes on cuda:%d are needed, got %d on %s" % (dev, other.nbytes, other.device))
+    return dev
 
 
 def tweo_grad_sumsq(plan, sumsq_out, workspace):
-    _on_device(plan, sumsq_out, workspace)
-    wp, wb = _ws(workspace)
+    wp, wb = _scratch(_on_device(plan, sumsq_out), workspace, "workspace")
     _check(load().tweo_grad_sumsq(ctypes.byref(plan), _ptr(sumsq_out), wp, wb, _stream()), "tweo_grad_sumsq")
 
 
 def tweo_adamw_step(plan, lr=None, step=None, beta1=0.9, beta2=0.999, eps=1e-8, grad_sumsq=None, max_norm=1.0, schedule=None):
     """lr and step, or schedule: a torch.int32 (or uint32) tensor of two words on the device, the bits of lr as fp32 and step
     (schedule[:1].view(torch.float32).fill_(lr); schedule[1:].fill_(step))."""
-    _on_device(plan, grad_sumsq, schedule)
-    if schedule is not None and (schedule.dtype not in _types()[3:] or not schedule.is_contiguous()):
-        raise ValueError("schedule: contiguous 32-bit integers are needed, got %s of strides %s" % (schedule.dtype, schedule.stride()))
+    dev = _on_device(plan, grad_sumsq)
+    if schedule is not None and (schedule.dtype not in _types()[3:] or schedule.numel() < 2 or not schedule.is_contiguous() or schedule.get_device() != dev):
+        raise ValueError("schedule: two contiguous 32-bit integers on cuda:%d are needed, got %d of %s, strides %s, on %s" %
+                         (dev, schedule.numel(), schedule.dtype, schedule.stride(), schedule.device))
     if schedule is None:
         if lr is None or step is None:
             raise ValueError("lr and step are needed without a schedule")

@@ -136,3 +136,23 @@ def test_statistics_in_a_workspace_of_any_type():
     for bad, count in ((whole[:need:2], rows), (whole[:offset + 16 * rows - 1], rows), (whole[:offset], 1), (whole, 0), (whole, -1), (whole[:need], 1 << 20)):
         with pytest.raises(ValueError):
             tw.layernorm_stats(bad, count)
+
+
+def test_scratch_memory_lies_in_one_piece(on_device):
+    """The library takes an address and a number of bytes: of a tensor with strides they would name memory that is not its own."""
+    plan, reached = on_device
+    n = 1 << 16
+    for bad in (Elsewhere(torch.zeros(2 * n, dtype=torch.uint8)[::2]), Elsewhere(torch.zeros(1, dtype=torch.uint8).expand(n)),
+                Elsewhere(torch.zeros((64, n // 32), dtype=torch.uint8)[:, :n // 64]), Elsewhere(torch.zeros(n, dtype=torch.uint8), 1)):
+        with pytest.raises(ValueError):
+            tw.tweo_grad_sumsq(plan, Elsewhere(torch.zeros(1, dtype=torch.float64)), bad)
+        with pytest.raises(ValueError):
+            tw.make_optim_plan([], bad)
+        x, row = Elsewhere(torch.zeros((4, 16), dtype=torch.bfloat16)), Elsewhere(torch.zeros(16, dtype=torch.bfloat16))
+        with pytest.raises(ValueError):
+            tw.tweo_layernorm_bwd(x, x, row, Elsewhere(torch.zeros((4, 2), dtype=torch.float64)), x, Elsewhere(torch.zeros(16)), workspace=bad)
+    assert not reached
+    good = Elsewhere(torch.zeros(n, dtype=torch.uint8))
+    tw.tweo_grad_sumsq(plan, Elsewhere(torch.zeros(1, dtype=torch.float64)), good)
+    tw.make_optim_plan([], good)
+    assert reached == ["tweo_grad_sumsq", "tweo_optim_plan_init"]
