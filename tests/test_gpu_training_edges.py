@@ -139,3 +139,24 @@ def test_the_least_eps_keeps_what_has_no_gradient(bits):
     after = t.state()
     assert torch.equal(after["param"][:300], before["param"][:300]) and bool(torch.isfinite(after["param"]).all())
     check(before, after, 1, bits, t.weight_decay, dict(HYPER, eps=2.0 ** -126), 1.0, bits)
+
+
+@pytest.mark.parametrize("beta2,spread", [(0.95, 0.23), (0.999, 0.30)])
+def test_second_moments_in_8_bits_at_other_rates(beta2, spread):
+    """300 steps, the gradients' variance falling a hundredfold at half of them.  The oracle's codes over 25600 other elements end 1.3 to
+    1.7 % low with spreads of 0.18 and 0.25; `spread` is what independent random thresholds, which are unbiased, leave.  Standard errors
+    over 40000 elements are 0.1 %."""
+    n, rng = 40000, np.random.default_rng(44)
+    eight, exact = (Tensor(rng, n, ("fp32", False, "fp32"), bits, fresh=True) for bits in (8, 32))
+    plans = plan_of([eight]), plan_of([exact])
+    sigma = torch.rand(n, device=DEV, generator=torch.Generator(DEV).manual_seed(3)) + 0.5
+    gen = torch.Generator(DEV).manual_seed(4)
+    for t in range(1, 301):
+        g = torch.randn(n, device=DEV, generator=gen) * sigma * (1.0 if t < 150 else 0.1)
+        for x, p in zip((eight, exact), plans):
+            x.grad.copy_(g)
+            tw.tweo_adamw_step(p, step=t, **dict(HYPER, beta2=beta2))
+        if t in (149, 300):
+            ratio = moments(eight.state(), 8)[1].astype(np.float64) / exact.state()["v"].double().numpy()
+            say("beta2", beta2, "t", t, "mean", ratio.mean(), "spread", ratio.std())
+            assert abs(ratio.mean() - 1) <= 0.02 and ratio.std() < spread
