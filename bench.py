@@ -251,7 +251,8 @@ def time_layernorm(tw, torch, dev, rows=16384, cols=2048, copies=6, iters=24):
 def time_training_rest(tw, torch, layers, dev, iters=12):
     """What a training step runs around the block's linears, on the gradients that the timed steps have left: the norm in bf16 over the
     residual stream and its gradients (cold: four streams in turn), the norm of all weight gradients, and the clipped AdamW step on
-    all weights with fp32 masters, moments in fp32 and in 8 bits.  Each with the bytes that it can not do without."""
+    all weights with fp32 masters, moments in fp32 and in 8 bits.  Each with the bytes that it can not do without.  The norm of the
+    gradients and the step run on the same tensors again and again: what the memory-side cache keeps of them is in their rates."""
     g = torch.Generator(device=dev)
     g.manual_seed(11)
     rows, cols, sets = layers[0].M, layers[0].K, 4

@@ -245,6 +245,7 @@ tweo_status tweo_layernorm_fwd(const void *x_bf16, const void *residual_bf16, co
  *   or residual_grad (exactly, in place), else nothing overlaps.
  *   stats: fp64 [rows][2] from tweo_layernorm_fwd, or bytes 2304 and on of the workspace
  *   after tweo_layernorm_quantize_e4m3 / _delayed.
+ *   rstd is taken in fp32: without an eps, rows whose deviation is below 3e-39 have none.
  *   gamma_bf16 [cols]; dgamma fp32 [cols]; dbeta fp32 [cols] or NULL.
  *   workspace: tweo_workspace_bytes(TWEO_OP_LAYERNORM_BWD, rows, cols, 1); 256 bytes up to
  *   512 rows of up to 8192 columns, which leave nothing there.  The LayerNorm -> cast

@@ -1,4 +1,5 @@
 // LayerNorm to bf16, forward and backward.  Rows of any length; gfx950 only.
+// Times in the comments: a call among others in a replayed graph, on three sets of inputs in turn, where no kernel is named alone.
 #include <algorithm>
 #include <type_traits>
 #include "kernels.h"
@@ -13,7 +14,7 @@ namespace {
 // that has four or eight rows at once (524288x64 forward 140 us with a wave a row, 33; backward 130, 46); lane l of the team
 // holds the pieces l, l + 64 T, ... of it, P of them, V elements (4 or 8: 8 or 16 bytes) each, in registers.  RAGGED: cols is no
 // multiple of V, so that rows start at any even address and their last piece is short; what they cost is accesses that straddle
-// lines (16384x2041 forward 63 us, 2048 wide 49; backward 66 and 51).  ONCE: past the caches.
+// lines (16384x2041 forward 60 us, 2048 wide 45; backward 67 and 51; 4096x4093 37 and 45, 3.0 TB/s).  ONCE: past the caches.
 
 // T = 0 and -1: 16 and 8 lanes
 template <int T>
@@ -220,11 +221,12 @@ __device__ __forceinline__ double divided(double s, double n, double inv_n)
 // ---------------------------------------------------------------------------
 // Forward: y = (h - mu) / sqrt(var + eps) * gamma + beta, h = x or bf16(x + residual).  One read of a row (2 B an element, 4 with
 // a residual), one write (2, 4): mean and squared differences are taken of the registers, in fp64 as in the pass in front of the
-// FP8 cast, whose stored activation this one's equals bit for bit (fp32 in its place: no faster where memory bounds it, 54.4 us
-// and 54.1 at 16384x2048; 19.2 and 15.8 at 16384x1024, which the caches hold).  The next row is under way while one is worked on.
+// FP8 cast, whose stored activation has these bits (but where sums in another order and another root, 1e-16 of the value, lie on two
+// sides of a rounding boundary).  fp32 in its place: no faster where memory bounds it, 54.4 us and 54.1 at 16384x2048; 19.2 and
+// 15.8 at 16384x1024, which the caches hold.  The next row is under way while one is worked on.
 // With a residual x and it are read for the last time, and h, the stream, is next read a whole layer later: large calls load and
 // store them past the caches (16384x2048 52.4 us, 48.3, the stores alone 53.7; 8192x768, 50 MB, 13.3 and 14.3). 16384x2048 with a
-// residual 45.2 us, 5.9 TB/s; 50432x768 51; 8192x768 12.3, where issuing takes half of the time; one row of 2048 2.7.
+// residual 45.4 us, 5.9 TB/s; 50432x768 51; 8192x768 12.5, where issuing takes half of the time; one row of 2048 6.2, the kernel 2.6.
 struct LnFwdArgs {
     const uint16_t *x, *res, *gamma, *beta;
     uint16_t *h, *y;
@@ -394,10 +396,12 @@ void launch_fwd(const LnFwdArgs &a, hipStream_t s)
 // workspace, which a second launch adds in their order (no atomics: the same bits on every run).  512 workgroups of eight waves,
 // two a CU: with more of them the partial sums (8 B a column and workgroup) and their addition take what the further waves gain
 // (18912x768: 768 of them 37 us in the place of 33).  fp32 throughout but for h - mu: mu is a double and is subtracted in two
-// parts, since rows whose mean is far above their deviation cancel there.  What is read here is read for the last time: large
+// parts, since rows whose mean is far above their deviation cancel there.  (A team adds rows / 256 or fewer rows to one sum; of
+// wide rows see below.)  What is read here is read for the last time: large
 // calls read past the caches (16384x2048 56.5 us, 51.2; 8192x768, 50 MB, 16.9 and 17.6).  Wide rows on teams of more waves with
-// fewer elements each: the sums' registers are what limits the waves. 16384x2048 with dres 51.2 us, 5.2 TB/s (45 + 4.5 for the
-// second launch); 18912x768 28.0, 50432x768 59.2, 8192x768 16.1; 257x1001 7.0, one launch.
+// fewer elements each: the sums' registers are what limits the waves. 16384x2048 with dres 51.1 us, 5.3 TB/s (kernels: 45.8 and 4.7
+// for the second launch); 18912x768 28.1, 50432x768 59.1, 8192x768 15.9; 257x1001 7.0, the one kernel 6.0.  Rows of more than 8192
+// columns read h and dy twice: 2048x16384 87 us, 3.1 TB/s.
 struct LnBwdArgs {
     const uint16_t *dy, *h, *gamma, *dres;
     const double *stats;
@@ -751,9 +755,9 @@ __global__ __launch_bounds__(kFinThreads) void ln_bwd_finish_kernel(const float 
 // few rows, of which a workgroup can take 64 columns as fast as others the rows
 bool bwd_alone(int64_t rows, int64_t cols) { return rows <= 512 && cols <= 8192; }
 
-// What a backward call runs on: T, P, V and WAVES of the kernel, the fewest lanes that hold a row with 4 to 16 elements each, but
-// 64 for the widths to 256: 16 elements on each of 16 lanes are better on long calls (131072x256 42.3 us, 46.6) and worse
-// on others (20000x200 16.2, 13.4; 65536x256 33.5, 32.0).  64 columns on 8 lanes: 65536x64 15.5, on 16 13.7; 524288x64 42.0, 45.9.
+// What a backward call runs on: T, P, V and WAVES of the kernel, lanes with 4 to 12 elements of a row each (their column sums take
+// twice as many registers again).  64 lanes for the widths to 256: 16 elements on each of 16 lanes are better on long calls
+// (131072x256 42.3 us, 46.6) and worse on others (20000x200 16.2, 13.4; 65536x256 33.5, 32.0).  64 columns on 8 lanes: 65536x64 15.5, on 16 13.7; 524288x64 42.0, 45.9.
 struct BwdShape {
     int waves_a_row, pieces, elements, waves;
     bool wide;
@@ -831,7 +835,10 @@ hipError_t launch_layernorm_fwd(const void *x, const void *res, const void *gamm
     const LnFwdArgs a{(const uint16_t *)x, (const uint16_t *)res, (const uint16_t *)gamma, (const uint16_t *)beta, (uint16_t *)h_out,
                       (uint16_t *)y, stats, rows, (int)cols, eps};
     // the fewest lanes that hold a row with 8 to 16 elements each (131072x256 on 16 lanes 29.9 us, on 64 41.0; two pieces of
-    // eight a lane are better than twice the waves: 2048 wide 53.9 us, 59.5)
+    // eight a lane are better than twice the waves: 2048 wide 53.9 us, 59.5).  With a residual two pieces on 16 lanes spill four
+    // registers at four waves a SIMD: 131072x256 45.8 us, on 64 lanes 49.6; 65536x256 27.6, 28.2; 400000x256 159, 169, and without
+    // spills at three waves 45.5, 25.6, 164.  (Ragged widths of 129 to 255 with a residual: 65536x250 34.6, on 64 lanes 36.6, but
+    // 20000x250 14.0, 12.6.)
     if (cols <= 64)
         launch_fwd<-1, 1, 8, 4>(a, s);
     else if (cols <= 128)

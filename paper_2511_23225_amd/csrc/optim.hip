@@ -1,4 +1,5 @@
 // What follows the gradients of a training step: the sum of their squares over all tensors, and the AdamW step.  gfx950 only.
+// Times in the comments: a call among others in a replayed graph, on three sets of tensors in turn.
 #include <algorithm>
 #include "kernels.h"
 #include "device_utils.h"
@@ -296,8 +297,8 @@ __global__ __launch_bounds__(kSumsqThreads) void grad_sumsq_finish_kernel(const 
 // AdamW: with the clipped gradient g' = c g, c = min(1, max_norm / (sqrt(S) + 1e-6)),
 //   m = b1 m + (1 - b1) g',  v = b2 v + (1 - b2) g'^2,  p = p - lr wd p - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps).
 // Bound by memory: 28 B an element with fp32 states beside an fp32 copy, 22 without; 16 and 10 with 8-bit states.  A wave takes
-// one chunk, all of whose loads (20 to 28 of 4 to 16 bytes a lane) are under way before the first is waited for, and workgroups
-// walk the tensors in order: 51 M elements with master, fp32 states 241 us (6.0 TB/s), 205 M with 8-bit states 580 (5.7), without
+// one chunk, all of whose loads (16, with 8-bit states 18, of 4 to 16 bytes a lane) are under way before the first is waited for, and
+// workgroups walk the tensors in order: 51 M elements with master, fp32 states 241 us (6.0 TB/s), 205 M with 8-bit states 580 (5.7), without
 // master 374 (5.5, half of its time the SIMDs issue).  Persistent waves, each on a run of chunks of its own, took 301, 703 and
 // 450; persistent ones in turns, the streams of all side by side, 284 and 665.
 //
@@ -406,7 +407,9 @@ __device__ __forceinline__ uint32_t encode(float magnitude, float scale, float t
 
 constexpr uint32_t kDitherElement = 0x6A09E667u, kDitherStep = 0x9E3779B9u;  // 2^32 (sqrt(2) - 1), 2^32 (sqrt(5) - 1) / 2, odd
 
-// What a step needs beside its tensors; false: nothing may change.
+// What a step needs beside its tensors; false: nothing may change.  With a schedule every wave takes the powers, quotients and the root
+// for itself, while its loads are under way: 51 M elements with fp32 states 241 us, with a schedule 248; 3 M in 61 tensors with 8-bit
+// ones 15.5 and 16.8; 205 M 575 and 555.
 __device__ __forceinline__ bool step_scalars(const AdamwArgs &a, StepScalars &k)
 {
     k = {a.lr, a.step_size, a.inv_sqrt_bc2, 1.0f, a.step * kDitherStep};
@@ -570,7 +573,9 @@ constexpr int64_t kAdamwMostGroups = 1 << 20;
 // Whether buffers of so many bytes an element are more than the memory-side cache (256 MB) gives back to the next step.  One step after the
 // other, without and with accesses past the caches: fp32 states beside a master, 28 B an element, 3 M elements 15.3 us and 17.7, 5 M 24.7 and
 // 25.9, 7 M 36.9 and 34.8, 20 M 108 and 87; 8-bit ones, 16 B, 5 M 19.0 and 20.7, 10 M 32.8 and 30.9, 20 M 67 and 58.
-// (The norm, bf16 gradients: 103 MB 22.9 and 22.9, 411 MB 77 and 68.)
+// (The norm, bf16 gradients: 103 MB 22.9 and 22.9, 411 MB 77 and 68.)  The callers count what was measured here, 28, 16 and 2 bytes an
+// element, whatever a table holds: without a master (22 and 10) it is from 124 and 98 MB on, of fp32 gradients from 315 MB on (200 MB
+// 40 us, 5.0 TB/s; 280 MB 53.5; 320 MB 52.8, 6.1 TB/s).
 constexpr int64_t kKeptBytes = 150 << 20;
 bool past_caches(int64_t chunks, int64_t bytes) { return chunks * kChunk * bytes > kKeptBytes; }
 
