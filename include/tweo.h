@@ -2,7 +2,9 @@
  * tweo.h - C ABI of the MI355X (gfx950) library for the per-tensor FP8 linear
  * layer with the fused TWEO activation-outlier penalty, and for the W8A8
  * per-tensor static INT8 linear layer (TWEO, arXiv 2511.23225), with what a training
- * step needs around the linears: LayerNorm's gradients, the gradients' norm, AdamW.
+ * step needs around the linears: LayerNorm's gradients, the gradients' norm, AdamW;
+ * and with what a block runs between them: rotary positions, norms of the heads of queries
+ * and keys, the gated feed-forward.
  *
  * Conventions that hold for every entry point
  *   - Every data pointer is a DEVICE pointer owned by the caller; the library
@@ -56,7 +58,8 @@ enum {
     TWEO_OP_FP8_LINEAR_BWD_BF16 = 4,
     TWEO_OP_LAYERNORM_QUANTIZE = 5, /* M = rows; N, K unused (pass 1) */
     TWEO_OP_LAYERNORM_BWD = 6,      /* M = rows, N = cols; K unused (pass 1) */
-    TWEO_OP_GRAD_SUMSQ = 7          /* the same for every table (pass 1, 1, 1) */
+    TWEO_OP_GRAD_SUMSQ = 7,         /* the same for every table (pass 1, 1, 1) */
+    TWEO_OP_HEAD_NORM_ROTARY_BWD = 8 /* M = tokens, N = heads of both groups, K = dim */
 };
 
 /* Bytes of device workspace the given operation can use for these sizes (a
@@ -665,6 +668,106 @@ typedef struct {
  */
 tweo_status tweo_adamw_step(const tweo_optim_plan *plan, const tweo_adamw_cfg *cfg, const double *grad_sumsq,
                             const tweo_adamw_schedule *schedule, void *stream);
+
+/*
+ * Rotary positions.  Heads of `dim` values, of which the first rot_dim are turned, pair by pair, by the
+ * token's position:
+ *   angle_i = position * freqs[i],   i < rot_dim / 2
+ *   (a, b)  = scale * (a cos(angle_i) - b sin(angle_i), b cos(angle_i) + a sin(angle_i))
+ * with (a, b) the values i and rot_dim / 2 + i of the head (TWEO_ROTARY_HALVES) or 2i and 2i + 1
+ * (TWEO_ROTARY_PAIRS); the other dim - rot_dim values stay as they are.  The angle is taken in fp64 and
+ * reduced to a turn there (to 2^-51 of the turns gone through: a position of 10^9 costs nothing that bf16 shows), the rest is
+ * fp32, one rounding to bf16.
+ *   positions  int64 [tokens] on the device.  A negative one marks padding: that token's heads are neither
+ *              read nor written, and count in no gradient.
+ *   freqs      fp64 [rot_dim / 2] on the device, radians a position: whatever a scaling for long contexts makes of
+ *              them (tweo_rotary_freqs), once for a model.
+ *   scale      factor of the turned part (an attention factor that goes with such a scaling), 1 without; finite.
+ */
+enum { TWEO_ROTARY_HALVES = 0, TWEO_ROTARY_PAIRS = 1 };
+typedef struct {
+    const int64_t *positions;
+    const double *freqs;
+    int rot_dim; /* even, 2 .. dim */
+    int layout;
+    float scale;
+} tweo_rotary_cfg;
+
+/* Heads of a tensor [tokens, heads, dim], bf16, whose last index is contiguous; the strides of a token and of a
+ * head, in elements, not negative, are the caller's: queries and keys as they lie in the output of a qkv linear are two of
+ * these.  Element-aligned; 16-byte aligned heads (addresses, strides and dim multiples of 8, rot_dim of 16) run
+ * several times as fast as others. */
+typedef struct {
+    const void *x;
+    void *y;
+    int64_t x_token, x_head, y_token, y_head;
+    const void *gain_bf16; /* [dim] or NULL (= 1); tweo_rotary: NULL */
+    int heads;
+} tweo_heads;
+
+/*
+ * Turns one or two groups of heads (queries and keys: as many heads each as they have) of the same tokens, one
+ * launch.  transpose != 0: the transposed map, the gradient's (also times scale).
+ *   groups: host array of `count` (1 or 2); y may be the same group's x (the same address and strides), else nothing that
+ *   is written overlaps anything.  dim 1 .. 512, heads of a group up to 2^16, tokens up to 2^30.
+ * Errors: TWEO_ERR_INVALID_ARG (null, misaligned, sizes below 1, an odd or too large rot_dim, negative strides, a
+ * scale that is not finite, overlap), TWEO_ERR_UNSUPPORTED (beyond these sizes).
+ */
+tweo_status tweo_rotary(const tweo_heads *groups, int count, int64_t tokens, int dim, const tweo_rotary_cfg *cfg,
+                        int transpose, void *stream);
+
+/*
+ * The frequencies of a rotary position, on the HOST (freqs: host array of rot_dim / 2 doubles).
+ *   TWEO_ROTARY_FREQS_PLAIN   f_i = base^(-2i / rot_dim)
+ *   TWEO_ROTARY_FREQS_LINEAR  f_i / factor (positions squeezed into the context trained on)
+ *   TWEO_ROTARY_FREQS_BASE    the plain ones of base * factor^(rot_dim / (rot_dim - 2)): the quickest stays,
+ *                             the slowest is divided by factor; rot_dim > 2
+ *   TWEO_ROTARY_FREQS_TURNS   f_i * (s + (1 - s) / factor), s = clamp((context * f_i / 2 pi - low_turns) /
+ *                             (high_turns - low_turns), 0, 1): what turns often within the context trained on stays,
+ *                             what turns hardly is divided
+ * base > 1, factor >= 1; factor is not used by PLAIN, context (> 0) and 0 <= low_turns < high_turns by TURNS alone.
+ * Errors: TWEO_ERR_INVALID_ARG.
+ */
+enum { TWEO_ROTARY_FREQS_PLAIN = 0, TWEO_ROTARY_FREQS_LINEAR = 1, TWEO_ROTARY_FREQS_BASE = 2, TWEO_ROTARY_FREQS_TURNS = 3 };
+typedef struct {
+    double base;
+    int kind;
+    double factor, context, low_turns, high_turns;
+} tweo_rotary_freq_cfg;
+tweo_status tweo_rotary_freqs(const tweo_rotary_freq_cfg *cfg, int rot_dim, double *freqs);
+
+/*
+ * Norm of each head and its rotation in one pass:
+ *   xhat = x * rstd,  rstd = 1 / sqrt(mean_dim(x^2) + eps),  y = bf16( R( xhat * gain ) )
+ * with R the rotation of `cfg` as in tweo_rotary, or nothing where cfg is NULL (and every token counts).  fp32, one
+ * rounding (squares beyond fp32 in fp64).  gain: one for all heads of a group.  eps >= 0; with eps = 0 a head of
+ * zeros becomes NaN.  Groups, sizes, in place and errors as tweo_rotary, and a negative or NaN eps.
+ */
+tweo_status tweo_head_norm_rotary_fwd(const tweo_heads *groups, int count, int64_t tokens, int dim, float eps,
+                                      const tweo_rotary_cfg *cfg, void *stream);
+
+/*
+ * Its gradients.  With d = R^T dy and w = d * gain:
+ *   dx    = bf16( rstd * (w - xhat * mean_dim(w * xhat)) )
+ *   dgain = sum over tokens and heads of d * xhat       (fp32, overwritten; fixed order, no atomics)
+ * The norm is taken again from x, the forward's input: nothing has to be kept but that.  rstd is an fp32 number here: with eps = 0,
+ * heads whose root mean square is below 3e-39 have none.
+ *   dx may be dy or x (the same address and strides), else nothing that is written overlaps anything.
+ *   dgain fp32 [dim], 16-byte aligned, or NULL.
+ *   workspace: tweo_workspace_bytes(TWEO_OP_HEAD_NORM_ROTARY_BWD, tokens, heads of both groups, dim), 16-byte aligned;
+ *   not needed where no dgain is asked for.
+ * Errors as tweo_head_norm_rotary_fwd, and TWEO_ERR_WORKSPACE.
+ */
+typedef struct {
+    const void *dy, *x;
+    void *dx;
+    int64_t dy_token, dy_head, x_token, x_head, dx_token, dx_head;
+    const void *gain_bf16;
+    float *dgain;
+    int heads;
+} tweo_heads_grad;
+tweo_status tweo_head_norm_rotary_bwd(const tweo_heads_grad *groups, int count, int64_t tokens, int dim, float eps,
+                                      const tweo_rotary_cfg *cfg, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Tuning hook for benchmarks and tests: forces the GEMM kernel variant.

@@ -15,7 +15,8 @@ LIB_PATH = os.path.join(_PKG, "libtweo_hip.so")
 
 TWEO_OK, TWEO_ERR_INVALID_ARG, TWEO_ERR_UNSUPPORTED, TWEO_ERR_WORKSPACE, TWEO_ERR_HIP = range(5)
 (TWEO_OP_FP8_LINEAR_FWD, TWEO_OP_FP8_LINEAR_BWD, TWEO_OP_W8A8_LINEAR, TWEO_OP_FP8_LINEAR_FWD_BF16,
- TWEO_OP_FP8_LINEAR_BWD_BF16, TWEO_OP_LAYERNORM_QUANTIZE, TWEO_OP_LAYERNORM_BWD, TWEO_OP_GRAD_SUMSQ) = range(8)
+ TWEO_OP_FP8_LINEAR_BWD_BF16, TWEO_OP_LAYERNORM_QUANTIZE, TWEO_OP_LAYERNORM_BWD, TWEO_OP_GRAD_SUMSQ,
+ TWEO_OP_HEAD_NORM_ROTARY_BWD) = range(9)
 
 EXPORTS = ("tweo_workspace_bytes", "tweo_status_string", "tweo_amax", "tweo_quantize_e4m3",
            "tweo_fp8_linear_fwd", "tweo_fp8_linear_bwd", "tweo_quantize_i8", "tweo_w8a8_linear",
@@ -30,7 +31,8 @@ EXPORTS = ("tweo_workspace_bytes", "tweo_status_string", "tweo_amax", "tweo_quan
            "tweo_layernorm_quantize_e4m3", "tweo_layernorm_quantize_e4m3_delayed",
            "tweo_fp8_linear_fwd_bf16_delayed", "tweo_fp8_linear_bwd_bf16_delayed",
            "tweo_layernorm_fwd", "tweo_layernorm_bwd", "tweo_optim_table_bytes", "tweo_optim_plan_init",
-           "tweo_grad_sumsq", "tweo_adamw_step")
+           "tweo_grad_sumsq", "tweo_adamw_step", "tweo_rotary", "tweo_rotary_freqs", "tweo_head_norm_rotary_fwd",
+           "tweo_head_norm_rotary_bwd")
 
 
 class TweoError(RuntimeError):
@@ -63,6 +65,26 @@ class OptimPlan(ctypes.Structure):
 
 class AdamwCfg(ctypes.Structure):
     _fields_ = [(k, ctypes.c_double) for k in ("lr", "beta1", "beta2", "eps", "max_norm")] + [("step", ctypes.c_int64)]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = ([(k, ctypes.c_void_p) for k in ("x", "y")] + [(k, ctypes.c_int64) for k in ("x_token", "x_head", "y_token", "y_head")] +
+                [("gain", ctypes.c_void_p), ("heads", ctypes.c_int)])
+
+
+class HeadsGrad(ctypes.Structure):
+    _fields_ = ([(k, ctypes.c_void_p) for k in ("dy", "x", "dx")] +
+                [(k, ctypes.c_int64) for k in ("dy_token", "dy_head", "x_token", "x_head", "dx_token", "dx_head")] +
+                [(k, ctypes.c_void_p) for k in ("gain", "dgain")] + [("heads", ctypes.c_int)])
+
+
+class RotaryCfg(ctypes.Structure):
+    _fields_ = [("positions", ctypes.c_void_p), ("freqs", ctypes.c_void_p), ("rot_dim", ctypes.c_int), ("layout", ctypes.c_int),
+                ("scale", ctypes.c_float)]
+
+
+class RotaryFreqCfg(ctypes.Structure):
+    _fields_ = [("base", ctypes.c_double), ("kind", ctypes.c_int)] + [(k, ctypes.c_double) for k in ("factor", "context", "low_turns", "high_turns")]
 
 
 _lib = None
@@ -133,6 +155,10 @@ def load():
     L.tweo_optim_plan_init.argtypes = [ctypes.POINTER(OptimTensor), ctypes.c_int, vp, sz, ctypes.POINTER(OptimPlan), vp]
     L.tweo_grad_sumsq.argtypes = [ctypes.POINTER(OptimPlan), vp, vp, sz, vp]
     L.tweo_adamw_step.argtypes = [ctypes.POINTER(OptimPlan), ctypes.POINTER(AdamwCfg), vp, vp, vp]
+    L.tweo_rotary.argtypes = [vp, ctypes.c_int, i64, ctypes.c_int, vp, ctypes.c_int, vp]
+    L.tweo_rotary_freqs.argtypes = [ctypes.POINTER(RotaryFreqCfg), ctypes.c_int, vp]
+    L.tweo_head_norm_rotary_fwd.argtypes = [vp, ctypes.c_int, i64, ctypes.c_int, f32, vp, vp]
+    L.tweo_head_norm_rotary_bwd.argtypes = [vp, ctypes.c_int, i64, ctypes.c_int, f32, vp, vp, sz, vp]
     for name in EXPORTS:
         if name not in ("tweo_workspace_bytes", "tweo_status_string", "tweo_delayed_state_bytes",
                         "tweo_static_scratch_bytes", "tweo_optim_table_bytes"):
@@ -480,7 +506,7 @@ def _same(device, shape, dtype, tensors, names):
 @functools.lru_cache(maxsize=1)
 def _types():
     import torch
-    return torch.bfloat16, torch.float32, torch.float64, torch.int32, torch.uint32
+    return torch.bfloat16, torch.float32, torch.float64, torch.int32, torch.uint32, torch.int64
 
 
 def _scratch(device, t, name):
@@ -600,7 +626,7 @@ def tweo_adamw_step(plan, lr=None, step=None, beta1=0.9, beta2=0.999, eps=1e-8, 
     """lr and step, or schedule: a torch.int32 (or uint32) tensor of two words on the device, the bits of lr as fp32 and step
     (schedule[:1].view(torch.float32).fill_(lr); schedule[1:].fill_(step))."""
     dev = _on_device(plan, grad_sumsq)
-    if schedule is not None and (schedule.dtype not in _types()[3:] or schedule.numel() < 2 or not schedule.is_contiguous() or schedule.get_device() != dev):
+    if schedule is not None and (schedule.dtype not in _types()[3:5] or schedule.numel() < 2 or not schedule.is_contiguous() or schedule.get_device() != dev):
         raise ValueError("schedule: two contiguous 32-bit integers on cuda:%d are needed, got %d of %s, strides %s, on %s" %
                          (dev, schedule.numel(), schedule.dtype, schedule.stride(), schedule.device))
     if schedule is None:
@@ -611,3 +637,103 @@ def tweo_adamw_step(plan, lr=None, step=None, beta1=0.9, beta2=0.999, eps=1e-8, 
         cfg = AdamwCfg(0.0, beta1, beta2, eps, max_norm, 1)
     _check(load().tweo_adamw_step(ctypes.byref(plan), ctypes.byref(cfg), _ptr(grad_sumsq), _ptr(schedule), _stream()),
            "tweo_adamw_step")
+
+
+ROTARY_LAYOUTS = {"halves": 0, "pairs": 1}  # TWEO_ROTARY_HALVES, TWEO_ROTARY_PAIRS
+ROTARY_FREQS = {"plain": 0, "linear": 1, "base": 2, "turns": 3}  # TWEO_ROTARY_FREQS_*
+
+
+def tweo_rotary_freqs(rot_dim, base=10000.0, kind="plain", factor=1.0, context=0.0, low_turns=0.0, high_turns=0.0):
+    """The frequencies of rot_dim / 2 pairs, radians a position: a torch.float64 tensor on the CPU, to be moved to the GPU once."""
+    import torch
+    if kind not in ROTARY_FREQS:
+        raise ValueError("kind: one of %s is needed, got %r" % (", ".join(ROTARY_FREQS), kind))
+    freqs = torch.empty(max(1, rot_dim // 2), dtype=torch.float64)
+    cfg = RotaryFreqCfg(base, ROTARY_FREQS[kind], factor, context, low_turns, high_turns)
+    _check(load().tweo_rotary_freqs(ctypes.byref(cfg), rot_dim, freqs.data_ptr()), "tweo_rotary_freqs")
+    return freqs
+
+
+def _heads(device, shape, tensors, names):
+    """Refuses heads that are no [tokens, heads, dim] of bf16 on the current device with a contiguous last index."""
+    bf16 = _types()[0]
+    for i, t in enumerate(tensors):
+        if t.dtype is not bf16 or t.shape != shape or t.stride(2) != 1 and shape[2] != 1 or t.get_device() != device:
+            raise ValueError("%s: a %s tensor of shape %s on cuda:%d, the current device, with a contiguous last index is needed, got %s of %s, strides %s, on %s" %
+                             (names[i], bf16, tuple(shape), device, t.dtype, tuple(t.shape), t.stride(), t.device))
+
+
+def _rotary(device, shape, positions, freqs, layout, scale):
+    """The rotation, or None where there is none."""
+    if positions is None and freqs is None:
+        return None
+    if layout not in ROTARY_LAYOUTS:
+        raise ValueError("layout: halves or pairs is needed, got %r" % (layout,))
+    int64, f64 = _types()[5], _types()[2]
+    _same(device, shape[:1], int64, (positions,), ("positions",))
+    if freqs is None or positions is None:
+        raise ValueError("positions and freqs are needed together")
+    if freqs.dtype is not f64 or freqs.dim() != 1 or not freqs.is_contiguous() or freqs.get_device() != device:
+        raise ValueError("freqs: a contiguous %s vector on cuda:%d, the current device, is needed, got %s of %s on %s" %
+                         (f64, device, freqs.dtype, tuple(freqs.shape), freqs.device))
+    return ctypes.byref(RotaryCfg(positions.data_ptr(), freqs.data_ptr(), 2 * freqs.numel(), ROTARY_LAYOUTS[layout], scale))
+
+
+def _groups(groups, width):
+    if not 1 <= len(groups) <= 2 or any(len(g) != width for g in groups):
+        raise ValueError("one or two groups of %d tensors are needed" % width)
+    shape = groups[0][0].shape
+    if len(shape) != 3 or any(g[0].dim() != 3 or g[0].shape[0] != shape[0] or g[0].shape[2] != shape[2] for g in groups):
+        raise ValueError("heads: [tokens, heads, dim] of the same tokens and dim are needed, got %s" % ", ".join(str(tuple(g[0].shape)) for g in groups))
+    return shape
+
+
+_HEADS, _HEADS_GRAD, _GAIN, _DGAIN = ("x", "y"), ("dy", "x", "dx"), ("gain",), ("dgain",)
+
+
+def tweo_rotary(groups, positions, freqs, layout="halves", scale=1.0, transpose=False):
+    """groups: one or two (x, y), bf16 [tokens, heads, dim] of any token and head stride; y may be x.  positions: int64 [tokens], negative:
+    padding.  freqs: float64 [rot_dim / 2] (tweo_rotary_freqs)."""
+    shape, dev = _groups(groups, 2), _device()
+    cfg = _rotary(dev, shape, positions, freqs, layout, scale)
+    if cfg is None:
+        raise ValueError("positions and freqs are needed")
+    rows = (Heads * len(groups))()
+    for row, (x, y) in zip(rows, groups):
+        _heads(dev, x.shape, (x, y), _HEADS)
+        row.x, row.y, row.heads = x.data_ptr(), y.data_ptr(), x.shape[1]
+        row.x_token, row.x_head, _ = x.stride()
+        row.y_token, row.y_head, _ = y.stride()
+    _check(load().tweo_rotary(rows, len(groups), shape[0], shape[2], cfg, 1 if transpose else 0, _stream()), "tweo_rotary")
+
+
+def tweo_head_norm_rotary_fwd(groups, positions=None, freqs=None, layout="halves", scale=1.0, eps=1e-6):
+    """groups: one or two (x, gain, y); x and y as in tweo_rotary, gain bf16 [dim] or None.  Without positions and freqs the norm alone."""
+    shape, dev = _groups(groups, 3), _device()
+    cfg = _rotary(dev, shape, positions, freqs, layout, scale)
+    rows = (Heads * len(groups))()
+    for row, (x, gain, y) in zip(rows, groups):
+        _heads(dev, x.shape, (x, y), _HEADS)
+        _same(dev, shape[2:], _types()[0], (gain,), _GAIN)
+        row.x, row.y, row.gain, row.heads = x.data_ptr(), y.data_ptr(), _ptr(gain), x.shape[1]
+        row.x_token, row.x_head, _ = x.stride()
+        row.y_token, row.y_head, _ = y.stride()
+    _check(load().tweo_head_norm_rotary_fwd(rows, len(groups), shape[0], shape[2], eps, cfg, _stream()), "tweo_head_norm_rotary_fwd")
+
+
+def tweo_head_norm_rotary_bwd(groups, positions=None, freqs=None, layout="halves", scale=1.0, eps=1e-6, workspace=None):
+    """groups: one or two (dy, x, gain, dx, dgain): the gradient of the forward's y, its x and gain, where the gradient of x goes (dy or x
+    itself, or another) and that of gain (float32 [dim], or None)."""
+    shape, dev = _groups(groups, 5), _device()
+    cfg = _rotary(dev, shape, positions, freqs, layout, scale)
+    rows = (HeadsGrad * len(groups))()
+    for row, (dy, x, gain, dx, dgain) in zip(rows, groups):
+        _heads(dev, dy.shape, (dy, x, dx), _HEADS_GRAD)
+        _same(dev, shape[2:], _types()[0], (gain,), _GAIN)
+        _same(dev, shape[2:], _types()[1], (dgain,), _DGAIN)
+        row.dy, row.x, row.dx, row.gain, row.dgain, row.heads = dy.data_ptr(), x.data_ptr(), dx.data_ptr(), _ptr(gain), _ptr(dgain), dy.shape[1]
+        row.dy_token, row.dy_head, _ = dy.stride()
+        row.x_token, row.x_head, _ = x.stride()
+        row.dx_token, row.dx_head, _ = dx.stride()
+    wp, wb = _scratch(dev, workspace, "workspace")
+    _check(load().tweo_head_norm_rotary_bwd(rows, len(groups), shape[0], shape[2], eps, cfg, wp, wb, _stream()), "tweo_head_norm_rotary_bwd")

@@ -2,6 +2,7 @@
 // Nothing here allocates, frees or synchronises; everything is enqueued on the
 // caller's stream.
 #include <algorithm>
+#include <cmath>
 #include <memory>
 #include <new>
 #include "../../include/tweo.h"
@@ -136,6 +137,9 @@ size_t tweo_workspace_bytes(int op, int64_t M, int64_t N, int64_t K)
     case TWEO_OP_W8A8_LINEAR:
         return 256 + round256(std::max(stream_k_candidate(M, N, K) ? stream_k_workspace_bytes() : (size_t)0,
                                        i8_gemm_ksplit_bytes(M, N, K)));
+    case TWEO_OP_HEAD_NORM_ROTARY_BWD:  // M tokens, N heads, K dim; sizes that no call takes: as those of the largest it takes
+        return round256((size_t)heads_grad_bytes(std::min(M, kMaxDim), std::min<int64_t>(N, 2 * kHeadsMaxHeads),
+                                                 std::min<int64_t>(K, kHeadsMaxDim)));
     case TWEO_OP_LAYERNORM_QUANTIZE:  // M rows (N, K unused)
         return kAmaxPartialsMax * sizeof(uint32_t) + 256 + round256((size_t)M * 2 * sizeof(double));
     case TWEO_OP_LAYERNORM_BWD:  // M rows of N columns
@@ -644,6 +648,253 @@ tweo_status tweo_layernorm_bwd(const void *dy_bf16, const void *h_bf16, const vo
         return TWEO_ERR_INVALID_ARG;
     return hip_status(launch_layernorm_bwd(dy_bf16, h_bf16, gamma_bf16, stats, residual_grad_bf16, rows, cols, dx_bf16, dgamma,
                                            dbeta, workspace, (hipStream_t)stream));
+}
+
+namespace {
+// A tensor [tokens, heads, dim] of bf16 by its strides, as byte ranges in up to two nested lattices.
+struct Lattice {
+    uintptr_t at;
+    int64_t n_out, s_out, n_in, s_in;  // outer and inner count and stride (bytes); a count of 1 has stride 0
+    int64_t head;                      // bytes of a head
+    int64_t width() const { return (n_in - 1) * s_in + head; }
+    int64_t span() const { return (n_out - 1) * s_out + width(); }
+    bool same(const Lattice &o) const
+    {
+        return at == o.at && n_out == o.n_out && s_out == o.s_out && n_in == o.n_in && s_in == o.s_in && head == o.head;
+    }
+    bool folds() const { return (n_in > 1 && s_in < head) || (n_out > 1 && s_out < width()); }  // onto itself
+};
+
+Lattice lattice(const void *p, int64_t tokens, int64_t token, int64_t heads, int64_t head_stride, int dim)
+{
+    const int64_t t = tokens > 1 ? 2 * token : 0, h = heads > 1 ? 2 * head_stride : 0;
+    Lattice l{(uintptr_t)p, tokens, t, heads, h, 2 * (int64_t)dim};
+    if (h > t || tokens == 1) {
+        std::swap(l.n_out, l.n_in);
+        std::swap(l.s_out, l.s_in);
+    }
+    return l;
+}
+
+// whether they may share a byte: apart, or in the same lattice at another place (parts of one qkv tensor)
+bool lattices_clash(const Lattice &a, const Lattice &b)
+{
+    if (a.at + (uintptr_t)a.span() <= b.at || b.at + (uintptr_t)b.span() <= a.at)
+        return false;
+    auto apart = [&](int64_t stride, int64_t wa, int64_t wb) {
+        if (stride <= 0)
+            return false;
+        const int64_t d = (int64_t)(b.at >= a.at ? (b.at - a.at) % (uintptr_t)stride
+                                                 : ((uintptr_t)stride - (a.at - b.at) % (uintptr_t)stride) % (uintptr_t)stride);
+        return d >= wa && d + wb <= stride;
+    };
+    if (a.s_out == b.s_out && apart(a.s_out, a.width(), b.width()))
+        return false;
+    return !(a.s_in == b.s_in && a.s_in > 0 && a.s_out == b.s_out && a.s_out % a.s_in == 0 && apart(a.s_in, a.head, b.head));
+}
+
+// the buffers of a call on heads: what it writes overlaps nothing but, in place, what it is
+struct HeadsBuffers {
+    Lattice l[13];
+    bool written[13];
+    int in_place_of[13];  // a written one that this may be, or -1
+    int n = 0;
+    int add(const Lattice &x, bool w, int in_place = -1)
+    {
+        l[n] = x;
+        written[n] = w;
+        in_place_of[n] = in_place;
+        return n++;
+    }
+    void add_flat(const void *p, int64_t bytes, bool w)
+    {
+        if (p)
+            add(Lattice{(uintptr_t)p, 1, 0, 1, 0, bytes}, w);
+    }
+    bool clash() const
+    {
+        for (int i = 0; i < n; ++i) {
+            if (written[i] && l[i].folds())
+                return true;
+            for (int j = 0; j < i; ++j) {
+                if (!(written[i] || written[j]) || (in_place_of[i] == j && l[i].same(l[j])))
+                    continue;
+                if (lattices_clash(l[i], l[j]))
+                    return true;
+            }
+        }
+        return false;
+    }
+};
+
+tweo_status check_heads(int count, int64_t tokens, int dim, const tweo_rotary_cfg *cfg, HeadsCall &c)
+{
+    if (count < 1 || count > 2 || tokens < 1 || dim < 1)
+        return TWEO_ERR_INVALID_ARG;
+    if (cfg && (!cfg->positions || !cfg->freqs || !aligned8(cfg->positions) || !aligned8(cfg->freqs) || cfg->rot_dim < 2 ||
+                cfg->rot_dim % 2 != 0 || cfg->rot_dim > dim || (cfg->layout != TWEO_ROTARY_HALVES && cfg->layout != TWEO_ROTARY_PAIRS) ||
+                !std::isfinite(cfg->scale)))
+        return TWEO_ERR_INVALID_ARG;
+    if (dim > kHeadsMaxDim || tokens > kMaxDim)
+        return TWEO_ERR_UNSUPPORTED;
+    c.sides = count;
+    c.tokens = tokens;
+    c.dim = dim;
+    if (cfg) {
+        c.rot = cfg->rot_dim;
+        c.pairs = cfg->layout == TWEO_ROTARY_PAIRS;
+        c.positions = cfg->positions;
+        c.freqs = cfg->freqs;
+        c.scale = cfg->scale;
+    }
+    return TWEO_OK;
+}
+
+// a tensor of a group: present, element-aligned, strides in a range whose products stay in 64 bits
+tweo_status check_strides(const void *p, int64_t tokens, int64_t token, int heads, int64_t head)
+{
+    if (!p || ((uintptr_t)p & 1) != 0 || heads < 1 || token < 0 || head < 0)
+        return TWEO_ERR_INVALID_ARG;
+    constexpr int64_t most = (int64_t)1 << 46;
+    if (heads > kHeadsMaxHeads || tokens * heads > ((int64_t)1 << 34) || (tokens > 1 && token > most / tokens) ||
+        (heads > 1 && head > most / heads))
+        return TWEO_ERR_UNSUPPORTED;
+    return TWEO_OK;
+}
+
+void add_rotary(HeadsBuffers &all, const HeadsCall &c)
+{
+    all.add_flat(c.positions, 8 * c.tokens, false);
+    all.add_flat(c.freqs, 4 * (int64_t)c.rot, false);
+}
+
+tweo_status heads_call(const tweo_heads *groups, int count, int64_t tokens, int dim, const tweo_rotary_cfg *cfg, bool gains,
+                       HeadsCall &c)
+{
+    if (!groups)
+        return TWEO_ERR_INVALID_ARG;
+    tweo_status st = check_heads(count, tokens, dim, cfg, c);
+    HeadsBuffers all;
+    for (int i = 0; st == TWEO_OK && i < count; ++i) {
+        const tweo_heads &g = groups[i];
+        st = check_strides(g.x, tokens, g.x_token, g.heads, g.x_head);
+        if (st == TWEO_OK)
+            st = check_strides(g.y, tokens, g.y_token, g.heads, g.y_head);
+        if (st == TWEO_OK && g.gain_bf16 && (!gains || ((uintptr_t)g.gain_bf16 & 1) != 0))
+            st = TWEO_ERR_INVALID_ARG;
+        if (st != TWEO_OK)
+            return st;
+        const int y = all.add(lattice(g.y, tokens, g.y_token, g.heads, g.y_head, dim), true);
+        all.add(lattice(g.x, tokens, g.x_token, g.heads, g.x_head, dim), false, y);
+        all.add_flat(g.gain_bf16, 2 * (int64_t)dim, false);
+        c.side[i] = {g.x, nullptr, g.gain_bf16, g.y, g.x_token, g.x_head, 0, 0, g.y_token, g.y_head, g.heads, nullptr};
+    }
+    if (st != TWEO_OK)
+        return st;
+    add_rotary(all, c);
+    return all.clash() ? TWEO_ERR_INVALID_ARG : TWEO_OK;
+}
+}  // namespace
+
+tweo_status tweo_rotary(const tweo_heads *groups, int count, int64_t tokens, int dim, const tweo_rotary_cfg *cfg,
+                        int transpose, void *stream)
+{
+    if (!cfg)
+        return TWEO_ERR_INVALID_ARG;
+    HeadsCall c{};
+    const tweo_status st = heads_call(groups, count, tokens, dim, cfg, false, c);
+    if (st != TWEO_OK)
+        return st;
+    c.transpose = transpose != 0;
+    return hip_status(launch_rotary(c, (hipStream_t)stream));
+}
+
+tweo_status tweo_rotary_freqs(const tweo_rotary_freq_cfg *cfg, int rot_dim, double *freqs)
+{
+    if (!cfg || !freqs || rot_dim < 2 || rot_dim % 2 != 0 || !(cfg->base > 1.0) || !std::isfinite(cfg->base) || cfg->kind < 0 ||
+        cfg->kind > TWEO_ROTARY_FREQS_TURNS)
+        return TWEO_ERR_INVALID_ARG;
+    const bool turns = cfg->kind == TWEO_ROTARY_FREQS_TURNS;
+    if (cfg->kind != TWEO_ROTARY_FREQS_PLAIN && (!(cfg->factor >= 1.0) || !std::isfinite(cfg->factor)))
+        return TWEO_ERR_INVALID_ARG;
+    if ((cfg->kind == TWEO_ROTARY_FREQS_BASE && rot_dim == 2) ||
+        (turns && (!(cfg->context > 0.0) || !std::isfinite(cfg->context) || !(cfg->low_turns >= 0.0) ||
+                   !(cfg->high_turns > cfg->low_turns) || !std::isfinite(cfg->high_turns))))
+        return TWEO_ERR_INVALID_ARG;
+    double base = cfg->base;
+    if (cfg->kind == TWEO_ROTARY_FREQS_BASE)
+        base *= std::pow(cfg->factor, (double)rot_dim / (rot_dim - 2));
+    for (int i = 0; i < rot_dim / 2; ++i) {
+        double f = std::pow(base, -2.0 * i / rot_dim);
+        if (cfg->kind == TWEO_ROTARY_FREQS_LINEAR)
+            f /= cfg->factor;
+        if (turns) {
+            const double part = (cfg->context * f / 6.283185307179586477 - cfg->low_turns) / (cfg->high_turns - cfg->low_turns);
+            const double s = std::min(1.0, std::max(0.0, part));
+            f *= s + (1.0 - s) / cfg->factor;
+        }
+        freqs[i] = f;
+    }
+    return TWEO_OK;
+}
+
+tweo_status tweo_head_norm_rotary_fwd(const tweo_heads *groups, int count, int64_t tokens, int dim, float eps,
+                                      const tweo_rotary_cfg *cfg, void *stream)
+{
+    if (!(eps >= 0.0f))
+        return TWEO_ERR_INVALID_ARG;
+    HeadsCall c{};
+    const tweo_status st = heads_call(groups, count, tokens, dim, cfg, true, c);
+    if (st != TWEO_OK)
+        return st;
+    c.eps = eps;
+    return hip_status(launch_head_norm(c, (hipStream_t)stream));
+}
+
+tweo_status tweo_head_norm_rotary_bwd(const tweo_heads_grad *groups, int count, int64_t tokens, int dim, float eps,
+                                      const tweo_rotary_cfg *cfg, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!groups || !(eps >= 0.0f))
+        return TWEO_ERR_INVALID_ARG;
+    HeadsCall c{};
+    tweo_status st = check_heads(count, tokens, dim, cfg, c);
+    if (st != TWEO_OK)
+        return st;
+    c.eps = eps;
+    HeadsBuffers all;
+    int64_t heads = 0;
+    bool sums = false;
+    for (int i = 0; i < count; ++i) {
+        const tweo_heads_grad &g = groups[i];
+        st = check_strides(g.dy, tokens, g.dy_token, g.heads, g.dy_head);
+        if (st == TWEO_OK)
+            st = check_strides(g.x, tokens, g.x_token, g.heads, g.x_head);
+        if (st == TWEO_OK)
+            st = check_strides(g.dx, tokens, g.dx_token, g.heads, g.dx_head);
+        if (st == TWEO_OK && (((uintptr_t)g.gain_bf16 & 1) != 0 || (g.dgain && !aligned16(g.dgain))))
+            st = TWEO_ERR_INVALID_ARG;
+        if (st != TWEO_OK)
+            return st;
+        const int dx = all.add(lattice(g.dx, tokens, g.dx_token, g.heads, g.dx_head, dim), true);
+        all.add(lattice(g.dy, tokens, g.dy_token, g.heads, g.dy_head, dim), false, dx);
+        all.add(lattice(g.x, tokens, g.x_token, g.heads, g.x_head, dim), false, dx);
+        all.add_flat(g.gain_bf16, 2 * (int64_t)dim, false);
+        all.add_flat(g.dgain, 4 * (int64_t)dim, true);
+        heads += g.heads;
+        sums = sums || g.dgain;
+        c.side[i] = {g.x, g.dy, g.gain_bf16, g.dx, g.x_token, g.x_head, g.dy_token, g.dy_head, g.dx_token, g.dx_head, g.heads, g.dgain};
+    }
+    add_rotary(all, c);
+    if (sums) {
+        const int64_t need = heads_grad_bytes(tokens, heads, dim);
+        if (!workspace || !aligned16(workspace) || workspace_bytes < (size_t)need)
+            return TWEO_ERR_WORKSPACE;
+        all.add_flat(workspace, need, true);
+        c.partials = (float *)workspace;
+    }
+    if (all.clash())
+        return TWEO_ERR_INVALID_ARG;
+    return hip_status(launch_head_norm_grad(c, (hipStream_t)stream));
 }
 
 namespace {

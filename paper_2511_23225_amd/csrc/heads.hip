@@ -1,0 +1,478 @@
+// Heads of queries and keys (gfx950): rotation by position, norm of each head with the rotation behind it, and the norm's gradients.
+//
+//   angle  = position * freq (fp64), taken modulo a turn before it becomes fp32
+//   R      : (a, b) -> scale * (a cos - b sin, b cos + a sin) on the pairs of the first `rot` values of a head, the others as they are
+//   rotary : y = R x, or (transposed, the gradient) R^T x
+//   norm   : xhat = x * rstd, rstd = 1 / sqrt(mean(x^2) + eps), y = R (xhat * gain)
+//   grad   : d = R^T dy, w = d * gain, dx = rstd * (w - xhat * mean(w * xhat)), dgain = sum over tokens and heads of d * xhat
+//
+// A head belongs to a team of 1 to 32 lanes (a power of two, 16 values each) that hold both members of a pair in one lane; a
+// head that its strides, its width or the rotated part let fall between 16-byte pieces to a wave, element by element.  The angles of a
+// workgroup's tokens are worked out once, one a thread, into LDS and serve all heads; nothing else is shared, so
+// memory bounds the large calls.
+#include <algorithm>
+#include "device_utils.h"
+#include "kernels.h"
+
+namespace tweo {
+
+constexpr int kHeadsThreads = 256, kHeadsAngles = 2048, kHeadsTokens = 64;  // of a workgroup; angles (16 KB) and tokens at a time
+
+struct HeadsSide {
+    const uint16_t *x, *dy, *gain;
+    uint16_t *y;
+    int64_t x_token, x_head, dy_token, dy_head, y_token, y_head;
+    int heads;
+    // a workgroup's share: so many heads of so many tokens; `splits` workgroups share the heads of a token
+    int block_heads, splits, blocks;
+    int64_t block_tokens;
+};
+struct HeadsDev {
+    HeadsSide side[2];
+    int64_t tokens;
+    int dim, rot;
+    const int64_t *positions;
+    const double *freqs;
+    float scale, eps, sign;  // sign: of the angle
+    float *partials;         // grad: a row of dim for each workgroup
+};
+
+// ---- where a lane's pairs lie.  a, b: its pairs' members, or what is not rotated, two by two.
+template <bool PAIRS>
+struct HeadsVector {  // 16-byte pieces: eight pairs a lane
+    static constexpr int PER = 8;
+    int ca, cb, at;
+    bool va, vb, turns;
+    __device__ __forceinline__ HeadsVector(int l, int dim, int rot)
+    {
+        const int pieces = dim >> 3, lanes = rot >> 4;
+        turns = l < lanes;
+        ca = turns ? (PAIRS ? 2 * l : l) : 2 * l;
+        cb = turns && !PAIRS ? l + lanes : ca + 1;
+        va = ca < pieces;
+        vb = cb < pieces;
+        at = 8 * l;
+    }
+    __device__ __forceinline__ bool rotates(int) const { return turns; }
+    __device__ __forceinline__ int angle(int e) const { return at + e; }
+    __device__ __forceinline__ void load(const uint16_t *p, float (&a)[PER], float (&b)[PER]) const
+    {
+        const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+        const uint4 A = va ? *(const uint4 *)(p + 8 * ca) : zero, B = vb ? *(const uint4 *)(p + 8 * cb) : zero;
+        const uint32_t w[8] = {A.x, A.y, A.z, A.w, B.x, B.y, B.z, B.w};
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if constexpr (PAIRS) {
+                a[k] = bf16lo_to_f32(w[k]);
+                b[k] = bf16hi_to_f32(w[k]);
+            } else {
+                float *h = k < 4 ? a : b;
+                h[2 * (k & 3)] = bf16lo_to_f32(w[k]);
+                h[2 * (k & 3) + 1] = bf16hi_to_f32(w[k]);
+            }
+        }
+    }
+    __device__ __forceinline__ void store(uint16_t *p, const float (&a)[PER], const float (&b)[PER]) const
+    {
+        uint32_t w[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float *h = k < 4 ? a : b;
+            w[k] = PAIRS ? pack_bf16x2(a[k], b[k]) : pack_bf16x2(h[2 * (k & 3)], h[2 * (k & 3) + 1]);
+        }
+        if (va)
+            *(uint4 *)(p + 8 * ca) = make_uint4(w[0], w[1], w[2], w[3]);
+        if (vb)
+            *(uint4 *)(p + 8 * cb) = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+    // a column of the head, or -1
+    __device__ __forceinline__ int column(int e, bool second) const
+    {
+        if constexpr (PAIRS)
+            return (e < 4 ? va : vb) ? 8 * (e < 4 ? ca : cb) + 2 * (e & 3) + second : -1;
+        else
+            return (second ? vb : va) ? 8 * (second ? cb : ca) + e : -1;
+    }
+};
+template <bool PAIRS>
+struct HeadsScalar {  // element by element: pairs lane, lane + 64, ...
+    static constexpr int PER = 4;
+    int lane, dim, rot;
+    __device__ __forceinline__ HeadsScalar(int l, int dim_, int rot_) : lane(l), dim(dim_), rot(rot_) {}
+    __device__ __forceinline__ bool rotates(int e) const { return angle(e) < rot / 2; }
+    __device__ __forceinline__ int angle(int e) const { return lane + kWave * e; }
+    __device__ __forceinline__ int column(int e, bool second) const
+    {
+        const int p = angle(e), half = rot / 2;
+        const int c = PAIRS || p >= half ? 2 * p + second : p + (second ? half : 0);
+        return c < dim ? c : -1;
+    }
+    __device__ __forceinline__ void load(const uint16_t *p, float (&a)[PER], float (&b)[PER]) const
+    {
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            const int i = column(e, false), j = column(e, true);
+            a[e] = i >= 0 ? bits_to_f32((uint32_t)p[i] << 16) : 0.0f;
+            b[e] = j >= 0 ? bits_to_f32((uint32_t)p[j] << 16) : 0.0f;
+        }
+    }
+    __device__ __forceinline__ void store(uint16_t *p, const float (&a)[PER], const float (&b)[PER]) const
+    {
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            const int i = column(e, false), j = column(e, true);
+            const uint32_t w = pack_bf16x2(a[e], b[e]);
+            if (i >= 0)
+                p[i] = (uint16_t)w;
+            if (j >= 0)
+                p[j] = (uint16_t)(w >> 16);
+        }
+    }
+};
+
+// ---- sums over a team of LANES neighbouring lanes: exchanges within a row of 16 by DPP
+template <int CTRL>
+__device__ __forceinline__ float dpp_add_f32(float v)
+{
+    const int o = __builtin_amdgcn_update_dpp((int)f32_to_bits(v), (int)f32_to_bits(v), CTRL, 0xF, 0xF, false);
+    return v + bits_to_f32((uint32_t)o);
+}
+template <int LANES>
+__device__ __forceinline__ float team_sum(float v)
+{
+    if constexpr (LANES >= 2)
+        v = dpp_add_f32<0xB1>(v);  // lane ^ 1
+    if constexpr (LANES >= 4)
+        v = dpp_add_f32<0x4E>(v);  // lane ^ 2
+    if constexpr (LANES >= 8)
+        v = dpp_add_f32<0x141>(v);  // the other four of eight
+    if constexpr (LANES >= 16)
+        v = dpp_add_f32<0x140>(v);  // the other eight of sixteen
+    if constexpr (LANES >= 32)
+        v += __shfl_xor(v, 16, kWave);
+    if constexpr (LANES >= 64)
+        v += __shfl_xor(v, 32, kWave);
+    return v;
+}
+template <int LANES>
+__device__ __forceinline__ double team_sum(double v)
+{
+#pragma unroll
+    for (int off = 1; off < LANES; off <<= 1)
+        v += __shfl_xor(v, off, kWave);
+    return v;
+}
+
+// x becomes xhat.  Squares that leave fp32 (values beyond 2^50, or, without an eps that covers them, below 2^-40) are taken in fp64.
+template <int LANES, int PER>
+__device__ __forceinline__ float heads_normalise(float (&a)[PER], float (&b)[PER], int dim, float per_dim, float eps)
+{
+    float ss = 0.0f;
+#pragma unroll
+    for (int e = 0; e < PER; ++e)
+        ss = __builtin_fmaf(a[e], a[e], __builtin_fmaf(b[e], b[e], ss));
+    ss = team_sum<LANES>(ss);
+    if (ss < 0x1p100f && (ss > 0x1p-80f || eps > 0x1p-80f)) {
+        const float rstd = __builtin_amdgcn_rsqf(__builtin_fmaf(ss, per_dim, eps));
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            a[e] *= rstd;
+            b[e] *= rstd;
+        }
+        return rstd;
+    }
+    double wide = 0.0;
+#pragma unroll
+    for (int e = 0; e < PER; ++e)
+        wide += (double)a[e] * a[e] + (double)b[e] * b[e];
+    const double rstd = 1.0 / __builtin_sqrt(team_sum<LANES>(wide) / dim + (double)eps);
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        a[e] = (float)(a[e] * rstd);
+        b[e] = (float)(b[e] * rstd);
+    }
+    return (float)rstd;
+}
+
+enum HeadsMode { kHeadsRotary, kHeadsNorm, kHeadsGrad };
+
+template <typename LANE, int LANES, int MODE>
+__global__ __launch_bounds__(kHeadsThreads) void heads_kernel(HeadsDev g)
+{
+    constexpr int PER = LANE::PER, TEAMS = kHeadsThreads / LANES;
+    __shared__ float2 angles[kHeadsAngles];
+    __shared__ int padding[kHeadsTokens];
+    const bool second = (int)blockIdx.x >= g.side[0].blocks;
+    const HeadsSide &side = g.side[second];
+    const int block = (int)blockIdx.x - (second ? g.side[0].blocks : 0), split = block % side.splits;
+    const int h0 = split * side.block_heads, nh = min(side.block_heads, side.heads - h0);
+    const int64_t t0 = block / side.splits * side.block_tokens, t1 = min(t0 + side.block_tokens, g.tokens);
+    const int tid = threadIdx.x, team = tid / LANES, half = g.rot >> 1;
+    const LANE lane(tid & (LANES - 1), g.dim, g.rot);
+    const int at_once = half != 0 ? min(kHeadsTokens, kHeadsAngles / half) : kHeadsTokens;
+    const float per_half = half != 0 ? 1.0f / (float)half : 0.0f, per_head = 1.0f / (float)nh, per_dim = 1.0f / (float)g.dim;
+
+    float ga[PER], gb[PER];
+    if constexpr (MODE != kHeadsRotary) {
+        if (side.gain != nullptr) {
+            lane.load(side.gain, ga, gb);
+        } else {
+#pragma unroll
+            for (int e = 0; e < PER; ++e)
+                ga[e] = gb[e] = 1.0f;
+        }
+    }
+    float sa[PER], sb[PER];  // dgain of what the lane has seen
+    if constexpr (MODE == kHeadsGrad)
+#pragma unroll
+        for (int e = 0; e < PER; ++e)
+            sa[e] = sb[e] = 0.0f;
+
+    for (int64_t t = t0; t < t1; t += at_once) {
+        const int nt = (int)min((int64_t)at_once, t1 - t);
+        if (t != t0)
+            __syncthreads();
+        for (int i = tid; i < nt * half; i += kHeadsThreads) {
+            const int ti = (int)(((float)i + 0.5f) * per_half), p = i - ti * half;
+            const int64_t position = g.positions[t + ti];
+            if (p == 0)
+                padding[ti] = position < 0;
+            // in turns: the fraction is exact to the product's own rounding, 2^-52 of the turns
+            const double turns = (double)position * g.freqs[p] * 0.15915494309189533577;
+            float sine, cosine;
+            sincospif(2.0f * (float)(turns - __builtin_rint(turns)), &sine, &cosine);
+            angles[i] = make_float2(cosine * g.scale, sine * g.sign * g.scale);
+        }
+        if (half != 0)
+            __syncthreads();
+        for (int item = team; item < nt * nh; item += TEAMS) {
+            const int ti = (int)(((float)item + 0.5f) * per_head);
+            const int64_t token = t + ti, head = h0 + item - ti * nh;
+            if (half != 0 && padding[ti])
+                continue;
+            const float2 *cs = angles + ti * half;
+            float a[PER], b[PER];
+            lane.load(side.x + token * side.x_token + head * side.x_head, a, b);
+            if constexpr (MODE != kHeadsGrad) {
+                if constexpr (MODE == kHeadsNorm) {
+                    heads_normalise<LANES>(a, b, g.dim, per_dim, g.eps);
+#pragma unroll
+                    for (int e = 0; e < PER; ++e) {
+                        a[e] *= ga[e];
+                        b[e] *= gb[e];
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < PER; ++e)
+                    if (lane.rotates(e)) {
+                        const float2 c = cs[lane.angle(e)];
+                        const float u = a[e] * c.x - b[e] * c.y, v = b[e] * c.x + a[e] * c.y;
+                        a[e] = u;
+                        b[e] = v;
+                    }
+                lane.store(side.y + token * side.y_token + head * side.y_head, a, b);
+            } else {
+                float da[PER], db[PER];
+                lane.load(side.dy + token * side.dy_token + head * side.dy_head, da, db);
+                const float rstd = heads_normalise<LANES>(a, b, g.dim, per_dim, g.eps);
+                float dot = 0.0f;
+#pragma unroll
+                for (int e = 0; e < PER; ++e) {
+                    if (lane.rotates(e)) {
+                        const float2 c = cs[lane.angle(e)];
+                        const float u = da[e] * c.x - db[e] * c.y, v = db[e] * c.x + da[e] * c.y;
+                        da[e] = u;
+                        db[e] = v;
+                    }
+                    sa[e] = __builtin_fmaf(da[e], a[e], sa[e]);
+                    sb[e] = __builtin_fmaf(db[e], b[e], sb[e]);
+                    da[e] *= ga[e];
+                    db[e] *= gb[e];
+                    dot = __builtin_fmaf(da[e], a[e], __builtin_fmaf(db[e], b[e], dot));
+                }
+                dot = team_sum<LANES>(dot) * per_dim;
+#pragma unroll
+                for (int e = 0; e < PER; ++e) {
+                    a[e] = rstd * __builtin_fmaf(-a[e], dot, da[e]);
+                    b[e] = rstd * __builtin_fmaf(-b[e], dot, db[e]);
+                }
+                lane.store(side.y + token * side.y_token + head * side.y_head, a, b);
+            }
+        }
+    }
+    if (MODE == kHeadsGrad && g.partials != nullptr) {
+        // over the teams of a wave, then over the waves, in this order
+        constexpr int WAVES = kHeadsThreads / kWave;
+        float *sums = (float *)angles;
+        static_assert(WAVES * LANES * 2 * PER <= 2 * kHeadsAngles, "the angles' room");
+        const int wave = tid / kWave, l = tid & (kWave - 1);
+#pragma unroll
+        for (int e = 0; e < PER; ++e)
+#pragma unroll
+            for (int off = kWave / 2; off >= LANES; off >>= 1) {
+                sa[e] += __shfl_xor(sa[e], off, kWave);
+                sb[e] += __shfl_xor(sb[e], off, kWave);
+            }
+        __syncthreads();
+        if (l < LANES)
+#pragma unroll
+            for (int e = 0; e < PER; ++e) {
+                sums[(wave * 2 * PER + 2 * e) * LANES + l] = sa[e];
+                sums[(wave * 2 * PER + 2 * e + 1) * LANES + l] = sb[e];
+            }
+        __syncthreads();
+        if (tid < LANES)
+#pragma unroll
+            for (int e = 0; e < 2 * PER; ++e) {
+                float s = 0.0f;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w)
+                    s += sums[(w * 2 * PER + e) * LANES + l];
+                const int c = lane.column(e >> 1, e & 1);
+                if (c >= 0)
+                    g.partials[(int64_t)blockIdx.x * g.dim + c] = s;
+            }
+    }
+}
+
+// dgain: the workgroups' rows, 16 columns a workgroup, added in a fixed order
+__global__ __launch_bounds__(256) void heads_gain_kernel(const float *__restrict__ partials, int rows0, int rows1, int dim,
+                                                         float *dgain0, float *dgain1)
+{
+    __shared__ float red[16][17];
+    const bool second = blockIdx.y != 0;
+    float *out = second ? dgain1 : dgain0;
+    const int from = second ? rows0 : 0, to = second ? rows0 + rows1 : rows0;
+    const int c = blockIdx.x * 16 + (threadIdx.x & 15), r = threadIdx.x >> 4;
+    if (out == nullptr)
+        return;
+    float s = 0.0f;
+    if (c < dim)
+#pragma unroll 8
+        for (int i = from + r; i < to; i += 16)
+            s += partials[(int64_t)i * dim + c];
+    red[r][threadIdx.x & 15] = s;
+    __syncthreads();
+    if (r == 0 && c < dim) {
+#pragma unroll
+        for (int i = 1; i < 16; ++i)
+            s += red[i][threadIdx.x];
+        out[c] = s;
+    }
+}
+
+// ---- host side
+constexpr int kHeadsBlockHeads = 2048;  // (a workgroup divides its items by them in fp32)
+constexpr int kHeadsGradBlocks = 640;   // workgroups of the gradients, two and a half a CU
+
+// a row of dgain for each workgroup: a side has at most twice its share of them (a share rounded up), one more, and two for each
+// 2048 heads (at most 2^16); never more than heads
+int64_t heads_grad_bytes(int64_t tokens, int64_t heads, int64_t dim)
+{
+    return std::min<int64_t>(2 * kHeadsGradBlocks + 2 + 2 * (heads / kHeadsBlockHeads + 2), tokens * heads) * dim * 4;
+}
+
+static bool on_pieces(const void *p, int64_t token, int64_t head)
+{
+    return ((uintptr_t)p & 15) == 0 && token % 8 == 0 && head % 8 == 0;
+}
+
+static void heads_share(HeadsSide &s, int64_t tokens, int64_t items, int at_once)
+{
+    s.block_heads = (int)std::min<int64_t>({s.heads, items, kHeadsBlockHeads});
+    s.block_tokens = std::min<int64_t>(at_once, (items + s.block_heads - 1) / s.block_heads);
+    s.splits = (s.heads + s.block_heads - 1) / s.block_heads;
+    s.blocks = (int)(s.splits * ((tokens + s.block_tokens - 1) / s.block_tokens));
+}
+
+template <typename LANE, int LANES>
+static hipError_t launch_lanes(HeadsDev &g, int mode, int sides, hipStream_t s)
+{
+    constexpr int TEAMS = kHeadsThreads / LANES;
+    const int half = g.rot / 2;
+    const int64_t at_once = half != 0 ? std::min(kHeadsTokens, kHeadsAngles / half) : kHeadsTokens;
+    int64_t all = 0;
+    for (int i = 0; i < sides; ++i)
+        all += g.tokens * g.side[i].heads;
+    for (int i = 0; i < sides; ++i) {
+        const int64_t mine = g.tokens * g.side[i].heads;
+        if (mode == kHeadsGrad) {
+            const int64_t most = std::max<int64_t>(1, kHeadsGradBlocks * mine / all);
+            heads_share(g.side[i], g.tokens, std::max<int64_t>(TEAMS, (mine + most - 1) / most), 1 << 30);
+        } else {
+            heads_share(g.side[i], g.tokens, std::min<int64_t>(8 * TEAMS, std::max<int64_t>(TEAMS, mine / 1024)), at_once);
+        }
+    }
+    const dim3 grid((unsigned)(g.side[0].blocks + g.side[1].blocks)), block(kHeadsThreads);
+    switch (mode) {
+    case kHeadsRotary: hipLaunchKernelGGL((heads_kernel<LANE, LANES, kHeadsRotary>), grid, block, 0, s, g); break;
+    case kHeadsNorm: hipLaunchKernelGGL((heads_kernel<LANE, LANES, kHeadsNorm>), grid, block, 0, s, g); break;
+    default: hipLaunchKernelGGL((heads_kernel<LANE, LANES, kHeadsGrad>), grid, block, 0, s, g); break;
+    }
+    return hipGetLastError();
+}
+
+template <bool PAIRS>
+static hipError_t launch_layout(HeadsDev &g, int mode, int sides, bool pieces, hipStream_t s)
+{
+    if (!pieces)
+        return launch_lanes<HeadsScalar<PAIRS>, 64>(g, mode, sides, s);
+    const int lanes = (g.dim + 15) / 16;
+    if (lanes <= 1)
+        return launch_lanes<HeadsVector<PAIRS>, 1>(g, mode, sides, s);
+    if (lanes <= 2)
+        return launch_lanes<HeadsVector<PAIRS>, 2>(g, mode, sides, s);
+    if (lanes <= 4)
+        return launch_lanes<HeadsVector<PAIRS>, 4>(g, mode, sides, s);
+    if (lanes <= 8)
+        return launch_lanes<HeadsVector<PAIRS>, 8>(g, mode, sides, s);
+    if (lanes <= 16)
+        return launch_lanes<HeadsVector<PAIRS>, 16>(g, mode, sides, s);
+    return launch_lanes<HeadsVector<PAIRS>, 32>(g, mode, sides, s);
+}
+
+hipError_t launch_heads(const HeadsCall &c, int mode, hipStream_t s)
+{
+    HeadsDev g{};
+    g.tokens = c.tokens;
+    g.dim = c.dim;
+    g.rot = c.rot;
+    g.positions = c.positions;
+    g.freqs = c.freqs;
+    g.scale = c.scale;
+    g.eps = c.eps;
+    g.sign = c.transpose || mode == kHeadsGrad ? -1.0f : 1.0f;
+    g.partials = c.partials;
+    bool pieces = c.dim % 8 == 0 && c.rot % 16 == 0;
+    for (int i = 0; i < c.sides; ++i) {
+        const HeadsCallSide &f = c.side[i];
+        HeadsSide &t = g.side[i];
+        t.x = (const uint16_t *)f.x;
+        t.dy = (const uint16_t *)f.dy;
+        t.gain = (const uint16_t *)f.gain;
+        t.y = (uint16_t *)f.y;
+        t.heads = f.heads;
+        // a stride that no second token or head is reached by says nothing
+        auto stride = [](int64_t v, int64_t n) { return n > 1 ? v : 0; };
+        t.x_token = stride(f.x_token, c.tokens);
+        t.x_head = stride(f.x_head, f.heads);
+        t.dy_token = stride(f.dy_token, c.tokens);
+        t.dy_head = stride(f.dy_head, f.heads);
+        t.y_token = stride(f.y_token, c.tokens);
+        t.y_head = stride(f.y_head, f.heads);
+        pieces = pieces && on_pieces(t.x, t.x_token, t.x_head) && on_pieces(t.y, t.y_token, t.y_head) &&
+                 on_pieces(t.dy, t.dy_token, t.dy_head) && on_pieces(t.gain, 0, 0);
+    }
+    const hipError_t e = c.pairs ? launch_layout<true>(g, mode, c.sides, pieces, s) : launch_layout<false>(g, mode, c.sides, pieces, s);
+    if (e != hipSuccess || mode != kHeadsGrad || (c.side[0].dgain == nullptr && c.side[1].dgain == nullptr))
+        return e;
+    hipLaunchKernelGGL(heads_gain_kernel, dim3((unsigned)((c.dim + 15) / 16), (unsigned)c.sides), dim3(256), 0, s, g.partials,
+                       g.side[0].blocks, g.side[1].blocks, c.dim, c.side[0].dgain, c.side[1].dgain);
+    return hipGetLastError();
+}
+
+hipError_t launch_rotary(const HeadsCall &c, hipStream_t s) { return launch_heads(c, kHeadsRotary, s); }
+hipError_t launch_head_norm(const HeadsCall &c, hipStream_t s) { return launch_heads(c, kHeadsNorm, s); }
+hipError_t launch_head_norm_grad(const HeadsCall &c, hipStream_t s) { return launch_heads(c, kHeadsGrad, s); }
+
+}  // namespace tweo

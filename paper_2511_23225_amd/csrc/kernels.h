@@ -92,6 +92,32 @@ hipError_t launch_layernorm_bwd(const void *dy_bf16, const void *h_bf16, const v
                                 const void *dres_bf16, int64_t rows, int64_t cols, void *dx, float *dgamma, float *dbeta,
                                 void *workspace, hipStream_t s);
 
+// Rotation of heads by position, their norm with the rotation behind it, its gradients (heads.hip).  One or two sides (queries,
+// keys); strides in elements.
+struct HeadsCallSide {
+    const void *x, *dy, *gain;  // gain: bf16 [dim] or nullptr
+    void *y;                    // gradients: dx
+    int64_t x_token, x_head, dy_token, dy_head, y_token, y_head;
+    int heads;
+    float *dgain;
+};
+struct HeadsCall {
+    HeadsCallSide side[2];
+    int sides;
+    int64_t tokens;
+    int dim, rot;  // rot 0: no rotation, no positions
+    bool pairs, transpose;
+    const int64_t *positions;
+    const double *freqs;
+    float scale, eps;
+    float *partials;  // heads_grad_bytes, where a dgain is wanted, else nullptr
+};
+constexpr int kHeadsMaxDim = 512, kHeadsMaxHeads = 1 << 16;
+int64_t heads_grad_bytes(int64_t tokens, int64_t heads, int64_t dim);
+hipError_t launch_rotary(const HeadsCall &c, hipStream_t s);
+hipError_t launch_head_norm(const HeadsCall &c, hipStream_t s);
+hipError_t launch_head_norm_grad(const HeadsCall &c, hipStream_t s);
+
 // Gradient norm and AdamW over a table of tensors (optim.hip).
 enum OptimKind : uint32_t { kOptimParamF32 = 1, kOptimMaster = 2, kOptimGradF32 = 4 };
 constexpr int kOptimChunk = 1024, kOptimEntryBytes = 80;
