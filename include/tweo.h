@@ -59,7 +59,9 @@ enum {
     TWEO_OP_LAYERNORM_QUANTIZE = 5, /* M = rows; N, K unused (pass 1) */
     TWEO_OP_LAYERNORM_BWD = 6,      /* M = rows, N = cols; K unused (pass 1) */
     TWEO_OP_GRAD_SUMSQ = 7,         /* the same for every table (pass 1, 1, 1) */
-    TWEO_OP_HEAD_NORM_ROTARY_BWD = 8 /* M = tokens, N = heads of both groups, K = dim */
+    TWEO_OP_HEAD_NORM_ROTARY_BWD = 8, /* M = tokens, N = heads of both groups, K = dim */
+    TWEO_OP_FP8_GATED_FWD_BF16 = 9,   /* M, N = F, K */
+    TWEO_OP_FP8_GATED_BWD_BF16 = 10   /* M, N = F, K */
 };
 
 /* Bytes of device workspace the given operation can use for these sizes (a
@@ -768,6 +770,69 @@ typedef struct {
 } tweo_heads_grad;
 tweo_status tweo_head_norm_rotary_bwd(const tweo_heads_grad *groups, int count, int64_t tokens, int dim, float eps,
                                       const tweo_rotary_cfg *cfg, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Gated feed-forward, first half: both projections, the activation and the product in one kernel (FP8 operands, one
+ * scale each as everywhere).  The weight w [2F, K] holds the gate's rows 0 .. F - 1 and the up projection's rows F .. 2F - 1.
+ *   gu[m,n] = bf16( sum_k dec(xq[m,k]) dec(wq[n,k]) * (*sx_inv) * (*sw_inv) ),   n < 2F     (fp32 accumulate)
+ *   h[m,n]  = bf16( act(gu[m,n]) * gu[m,F+n] ),   n < F
+ * gu has the bits that tweo_fp8_linear_fwd gives for the weight (up to the order of its sums), and h is formed from the values as
+ * stored, whether they are kept or not: what the backward pass reads is what went into h.
+ *   act: TWEO_ACT_SILU, g * sigmoid(g); TWEO_ACT_GELU, the tanh form g/2 (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))).
+ *   A gate below -88 gives 0 (its true value is below 2^-120 of the up projection's); infinite ones what the formula does.
+ *   xq [M,K], wq [2F,K] codes, K % 16 == 0; h_bf16 [M,F], F % 8 == 0; gu_bf16 [M,2F] or NULL.
+ * Needs no workspace.  Errors: TWEO_ERR_INVALID_ARG (null, misaligned, an unknown act, an output that overlaps anything),
+ * TWEO_ERR_UNSUPPORTED (shape rules).
+ */
+enum { TWEO_ACT_SILU = 0, TWEO_ACT_GELU = 1 };
+tweo_status tweo_fp8_gated_fwd(const uint8_t *xq, const float *sx_inv, const uint8_t *wq, const float *sw_inv, int64_t M,
+                               int64_t F, int64_t K, int act, void *h_bf16, void *gu_bf16, void *stream);
+
+/*
+ * The same from bf16 operands: amax and cast of x [M,K] and w [2F,K] (with transposed copies, kept in `saved` as by
+ * tweo_fp8_linear_fwd_bf16 of N = 2F), then the kernel above.  state_x, state_w: NULL for current scaling, or the
+ * two tensors' delayed-scaling states, both and distinct (tweo_fp8_linear_fwd_bf16_delayed; bootstrap != 0 on the first call).
+ * M % 16 == 0, K % 16 == 0, F % 8 == 0.  workspace: current scaling, tweo_workspace_bytes(TWEO_OP_FP8_GATED_FWD_BF16, M, F, K),
+ * 16-byte aligned, else TWEO_ERR_WORKSPACE; not used under delayed scaling.
+ */
+tweo_status tweo_fp8_gated_fwd_bf16(const void *x_bf16, const void *w_bf16, int64_t M, int64_t F, int64_t K, int act,
+                                    void *h_bf16, void *gu_bf16, const tweo_fp8_saved *saved, void *state_x, void *state_w,
+                                    int bootstrap, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Its backward pass from dh [M,F] and the stored gu [M,2F]:
+ *   dg = bf16( dh * u * act'(g) ),  du = bf16( dh * act(g) )      (fp32, rounded once; never stored)
+ *   (dg | du) [M,2F] cast with one scale into dguq [M,2F] and dguqT [2F,M], E4M3 or (dy_e5m2 = 1) E5M2
+ *   dx[m,k] = bf16( (dguq wq)[m,k] * scales ),  dw[n,k] = bf16( (dguq^T xq)[n,k] * scales ),  dw [2F,K]
+ * the two products as tweo_fp8_linear_bwd of N = 2F, on what the forward pass left in `saved`.  saved->scalars words 6-8
+ * receive amax, scale and inverse.  state_dgu: NULL for current scaling (the gradients are formed twice, for their maximum
+ * and for the cast), or a delayed-scaling state (once), bootstrap != 0 on its first call.
+ *   dx_bf16 or dw_bf16 may be NULL to skip that product.  Shapes as the forward.
+ *   workspace: tweo_workspace_bytes(TWEO_OP_FP8_GATED_BWD_BF16, M, F, K), 16-byte aligned; 4 KB at least (with less than asked
+ *   for a product may run in fewer runs, as in tweo_fp8_linear_bwd), else TWEO_ERR_WORKSPACE.
+ * Errors: as tweo_fp8_linear_bwd_bf16, an unknown act, outputs that overlap anything.
+ */
+tweo_status tweo_fp8_gated_bwd_bf16(const void *dh_bf16, const void *gu_bf16, const tweo_fp8_saved *saved, int64_t M,
+                                    int64_t F, int64_t K, int act, int dy_e5m2, void *state_dgu, int bootstrap, uint8_t *dguq,
+                                    uint8_t *dguqT, void *dx_bf16, void *dw_bf16, void *workspace, size_t workspace_bytes,
+                                    void *stream);
+
+/*
+ * The forward half on INT8 operands, for inference (Sec. 4.4's granularities, as tweo_w8a8_linear_scaled):
+ *   g, u    = (fp32( sum_k xq[m,k] wq[n,k] ) * x_step[m or 0]) * w_step[n or 0]      (exact int32 accumulation)
+ *   h[m,n]  = bf16( act(g) * u )                                                     (fp32, one rounding)
+ *   xq [M,K], wq [2F,K] int8; w_step: fp32 [2F] when w_step_per_channel = 1, [1] when 0; x_step [M] or [1] likewise.
+ *   K % 16 == 0, F % 8 == 0; any M: one token and prompts.  Needs no workspace.
+ * tweo_w8a8_gated_i8out: hq [M,F] int8 = clamp( rne( act(g) * u * inv_step_h ), -127, 127 ) in its place, NaN -> 0: the down
+ * projection's input under a static step, inv_step_h = 127 / s.
+ * Errors as tweo_w8a8_linear_scaled, an unknown act, an output that overlaps anything, a NaN inv_step_h.
+ */
+tweo_status tweo_w8a8_gated(const int8_t *xq, const int8_t *wq, int64_t M, int64_t F, int64_t K, const float *x_step,
+                            int x_step_per_token, const float *w_step, int w_step_per_channel, int act, void *h_bf16,
+                            void *stream);
+tweo_status tweo_w8a8_gated_i8out(const int8_t *xq, const int8_t *wq, int64_t M, int64_t F, int64_t K, const float *x_step,
+                                  int x_step_per_token, const float *w_step, int w_step_per_channel, int act,
+                                  float inv_step_h, int8_t *hq, void *stream);
 
 /*
  * Tuning hook for benchmarks and tests: forces the GEMM kernel variant.

@@ -57,17 +57,18 @@ def head_norm_rotary_bwd(dy, x, gain, eps, positions=None, freqs=None, layout="h
 GELU = np.sqrt(2 / np.pi), 0.044715
 
 
+def gate_argument(g, act):
+    """z and dz/dg of act(g) = g * sigmoid(z): g itself, or, as 1 + tanh(y) = 2 sigmoid(2y), twice the tanh form's argument."""
+    return (g, np.ones_like(g)) if act == "silu" else (2 * GELU[0] * (g + GELU[1] * g ** 3), 2 * GELU[0] * (1 + 3 * GELU[1] * g * g))
+
+
 def activation(g, act):
     with np.errstate(all="ignore"):
-        if act == "silu":
-            return g / (1 + np.exp(-g))
-        return 0.5 * g * (1 + np.tanh(GELU[0] * (g + GELU[1] * g ** 3)))
+        return g / (1 + np.exp(-gate_argument(g, act)[0]))
 
 
 def activation_slope(g, act):
     with np.errstate(all="ignore"):
-        if act == "silu":
-            p = 1 / (1 + np.exp(-g))
-            return p * (1 + g * (1 - p))
-        t = np.tanh(GELU[0] * (g + GELU[1] * g ** 3))
-        return 0.5 * (1 + t) + 0.5 * g * (1 - t * t) * GELU[0] * (1 + 3 * GELU[1] * g * g)
+        z, dz = gate_argument(g, act)
+        p, rest = 1 / (1 + np.exp(-z)), 1 / (1 + np.exp(z))
+        return p + np.where(p * rest == 0, 0.0, g * p * rest * dz)

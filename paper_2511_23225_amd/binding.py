@@ -16,7 +16,7 @@ LIB_PATH = os.path.join(_PKG, "libtweo_hip.so")
 TWEO_OK, TWEO_ERR_INVALID_ARG, TWEO_ERR_UNSUPPORTED, TWEO_ERR_WORKSPACE, TWEO_ERR_HIP = range(5)
 (TWEO_OP_FP8_LINEAR_FWD, TWEO_OP_FP8_LINEAR_BWD, TWEO_OP_W8A8_LINEAR, TWEO_OP_FP8_LINEAR_FWD_BF16,
  TWEO_OP_FP8_LINEAR_BWD_BF16, TWEO_OP_LAYERNORM_QUANTIZE, TWEO_OP_LAYERNORM_BWD, TWEO_OP_GRAD_SUMSQ,
- TWEO_OP_HEAD_NORM_ROTARY_BWD) = range(9)
+ TWEO_OP_HEAD_NORM_ROTARY_BWD, TWEO_OP_FP8_GATED_FWD_BF16, TWEO_OP_FP8_GATED_BWD_BF16) = range(11)
 
 EXPORTS = ("tweo_workspace_bytes", "tweo_status_string", "tweo_amax", "tweo_quantize_e4m3",
            "tweo_fp8_linear_fwd", "tweo_fp8_linear_bwd", "tweo_quantize_i8", "tweo_w8a8_linear",
@@ -32,7 +32,8 @@ EXPORTS = ("tweo_workspace_bytes", "tweo_status_string", "tweo_amax", "tweo_quan
            "tweo_fp8_linear_fwd_bf16_delayed", "tweo_fp8_linear_bwd_bf16_delayed",
            "tweo_layernorm_fwd", "tweo_layernorm_bwd", "tweo_optim_table_bytes", "tweo_optim_plan_init",
            "tweo_grad_sumsq", "tweo_adamw_step", "tweo_rotary", "tweo_rotary_freqs", "tweo_head_norm_rotary_fwd",
-           "tweo_head_norm_rotary_bwd")
+           "tweo_head_norm_rotary_bwd", "tweo_fp8_gated_fwd", "tweo_fp8_gated_fwd_bf16", "tweo_fp8_gated_bwd_bf16",
+           "tweo_w8a8_gated", "tweo_w8a8_gated_i8out")
 
 
 class TweoError(RuntimeError):
@@ -159,6 +160,12 @@ def load():
     L.tweo_rotary_freqs.argtypes = [ctypes.POINTER(RotaryFreqCfg), ctypes.c_int, vp]
     L.tweo_head_norm_rotary_fwd.argtypes = [vp, ctypes.c_int, i64, ctypes.c_int, f32, vp, vp]
     L.tweo_head_norm_rotary_bwd.argtypes = [vp, ctypes.c_int, i64, ctypes.c_int, f32, vp, vp, sz, vp]
+    c_int = ctypes.c_int
+    L.tweo_fp8_gated_fwd.argtypes = [vp, vp, vp, vp, i64, i64, i64, c_int, vp, vp, vp]
+    L.tweo_fp8_gated_fwd_bf16.argtypes = [vp, vp, i64, i64, i64, c_int, vp, vp, ctypes.POINTER(Fp8Saved), vp, vp, c_int, vp, sz, vp]
+    L.tweo_fp8_gated_bwd_bf16.argtypes = [vp, vp, ctypes.POINTER(Fp8Saved), i64, i64, i64, c_int, c_int, vp, c_int, vp, vp, vp, vp, vp, sz, vp]
+    L.tweo_w8a8_gated.argtypes = [vp, vp, i64, i64, i64, vp, c_int, vp, c_int, c_int, vp, vp]
+    L.tweo_w8a8_gated_i8out.argtypes = [vp, vp, i64, i64, i64, vp, c_int, vp, c_int, c_int, f32, vp, vp]
     for name in EXPORTS:
         if name not in ("tweo_workspace_bytes", "tweo_status_string", "tweo_delayed_state_bytes",
                         "tweo_static_scratch_bytes", "tweo_optim_table_bytes"):
@@ -737,3 +744,116 @@ def tweo_head_norm_rotary_bwd(groups, positions=None, freqs=None, layout="halves
         row.dx_token, row.dx_head, _ = dx.stride()
     wp, wb = _scratch(dev, workspace, "workspace")
     _check(load().tweo_head_norm_rotary_bwd(rows, len(groups), shape[0], shape[2], eps, cfg, wp, wb, _stream()), "tweo_head_norm_rotary_bwd")
+
+
+ACTS = {"silu": 0, "gelu": 1}  # TWEO_ACT_SILU, TWEO_ACT_GELU
+
+
+def _act(act):
+    if act not in ACTS:
+        raise ValueError("act: silu or gelu is needed, got %r" % (act,))
+    return ACTS[act]
+
+
+def _gated_shape(x, w, names):
+    """M, F, K of [M, K] and [2F, K]."""
+    if x.dim() != 2 or w.dim() != 2 or x.shape[1] != w.shape[1] or w.shape[0] % 2 != 0:
+        raise ValueError("%s, %s: [M, K] and [2F, K] are needed, got %s and %s" % (names + (tuple(x.shape), tuple(w.shape))))
+    return x.shape[0], w.shape[0] // 2, x.shape[1]
+
+
+@functools.lru_cache(maxsize=1)
+def _bytes_types():
+    import torch
+    return torch.uint8, torch.int8
+
+
+def _scalar(device, t, name):
+    if t.dtype is not _types()[1] or t.numel() < 1 or t.get_device() != device:
+        raise ValueError("%s: one torch.float32 on cuda:%d, the current device, is needed, got %s on %s" % (name, device, t.dtype, t.device))
+
+
+def _state(device, t, name):
+    """A delayed-scaling state."""
+    if t is not None and (t.nbytes < 4 * DELAYED_STATE_WORDS or not t.is_contiguous() or t.get_device() != device):
+        raise ValueError("%s: %d contiguous bytes on cuda:%d, the current device, are needed, got %d on %s" %
+                         (name, 4 * DELAYED_STATE_WORDS, device, t.nbytes, t.device))
+
+
+_XQ, _WQ, _HB, _GU, _XB, _WB, _DGUQ, _DGUQT, _HQ = (("xq",), ("wq",), ("h_bf16",), ("gu_bf16",), ("x_bf16",), ("w_bf16",), ("dguq",), ("dguqT",), ("hq",))
+
+
+def tweo_fp8_gated_fwd(xq, sx_inv, wq, sw_inv, h_bf16, gu_bf16=None, act="silu"):
+    """wq [2F, K]: the gate's rows, then the up projection's.  gu_bf16 [M, 2F]: both projections, for the backward pass."""
+    M, F, K = _gated_shape(xq, wq, ("xq", "wq"))
+    dev, u8, bf16 = _device(), _bytes_types()[0], _types()[0]
+    _same(dev, (M, K), u8, (xq,), _XQ)
+    _same(dev, (2 * F, K), u8, (wq,), _WQ)
+    _same(dev, (M, F), bf16, (h_bf16,), _HB)
+    _same(dev, (M, 2 * F), bf16, (gu_bf16,), _GU)
+    _scalar(dev, sx_inv, "sx_inv")
+    _scalar(dev, sw_inv, "sw_inv")
+    _check(load().tweo_fp8_gated_fwd(_ptr(xq), _ptr(sx_inv), _ptr(wq), _ptr(sw_inv), M, F, K, _act(act), _ptr(h_bf16), _ptr(gu_bf16), _stream()),
+           "tweo_fp8_gated_fwd")
+
+
+def tweo_fp8_gated_fwd_bf16(x_bf16, w_bf16, h_bf16, gu_bf16, saved, act="silu", state_x=None, state_w=None, bootstrap=False, workspace=None):
+    """saved: make_saved of xq [M, K], wq [2F, K] and their transposes.  gu_bf16 may be None.  state_x and state_w: delayed scaling."""
+    M, F, K = _gated_shape(x_bf16, w_bf16, ("x_bf16", "w_bf16"))
+    dev, bf16 = _device(), _types()[0]
+    _same(dev, (M, K), bf16, (x_bf16,), _XB)
+    _same(dev, (2 * F, K), bf16, (w_bf16,), _WB)
+    _same(dev, (M, F), bf16, (h_bf16,), _HB)
+    _same(dev, (M, 2 * F), bf16, (gu_bf16,), _GU)
+    _state(dev, state_x, "state_x")
+    _state(dev, state_w, "state_w")
+    wp, wb = _scratch(dev, workspace, "workspace")
+    _check(load().tweo_fp8_gated_fwd_bf16(_ptr(x_bf16), _ptr(w_bf16), M, F, K, _act(act), _ptr(h_bf16), _ptr(gu_bf16), ctypes.byref(saved),
+                                          _ptr(state_x), _ptr(state_w), 1 if bootstrap else 0, wp, wb, _stream()), "tweo_fp8_gated_fwd_bf16")
+
+
+def tweo_fp8_gated_bwd_bf16(dh_bf16, gu_bf16, saved, K, dguq, dguqT, dx_bf16=None, dw_bf16=None, act="silu", dy_e5m2=False, state_dgu=None,
+                            bootstrap=False, workspace=None):
+    """dguq [M, 2F], dguqT [2F, M]: the codes of both projections' gradients.  dx_bf16 [M, K], dw_bf16 [2F, K] or None."""
+    if dh_bf16.dim() != 2:
+        raise ValueError("dh_bf16: two dimensions are needed")
+    M, F = dh_bf16.shape
+    dev, u8, bf16 = _device(), _bytes_types()[0], _types()[0]
+    _same(dev, (M, F), bf16, (dh_bf16,), ("dh_bf16",))
+    _same(dev, (M, 2 * F), bf16, (gu_bf16,), _GU)
+    _same(dev, (M, 2 * F), u8, (dguq,), _DGUQ)
+    _same(dev, (2 * F, M), u8, (dguqT,), _DGUQT)
+    _same(dev, (M, K), bf16, (dx_bf16,), ("dx_bf16",))
+    _same(dev, (2 * F, K), bf16, (dw_bf16,), ("dw_bf16",))
+    _state(dev, state_dgu, "state_dgu")
+    wp, wb = _scratch(dev, workspace, "workspace")
+    _check(load().tweo_fp8_gated_bwd_bf16(_ptr(dh_bf16), _ptr(gu_bf16), ctypes.byref(saved), M, F, K, _act(act), 1 if dy_e5m2 else 0, _ptr(state_dgu),
+                                          1 if bootstrap else 0, _ptr(dguq), _ptr(dguqT), _ptr(dx_bf16), _ptr(dw_bf16), wp, wb, _stream()),
+           "tweo_fp8_gated_bwd_bf16")
+
+
+def _w8a8_gated(xq, wq, x_step, w_step, out, dtype, name):
+    M, F, K = _gated_shape(xq, wq, ("xq", "wq"))
+    dev, i8, f32 = _device(), _bytes_types()[1], _types()[1]
+    _same(dev, (M, K), i8, (xq,), _XQ)
+    _same(dev, (2 * F, K), i8, (wq,), _WQ)
+    _same(dev, (M, F), dtype, (out,), name)
+    for t, n, what in ((x_step, M, "x_step"), (w_step, 2 * F, "w_step")):
+        if t.numel() not in (1, n) or t.dtype is not f32 or not t.is_contiguous() or t.get_device() != dev:
+            raise ValueError("%s: 1 or %d contiguous torch.float32 on cuda:%d, the current device, are needed, got %d of %s on %s" %
+                             (what, n, dev, t.numel(), t.dtype, t.device))
+    return M, F, K
+
+
+def tweo_w8a8_gated(xq, wq, x_step, w_step, h_bf16, act="silu"):
+    """wq [2F, K]: the gate's rows, then the up projection's.  x_step holds M steps (per token) or 1; w_step 2F (per channel) or 1."""
+    M, F, K = _w8a8_gated(xq, wq, x_step, w_step, h_bf16, _types()[0], _HB)
+    _check(load().tweo_w8a8_gated(_ptr(xq), _ptr(wq), M, F, K, _ptr(x_step), 1 if x_step.numel() > 1 else 0, _ptr(w_step),
+                                  1 if w_step.numel() > 1 else 0, _act(act), _ptr(h_bf16), _stream()), "tweo_w8a8_gated")
+
+
+def tweo_w8a8_gated_i8out(xq, wq, x_step, w_step, inv_step_h, hq, act="silu"):
+    """The same with an INT8 result under the static step 127 / inv_step_h, the input of the down projection."""
+    M, F, K = _w8a8_gated(xq, wq, x_step, w_step, hq, _bytes_types()[1], _HQ)
+    _check(load().tweo_w8a8_gated_i8out(_ptr(xq), _ptr(wq), M, F, K, _ptr(x_step), 1 if x_step.numel() > 1 else 0, _ptr(w_step),
+                                        1 if w_step.numel() > 1 else 0, _act(act), float(inv_step_h), _ptr(hq), _stream()), "tweo_w8a8_gated_i8out")

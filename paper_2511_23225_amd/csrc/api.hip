@@ -13,6 +13,7 @@ using namespace tweo;
 namespace {
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 inline bool aligned8(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
 inline size_t round256(size_t b) { return b == 0 ? 256 : (b + 255) / 256 * 256; }
 inline tweo_status hip_status(hipError_t e) { return e == hipSuccess ? TWEO_OK : TWEO_ERR_HIP; }
@@ -137,6 +138,10 @@ size_t tweo_workspace_bytes(int op, int64_t M, int64_t N, int64_t K)
     case TWEO_OP_W8A8_LINEAR:
         return 256 + round256(std::max(stream_k_candidate(M, N, K) ? stream_k_workspace_bytes() : (size_t)0,
                                        i8_gemm_ksplit_bytes(M, N, K)));
+    case TWEO_OP_FP8_GATED_FWD_BF16:
+        return kAmaxScratchBytes;
+    case TWEO_OP_FP8_GATED_BWD_BF16:  // M, F, K: a linear of 2F columns
+        return kAmaxScratchBytes + tweo_workspace_bytes(TWEO_OP_FP8_LINEAR_BWD, M, std::min(N, kMaxCols) * 2, K);
     case TWEO_OP_HEAD_NORM_ROTARY_BWD:  // M tokens, N heads, K dim; sizes that no call takes: as those of the largest it takes
         return round256((size_t)heads_grad_bytes(std::min(M, kMaxDim), std::min<int64_t>(N, 2 * kHeadsMaxHeads),
                                                  std::min<int64_t>(K, kHeadsMaxDim)));
@@ -1274,6 +1279,215 @@ tweo_status tweo_fp8_linear_bwd_bf16_inject(const void *dy_bf16, const void *a_b
     return fp8_linear_bwd_impl(dyq, dyqT, sc + 8, saved->wqT, sc + 5, saved->xqT, sc + 2, M, N, K, dx_bf16, dw_bf16,
                                (uint8_t *)workspace + kAmaxScratchBytes, workspace_bytes - kAmaxScratchBytes, stream,
                                dy_e5m2 != 0);
+}
+
+namespace {
+static_assert(kGatedPartials * sizeof(uint32_t) <= kAmaxScratchBytes, "the head of the workspace holds the maxima");
+
+bool act_ok(int act) { return act == TWEO_ACT_SILU || act == TWEO_ACT_GELU; }
+
+// sizes of the gated feed-forward's two products
+tweo_status check_gated(int64_t M, int64_t F, int64_t K, int act)
+{
+    if (M <= 0 || F <= 0 || K <= 0 || !act_ok(act))
+        return TWEO_ERR_INVALID_ARG;
+    return F <= kMaxCols && dims_ok(M, 2 * F, K) && K % 16 == 0 && F % 8 == 0 ? TWEO_OK : TWEO_ERR_UNSUPPORTED;
+}
+
+hipError_t fp8_gated(const uint8_t *xq, const float *sx_inv, const uint8_t *wq, const float *sw_inv, int64_t M, int64_t F,
+                     int64_t K, int act, void *h_bf16, void *gu_bf16, hipStream_t s)
+{
+    GemmArgs a{};
+    a.A = xq;
+    a.B = wq;
+    a.M = M;
+    a.N = F;
+    a.K = K;
+    a.s0 = sx_inv;
+    a.s1 = sw_inv;
+    a.out = h_bf16;
+    return launch_fp8_gated(a, act == TWEO_ACT_GELU, gu_bf16, s);
+}
+
+tweo_status w8a8_gated(const int8_t *xq, const int8_t *wq, int64_t M, int64_t F, int64_t K, const float *x_step,
+                       int x_step_per_token, const float *w_step, int w_step_per_channel, int act, void *h, bool out_i8,
+                       float out_inv_step, void *stream)
+{
+    if (!xq || !wq || !x_step || !w_step || !h || !aligned16(xq) || !aligned16(wq) || !aligned16(h) || !aligned4(x_step) ||
+        !aligned4(w_step) || (x_step_per_token != 0 && x_step_per_token != 1) ||
+        (w_step_per_channel != 0 && w_step_per_channel != 1) || !(out_inv_step == out_inv_step))
+        return TWEO_ERR_INVALID_ARG;
+    const tweo_status st = check_gated(M, F, K, act);
+    if (st != TWEO_OK)
+        return st;
+    Ranges all;
+    all.add(h, (size_t)(M * F) * (out_i8 ? 1 : 2), true);
+    all.add(xq, (size_t)(M * K), false);
+    all.add(wq, (size_t)(2 * F * K), false);
+    all.add(x_step, 4 * (size_t)(x_step_per_token ? M : 1), false);
+    all.add(w_step, 4 * (size_t)(w_step_per_channel ? 2 * F : 1), false);
+    if (all.clash())
+        return TWEO_ERR_INVALID_ARG;
+    GemmArgs a{};
+    a.A = (const uint8_t *)xq;
+    a.B = (const uint8_t *)wq;
+    a.M = M;
+    a.N = F;
+    a.K = K;
+    a.alpha = 1.0f;
+    a.out = h;
+    a.row_step = x_step;
+    a.row_step_stride = x_step_per_token;
+    a.col_step = w_step;
+    a.col_step_stride = w_step_per_channel;
+    a.out_i8 = out_i8;
+    a.out_inv_step = out_inv_step;
+    return hip_status(launch_i8_gated(a, act == TWEO_ACT_GELU, (hipStream_t)stream));
+}
+}  // namespace
+
+tweo_status tweo_fp8_gated_fwd(const uint8_t *xq, const float *sx_inv, const uint8_t *wq, const float *sw_inv, int64_t M,
+                               int64_t F, int64_t K, int act, void *h_bf16, void *gu_bf16, void *stream)
+{
+    if (!xq || !sx_inv || !wq || !sw_inv || !h_bf16 || !aligned16(xq) || !aligned16(wq) || !aligned16(h_bf16) ||
+        !aligned4(sx_inv) || !aligned4(sw_inv) || (gu_bf16 && !aligned16(gu_bf16)))
+        return TWEO_ERR_INVALID_ARG;
+    const tweo_status st = check_gated(M, F, K, act);
+    if (st != TWEO_OK)
+        return st;
+    Ranges all;
+    all.add(h_bf16, 2 * (size_t)(M * F), true);
+    all.add(gu_bf16, 4 * (size_t)(M * F), true);
+    all.add(xq, (size_t)(M * K), false);
+    all.add(wq, (size_t)(2 * F * K), false);
+    all.add(sx_inv, 4, false);
+    all.add(sw_inv, 4, false);
+    if (all.clash())
+        return TWEO_ERR_INVALID_ARG;
+    return hip_status(fp8_gated(xq, sx_inv, wq, sw_inv, M, F, K, act, h_bf16, gu_bf16, (hipStream_t)stream));
+}
+
+tweo_status tweo_fp8_gated_fwd_bf16(const void *x_bf16, const void *w_bf16, int64_t M, int64_t F, int64_t K, int act,
+                                    void *h_bf16, void *gu_bf16, const tweo_fp8_saved *saved, void *state_x, void *state_w,
+                                    int bootstrap, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!x_bf16 || !w_bf16 || !h_bf16 || !saved || !saved->xq || !saved->xqT || !saved->wq || !saved->wqT || !saved->scalars ||
+        !aligned16(x_bf16) || !aligned16(w_bf16) || !aligned16(h_bf16) || (gu_bf16 && !aligned16(gu_bf16)) ||
+        !aligned16(saved->xq) || !aligned16(saved->xqT) || !aligned16(saved->wq) || !aligned16(saved->wqT) ||
+        !aligned16(saved->scalars) || !state_x != !state_w || (state_x && (state_x == state_w || !aligned16(state_x) || !aligned16(state_w))))
+        return TWEO_ERR_INVALID_ARG;
+    const tweo_status st = check_gated(M, F, K, act);
+    if (st != TWEO_OK)
+        return st;
+    if (M % 16 != 0)
+        return TWEO_ERR_UNSUPPORTED;
+    if (!state_x && (!workspace || !aligned16(workspace) || workspace_bytes < kAmaxScratchBytes))
+        return TWEO_ERR_WORKSPACE;
+    const size_t x = (size_t)(M * K), w = (size_t)(2 * F * K);
+    Range r[13];
+    size_t n = 0;
+    auto add = [&](const void *p, size_t bytes, bool written) {
+        if (p)
+            r[n++] = {(uintptr_t)p, (uintptr_t)p + bytes, written};
+    };
+    add(x_bf16, 2 * x, false);
+    add(w_bf16, 2 * w, false);
+    add(saved->xq, x, true);
+    add(saved->xqT, x, true);
+    add(saved->wq, w, true);
+    add(saved->wqT, w, true);
+    add(saved->scalars, 64, true);
+    add(h_bf16, 2 * (size_t)(M * F), true);
+    add(gu_bf16, 4 * (size_t)(M * F), true);
+    add(state_x, tweo_delayed_state_bytes(), true);
+    add(state_w, tweo_delayed_state_bytes(), true);
+    add(state_x ? nullptr : workspace, kAmaxScratchBytes, true);
+    if (ranges_clash(r, n))
+        return TWEO_ERR_INVALID_ARG;
+    hipStream_t s = (hipStream_t)stream;
+    float *sc = saved->scalars;
+    hipError_t e;
+    if (state_x) {
+        e = launch_quantize2_e4m3_delayed(x_bf16, M, K, state_x, saved->xq, saved->xqT, sc + 0, w_bf16, 2 * F, K, state_w,
+                                          saved->wq, saved->wqT, sc + 3, bootstrap != 0, s);
+        if (e == hipSuccess && !bootstrap)
+            e = launch_delayed_update2(DelayedUpdate2{(uint32_t *)state_x, sc, (uint32_t *)state_w, sc + 3}, s);
+    } else if (fused_cast_applies(M, K, 2 * F, K, s)) {
+        e = launch_amax_cast_fused(x_bf16, M, K, sc + 0, saved->xq, saved->xqT, sc + 1, sc + 2, w_bf16, 2 * F, K, sc + 3,
+                                   saved->wq, saved->wqT, sc + 4, sc + 5, false, true, workspace, s);
+    } else {
+        uint32_t *px = (uint32_t *)workspace, *pw = px + kAmaxPartialsMax;
+        int nx = 0, nw = 0;
+        e = launch_amax2_partials(x_bf16, M * K, px, &nx, w_bf16, 2 * F * K, pw, &nw, s);
+        if (e == hipSuccess)
+            e = launch_quantize2_e4m3(x_bf16, M, K, sc + 0, saved->xq, saved->xqT, sc + 1, sc + 2, w_bf16, 2 * F, K, sc + 3,
+                                      saved->wq, saved->wqT, sc + 4, sc + 5, s, px, nx, pw, nw);
+    }
+    if (e == hipSuccess)
+        e = fp8_gated(saved->xq, sc + 2, saved->wq, sc + 5, M, F, K, act, h_bf16, gu_bf16, s);
+    return hip_status(e);
+}
+
+tweo_status tweo_fp8_gated_bwd_bf16(const void *dh_bf16, const void *gu_bf16, const tweo_fp8_saved *saved, int64_t M,
+                                    int64_t F, int64_t K, int act, int dy_e5m2, void *state_dgu, int bootstrap, uint8_t *dguq,
+                                    uint8_t *dguqT, void *dx_bf16, void *dw_bf16, void *workspace, size_t workspace_bytes,
+                                    void *stream)
+{
+    if (!dh_bf16 || !gu_bf16 || !saved || !saved->xqT || !saved->wqT || !saved->scalars || !dguq || !dguqT ||
+        !aligned16(dh_bf16) || !aligned16(gu_bf16) || !aligned16(dguq) || !aligned16(dguqT) || !aligned16(saved->xqT) ||
+        !aligned16(saved->wqT) || !aligned16(saved->scalars) || (dx_bf16 && !aligned16(dx_bf16)) ||
+        (dw_bf16 && !aligned16(dw_bf16)) || (dy_e5m2 != 0 && dy_e5m2 != 1) || (state_dgu && !aligned16(state_dgu)))
+        return TWEO_ERR_INVALID_ARG;
+    const tweo_status st = check_gated(M, F, K, act);
+    if (st != TWEO_OK)
+        return st;
+    if (M % 16 != 0)
+        return TWEO_ERR_UNSUPPORTED;
+    if (!workspace || !aligned16(workspace) || workspace_bytes < kAmaxScratchBytes)
+        return TWEO_ERR_WORKSPACE;
+    Range r[12];
+    size_t n = 0;
+    auto add = [&](const void *p, size_t bytes, bool written) {
+        if (p)
+            r[n++] = {(uintptr_t)p, (uintptr_t)p + bytes, written};
+    };
+    const size_t mf = (size_t)(M * F), x = (size_t)(M * K), w = (size_t)(2 * F * K);
+    add(dh_bf16, 2 * mf, false);
+    add(gu_bf16, 4 * mf, false);
+    add(saved->xqT, x, false);
+    add(saved->wqT, w, false);
+    add(saved->scalars, 64, true);
+    add(dguq, 2 * mf, true);
+    add(dguqT, 2 * mf, true);
+    add(dx_bf16, 2 * x, true);
+    add(dw_bf16, 2 * w, true);
+    add(state_dgu, tweo_delayed_state_bytes(), true);
+    add(workspace, std::min(workspace_bytes, tweo_workspace_bytes(TWEO_OP_FP8_GATED_BWD_BF16, M, F, K)), true);
+    if (ranges_clash(r, n))
+        return TWEO_ERR_INVALID_ARG;
+    float *sc = saved->scalars;
+    const GatedGradCall c{dh_bf16, gu_bf16, M, F, act == TWEO_ACT_GELU, dy_e5m2 != 0, dguq, dguqT, sc + 6, (uint32_t *)workspace,
+                          state_dgu, bootstrap != 0};
+    if (launch_gated_grad(c, (hipStream_t)stream) != hipSuccess)
+        return TWEO_ERR_HIP;
+    if (!dx_bf16 && !dw_bf16)
+        return TWEO_OK;
+    return fp8_linear_bwd_impl(dguq, dguqT, sc + 8, saved->wqT, sc + 5, saved->xqT, sc + 2, M, 2 * F, K, dx_bf16, dw_bf16,
+                               (uint8_t *)workspace + kAmaxScratchBytes, workspace_bytes - kAmaxScratchBytes, stream, dy_e5m2 != 0);
+}
+
+tweo_status tweo_w8a8_gated(const int8_t *xq, const int8_t *wq, int64_t M, int64_t F, int64_t K, const float *x_step,
+                            int x_step_per_token, const float *w_step, int w_step_per_channel, int act, void *h_bf16,
+                            void *stream)
+{
+    return w8a8_gated(xq, wq, M, F, K, x_step, x_step_per_token, w_step, w_step_per_channel, act, h_bf16, false, 0.0f, stream);
+}
+
+tweo_status tweo_w8a8_gated_i8out(const int8_t *xq, const int8_t *wq, int64_t M, int64_t F, int64_t K, const float *x_step,
+                                  int x_step_per_token, const float *w_step, int w_step_per_channel, int act,
+                                  float inv_step_h, int8_t *hq, void *stream)
+{
+    return w8a8_gated(xq, wq, M, F, K, x_step, x_step_per_token, w_step, w_step_per_channel, act, hq, true, inv_step_h, stream);
 }
 
 }  // extern "C"

@@ -19,6 +19,7 @@
 #include <utility>
 #include "gemm_common.h"
 #include "gemm_epilogue.h"
+#include "gemm_gated.h"
 #include "finish.h"
 
 namespace tweo {
@@ -72,9 +73,9 @@ __device__ __forceinline__ void ring_finish(const float *partials, const RingFin
 
 // KSPLIT: the grid is g.ksplit runs of the tile grid, run r multiplies its share of the stages and leaves fp32
 // (INT8: int32) sums in g.ksplit_out.  RAGGED: K may be no multiple of 128 (one of 16).  block: the workgroup's
-// number in g's grid.
-template <typename T, bool INT8, bool A_E5M2, bool KSPLIT, bool RAGGED, bool FINISH>
-__device__ __forceinline__ void gemm_nt_ring_body(const GemmDev &g, const int block, const RingFinish &fin)
+// number in g's grid.  GATED: the gated feed-forward's two products (gemm_gated.h).
+template <typename T, bool INT8, bool A_E5M2, bool KSPLIT, bool RAGGED, bool FINISH, bool GATED = false>
+__device__ __forceinline__ void gemm_nt_ring_body(const GemmDev &g, const int block, const RingFinish &fin, const GatedDev &gd = GatedDev{})
 {
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
@@ -110,13 +111,17 @@ __device__ __forceinline__ void gemm_nt_ring_body(const GemmDev &g, const int bl
     // ---- operand stream: an instruction fills 8 rows x 128 bytes, chunks XOR-swizzled with (row/2)%8
     const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem;
     const uint32_t k_first = (uint32_t)kt_begin * T::BK;
-    const uint8_t *Ag = g.A + (int64_t)tm * T::BM * g.K + k_first, *Bg = g.B + (int64_t)tn * T::BN * g.K + k_first;
-    const int a_rows = g.M - tm * T::BM, b_rows = g.N - tn * T::BN;
+    const int bn = GATED ? T::BN / 2 : T::BN;
+    const uint8_t *Ag = g.A + (int64_t)tm * T::BM * g.K + k_first, *Bg = g.B + (int64_t)tn * bn * g.K + k_first;
+    if (GATED && (wave & 1) != 0)  // this wave's rows of a tile are the up projection's
+        Bg += (int64_t)g.N * g.K;
+    const int a_rows = g.M - tm * T::BM, b_rows = g.N - tn * bn;
     const int chunk = (lane & 7) ^ ((4 * (wave & 1) + (lane >> 4)) & 7);  // NWAVES is even: the same in every piece
     uint32_t voff[T::LOADS];
 #pragma unroll
     for (int p = 0; p < T::LOADS; ++p) {
-        const int row = ((p < T::A_DMA ? p : p - T::A_DMA) * T::NWAVES + wave) * 8 + (lane >> 3);
+        const int eight = (p < T::A_DMA ? p : p - T::A_DMA) * T::NWAVES + wave;
+        const int row = GATED && p >= T::A_DMA ? gated_column(eight, lane >> 3) : eight * 8 + (lane >> 3);
         const int valid = p < T::A_DMA ? a_rows : b_rows;  // rows past the matrix: the last one, never stored
         voff[p] = (uint32_t)(row < valid ? row : valid - 1) * (uint32_t)g.K + chunk * 16;
     }
@@ -304,7 +309,9 @@ __device__ __forceinline__ void gemm_nt_ring_body(const GemmDev &g, const int bl
             }
     }
     typedef TileR<T::BM, T::BN, T::WM, T::WN, 1, T::NS> Out;  // the waves that write
-    if constexpr (KSPLIT) {
+    if constexpr (GATED) {
+        gated_epilogue<Out, INT8>(g, gd, acc, smem, tm, tn, wm, wn, lane, w, alpha);
+    } else if constexpr (KSPLIT) {
         store_ksplit_run<Out>(g, acc, split, tm, tn, wm, wn, l31, lh);
     } else {
         NoBandHook no_hook;
@@ -319,6 +326,12 @@ template <typename T, bool INT8, bool A_E5M2, bool KSPLIT, bool RAGGED>
 __global__ __launch_bounds__(T::THREADS, T::WG_PER_CU *T::NWAVES / 4) void gemm_nt_ring_kernel(GemmDev g, RingFinish fin)
 {
     gemm_nt_ring_body<T, INT8, A_E5M2, KSPLIT, RAGGED, !INT8 && !A_E5M2 && !KSPLIT>(g, (int)blockIdx.x, fin);
+}
+
+template <typename T, bool INT8, bool RAGGED>
+__global__ __launch_bounds__(T::THREADS, T::WG_PER_CU *T::NWAVES / 4) void gemm_nt_ring_gated_kernel(GemmDev g, GatedDev gd)
+{
+    gemm_nt_ring_body<T, INT8, false, false, RAGGED, false, true>(g, (int)blockIdx.x, RingFinish{}, gd);
 }
 
 // The two products of a linear layer's backward in one launch: workgroups [0, n0) are the grid of g0,

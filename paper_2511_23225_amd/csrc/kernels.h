@@ -72,6 +72,8 @@ struct DelayedUpdate2 {
     float *sc1;
 };
 hipError_t launch_delayed_update2(const DelayedUpdate2 &u, hipStream_t s);
+// one state; its tensor's amax: the accumulator, or the maximum over partials
+hipError_t launch_delayed_update(void *state, bool bootstrap, bool e5m2, const uint32_t *partials, int n_partials, float *sc_out, hipStream_t s);
 hipError_t launch_quantize2_e4m3_delayed(const void *x0_bf16, int64_t rows0, int64_t cols0, void *state0, uint8_t *q0,
                                          uint8_t *q0T, float *sc0, const void *x1_bf16, int64_t rows1, int64_t cols1,
                                          void *state1, uint8_t *q1, uint8_t *q1T, float *sc1, int bootstrap,
@@ -209,6 +211,28 @@ struct GemmArgs {
     bool out_i8;
     float out_inv_step;
 };
+
+// The gated feed-forward's first half (gemm_gated.hip): C[M,N] = act(A Bg^T) * (A Bu^T), B's rows 0 .. N-1 the gate's and N .. 2N-1 the
+// up projection's.  FP8: both products are rounded to bf16 (and stored to gu [M, 2N], if given), then multiplied; INT8: the
+// dequantised fp32 values are, with step vectors of A's rows and B's 2N rows.
+struct GateCoef {
+    float c0, c1;
+};
+hipError_t launch_fp8_gated(const GemmArgs &a, bool gelu, void *gu, hipStream_t s);
+hipError_t launch_i8_gated(const GemmArgs &a, bool gelu, hipStream_t s);
+// Its gradients by gate and up projection, bf16 (dg | du) [M, 2F], cast without being stored (gated.hip); M % 16 == 0, F % 8 == 0.
+struct GatedGradCall {
+    const void *dh, *gu;
+    int64_t M, F;
+    bool gelu, e5m2;
+    uint8_t *q, *qT;
+    float *scalars;      // amax, scale, its inverse
+    uint32_t *partials;  // current scaling and bootstrap: kGatedPartials words of scratch
+    void *state;         // delayed scaling, or nullptr
+    bool bootstrap;
+};
+constexpr int kGatedPartials = 1024;
+hipError_t launch_gated_grad(const GatedGradCall &c, hipStream_t s);
 
 // The ring GEMM (gemm_ring.h): tile shapes; the one that a product (a layer's two gradient products in one launch)
 // runs fastest on if all its workgroups are resident at once (the pair: also in rounds of 128x128 tiles, the weight
