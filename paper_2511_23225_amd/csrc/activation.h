@@ -21,6 +21,17 @@ __device__ __forceinline__ float gate_share(float g, const GateCoef &c)
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-z));
 }
 
+// The exponential of it by itself, p = 1 / (1 + this): the same bits
+template <bool GELU>
+__device__ __forceinline__ float gate_exp(float g, const GateCoef &c)
+{
+    if constexpr (GELU) {
+        const float b = __builtin_amdgcn_fmed3f(g, -0x1p60f, 0x1p60f);
+        return __builtin_amdgcn_exp2f(-(b * __builtin_fmaf(c.c1, b * b, c.c0)));
+    }
+    return __builtin_amdgcn_exp2f(-(g * c.c0));
+}
+
 __device__ __forceinline__ float gated(float g, float u, const GateCoef &c) { return g * gate_share(g, c) * u; }
 
 }  // namespace tweo

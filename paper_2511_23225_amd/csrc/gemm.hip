@@ -1249,6 +1249,7 @@ static const int kVariantBN[kNumVariants + 1] = {0, 256, 128, 128, 64, 256, 256,
 static int ring_variant(int shape) { return shape == 0 ? 4 : 17 + shape; }
 static int ring_shape(int variant) { return variant == 4 ? 0 : variant >= 18 && variant <= 22 ? variant - 17 : -1; }
 int gemm_num_variants() { return kNumVariants; }
+int gemm_tile_override() { return g_tile_override; }
 bool gemm_variant_exists(int v)
 {
     return v >= 0 && v <= kNumVariants && v != 2 && v != 5 && v != 7 && v != 9 && v != 10 && v != 12;

@@ -5,6 +5,7 @@
 //   192x256 tiles (EDGE): any M; with ANY also any N % 8 == 0 and K % 16 == 0, from 912 on and without a residual;
 //   both heights one after the other in a launch (gemm_mixed.hip);
 //   one unit of a K split (KSPLIT): 256x256 tiles, K in runs, with RAGGED any K % 16 == 0;
+//   both products of the gated feed-forward with its activation (GATE, gemm_gated.hip), on 256x256 tiles and, with edges, 192x256;
 //   both gradients of a layer, such a unit or a whole tile of the one and then tiles of the other, in a launch (gemm_pair.hip).
 //
 // One workgroup of four waves per CU (one wave per SIMD, so a wave may hold
@@ -44,6 +45,7 @@
 #pragma once
 #include <utility>
 #include "gemm_common.h"
+#include "gemm_gated.h"
 
 namespace tweo {
 
@@ -155,6 +157,77 @@ struct DrainPlanOf {  // evaluated once per tile shape and D, not once per slot 
     static constexpr DrainPlan<T, D, PEN> value = make_drain_plan<T, D, PEN>();
 };
 
+// The same for the gated feed-forward, by bands (32 rows of the wave: its two pairs are 64 columns of the gate and the same 64 of
+// the up projection).  A band takes 16 exchanges, with KEEP then the stores of both projections (8), as the product takes the gate's
+// registers; 16 words of the product in three steps each (exponentials, reciprocals, products), and its 4 stores, each behind its four words.
+// The exchanges of band i + 1 go in front of the product of band i, whose stores have that long.
+template <typename T, int D, bool KEEP>
+struct GatedPlan {
+    static constexpr int NSLOT = D * T::SLOTS, BANDS = T::MT, EXCHANGES = 16, PRODUCT = 48, ALU = BANDS * (EXCHANGES + PRODUCT);
+    static constexpr int KEPT = KEEP ? 8 : 0, STORES = BANDS * (KEPT + 4);
+    int alu_lo[NSLOT], alu_hi[NSLOT], store[NSLOT];
+    bool ok;
+    // Entry n of the order first(0), first(1), second(0), first(2), second(1), .. second(BANDS - 1), of `a` and `b` entries each: 64 * band +
+    // entry, those of `second` behind those of `first`.
+    __host__ __device__ __attribute__((always_inline)) static constexpr int in_order(int n, int a, int b)
+    {
+        if (n < a)
+            return n;
+        n -= a;
+        const int i = n / (a + b), r = n % (a + b);
+        if (i >= BANDS - 1)
+            return 64 * (BANDS - 1) + a + (n - (BANDS - 1) * (a + b));
+        return r < a ? 64 * (i + 1) + r : 64 * i + r;
+    }
+    __host__ __device__ __attribute__((always_inline)) static constexpr int alu(int n) { return in_order(n, EXCHANGES, PRODUCT); }
+    __host__ __device__ __attribute__((always_inline)) static constexpr int stored(int n) { return in_order(n, KEPT, 4); }
+};
+template <typename T, int D, bool KEEP>
+constexpr GatedPlan<T, D, KEEP> make_gated_plan()
+{
+    using P = GatedPlan<T, D, KEEP>;
+    constexpr int FIRST = 2;
+    // where each band's steps and stores come in their orders
+    int alu_place[64 * P::BANDS] = {}, store_place[64 * P::BANDS] = {};
+    for (int n = 0; n < P::ALU; ++n)
+        alu_place[P::alu(n)] = n;
+    for (int n = 0; n < P::STORES; ++n)
+        store_place[P::stored(n)] = n;
+    for (int end = P::NSLOT - 4; end > P::NSLOT / 2; end -= 2) {
+        P p{};
+        int done = 0, stored = 0;  // arithmetic steps and stores of the slots before
+        for (int s = 0; s < P::NSLOT; ++s) {
+            const int done_before = done, stored_before = stored;
+            p.alu_lo[s] = done;
+            const int due = s < FIRST ? 0 : (int)((long long)(s - FIRST + 1) * P::ALU / (end - FIRST));
+            while (done < P::ALU && done < due && done - done_before < 3) {
+                const int band = P::alu(done) / 64, r = P::alu(done) % 64;
+                if (KEEP && r >= P::EXCHANGES && stored_before <= store_place[64 * band + P::KEPT - 1])
+                    break;  // what this would overwrite has not been stored
+                ++done;
+            }
+            p.alu_hi[s] = done;
+            p.store[s] = -1;
+            if (stored < P::STORES && !T::load_slot(s % T::SLOTS)) {
+                const int band = P::stored(stored) / 64, k = P::stored(stored) % 64;
+                const int need = k < P::KEPT ? (k < 4 ? 8 : 16) : P::EXCHANGES + 12 * (k - P::KEPT + 1);  // steps of the band
+                if (done_before > alu_place[64 * band + need - 1])
+                    p.store[s] = stored++;
+            }
+        }
+        p.ok = done == P::ALU && stored == P::STORES;
+        if (p.ok)
+            return p;
+    }
+    P bad{};
+    bad.ok = false;
+    return bad;
+}
+template <typename T, int D, bool KEEP>
+struct GatedPlanOf {
+    static constexpr GatedPlan<T, D, KEEP> value = make_gated_plan<T, D, KEEP>();
+};
+
 // stages over which a residual is loaded, and the contraction that has room for them
 constexpr int kDeferResSpread = 8, kDeferResSpreadK = 128 * (5 + DeferTile<4>::res_stages(kDeferResSpread) + 1);
 
@@ -196,8 +269,12 @@ struct DeferEnd {
 // RAGGED (one unit of 256 rows) or ANY: a contraction that is no multiple of 128.  The lanes whose chunk of the last stage lies past
 // its end load the row's last stage from its first chunk instead, so the offsets change once, two stages before; the wave then
 // clears what it has brought of A there, in front of the barrier that publishes the stage.
-template <bool INT8, int PMODE, int D, int MT, bool A_E5M2, bool KSPLIT, int RES, bool RAGGED, bool ANY, typename WORK, typename BETWEEN>
-__device__ __forceinline__ void defer_tiles(const GemmDev &g, const WORK &work, bool opened, BETWEEN between, float &pen)
+// GATE (FP8): 1 SiLU, 2 GELU: g.N columns of the gated feed-forward.  A tile holds 128 of them: its B's pieces are 64 rows of the gate and the same
+// 64 of the up projection in turn, so that a wave's first pair of blocks is the gate's and its second the up projection's, lane by lane the
+// same elements.  They are rounded to bf16 as in a plain product; the product of a band is formed from its two pairs behind their exchanges.
+// KEEP: both are stored (gd.gu).
+template <bool INT8, int PMODE, int D, int MT, bool A_E5M2, bool KSPLIT, int RES, bool RAGGED, bool ANY, int GATE, bool KEEP, typename WORK, typename BETWEEN>
+__device__ __forceinline__ void defer_tiles(const GemmDev &g, const WORK &work, bool opened, BETWEEN between, float &pen, const GatedDev &gd = GatedDev{})
 {
     using T = DeferTile<MT>;
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
@@ -210,6 +287,8 @@ __device__ __forceinline__ void defer_tiles(const GemmDev &g, const WORK &work, 
     static_assert(!RAGGED || (WORK::ONE && MT == 4), "one unit, its last three stages apart");
     if (!work.has(0))
         return;
+    static_assert(GATE == 0 || (!INT8 && PMODE == 0 && RES == 0 && !KSPLIT && LAST_LIST && !RAGGED), "the gated product is a forward one");
+    constexpr int TILE_COLS = GATE != 0 ? T::BN / 2 : T::BN, WAVE_COLS = TILE_COLS / 2;  // of the output
     static_assert(!ANY || (MT == 3 && RES == 0 && !KSPLIT && LAST_LIST), "edges on every side");
     const int kt_all = RAGGED || ANY ? (g.K + T::BK - 1) / T::BK : g.K / T::BK;
     int kt = kt_all, k_first = 0;
@@ -243,9 +322,9 @@ __device__ __forceinline__ void defer_tiles(const GemmDev &g, const WORK &work, 
     const uint32_t past = (RAGGED || ANY) && k_first + kt == kt_all && (int)dma_chunk >= g.K - (kt_all - 1) * T::BK ? dma_chunk : 0u;
     auto set_voffs_b = [&](int tn) {  // ANY: rows past the matrix load the last valid one
         if constexpr (ANY) {
-            const int valid = g.N - tn * T::BN;
+            const int valid = g.N - tn * TILE_COLS;
 #pragma unroll
-            for (int p8 = 0; p8 < 8; ++p8) {
+            for (int p8 = 0; p8 < (GATE != 0 ? 4 : 8); ++p8) {
                 const int r = T::band_row(0, p8) + T::lane_row(wave * 8 + dma_row);
                 voffs[p8] = (uint32_t)(r < valid ? r : valid - 1) * (uint32_t)g.K + dma_chunk;
             }
@@ -270,7 +349,7 @@ __device__ __forceinline__ void defer_tiles(const GemmDev &g, const WORK &work, 
         int tm = 0, tn = 0;
         if (work.has(r0 + lane))
             tile_from_id(id_l, g.tiles_m, g.tiles_n, tm, tn);
-        const uint64_t oa = (uint64_t)tm * T::BM * (uint64_t)g.K, ob = (uint64_t)tn * T::BN * (uint64_t)g.K;
+        const uint64_t oa = (uint64_t)tm * T::BM * (uint64_t)g.K, ob = (uint64_t)tn * TILE_COLS * (uint64_t)g.K;
         ta_lo = (uint32_t)oa;
         ta_hi = (uint32_t)(oa >> 32);
         tb_lo = (uint32_t)ob;
@@ -338,11 +417,15 @@ __device__ __forceinline__ void defer_tiles(const GemmDev &g, const WORK &work, 
                      : "s"(dst0), "s"(sa.bufoff), "v"(T::EDGE ? voffs_a[T::EDGE ? p8 : 0] : voffs[p8]), "s"(sa.ptr)
                      : "memory", "m0", "scc");
     };
+    const int64_t up_rows = GATE != 0 ? (int64_t)g.N * g.K : 0;  // from the gate's to the up projection's
     auto dma_piece_b = [&](int p8) {
         const uint32_t dst0 = lds_base + T::A_BYTES + (p8 * 4 + wave) * 1024;
+        // (the tile's rows of either kind lie 0, 16, 64 and 80 behind the first, as those of A's first four pieces)
+        const uint32_t voff = voffs[GATE != 0 ? (p8 >> 2) * 2 + (p8 & 1) : p8];
+        const uint8_t *from = GATE != 0 && (p8 & 2) != 0 ? sb.ptr + up_rows : sb.ptr;
         asm volatile("s_add_u32 m0, %0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3"
                      :
-                     : "s"(dst0), "s"(sb.bufoff), "v"(voffs[p8]), "s"(sb.ptr)
+                     : "s"(dst0), "s"(sb.bufoff), "v"(voff), "s"(from)
                      : "memory", "m0", "scc");
     };
 
@@ -472,7 +555,7 @@ __device__ __forceinline__ void defer_tiles(const GemmDev &g, const WORK &work, 
     };
     // Stores walk the wave's sub-tile with one scalar pointer (first row of the band of blocks
     // being written); the pair of blocks goes into the instruction's offset field.
-    const uint8_t *sp = nullptr;
+    const uint8_t *sp = nullptr, *kept = nullptr;  // kept (KEEP): as sp, of both projections, whose rows are twice as long
     const int64_t rows16 = (int64_t)g.N * 32;
     auto next_band = [&](int i) { return ((wm * MT + i) & 1) ? 3 * rows16 : rows16; };  // from band i to the next one
     int rows_valid = 0;  // EDGE: rows of the tile in `packed` inside the matrix
@@ -481,9 +564,11 @@ __device__ __forceinline__ void defer_tiles(const GemmDev &g, const WORK &work, 
         if constexpr (T::EDGE)
             rows_valid = g.M - tm * T::BM;
         if constexpr (ANY)
-            cols_valid = g.N - tn * T::BN - wn * 128;
-        sp = (const uint8_t *)g.out +
-             (((int64_t)tm * T::BM + T::band_row(wm, 0)) * g.N + (int64_t)tn * T::BN + wn * 128) * 2;
+            cols_valid = g.N - tn * TILE_COLS - wn * WAVE_COLS;
+        const int64_t row = (int64_t)tm * T::BM + T::band_row(wm, 0), col = (int64_t)tn * TILE_COLS + wn * WAVE_COLS;
+        sp = (const uint8_t *)g.out + (row * g.N + col) * 2;
+        if constexpr (KEEP)
+            kept = (const uint8_t *)gd.gu + (row * g.N * 2 + col) * 2;
     };
     const int lane_row = T::lane_row(l31);
     // Arithmetic step a works on the pair of neighbouring blocks c = a / PER (blocks 2c,
@@ -512,6 +597,54 @@ __device__ __forceinline__ void defer_tiles(const GemmDev &g, const WORK &work, 
             else
                 quad_exchange<1>(A[d], A[4 + d], B[d], B[4 + d], qmasks);
         }
+    };
+    // GATE: step n of a tile's write-out (GatedPlan): r = 0 .. 15 the exchanges of both pairs, then three a word: w of the 16 words
+    // that the quad's lane holds of the gate (and of the up projection) becomes the product's
+    float gate0 = 0.0f, gate1 = 0.0f;
+    auto gated_alu = [&](int n) {
+        const int a = GatedPlan<T, D, KEEP>::alu(n), i = a / 64, r = a % 64;
+        if (r < 16) {
+            uint32_t *A = packed[i][2 * (r >> 3)], *B = packed[i][2 * (r >> 3) + 1];
+            const int d = (r & 7) >> 1;
+            if ((r & 1) == 0)
+                quad_exchange<0>(A[d], A[4 + d], B[d], B[4 + d], qmasks);
+            else
+                quad_exchange<1>(A[d], A[4 + d], B[d], B[4 + d], qmasks);
+            return;
+        }
+        const int w = (r - 16) / 3, part = (r - 16) % 3;
+        uint32_t &gw = packed[i][w >> 3][w & 7];
+        const uint32_t uw = packed[i][2 + (w >> 3)][w & 7];
+        if (part == 0) {
+            gate0 = gate_exp<GATE == 2>(bf16lo_to_f32(gw), gd.act);
+            gate1 = gate_exp<GATE == 2>(bf16hi_to_f32(gw), gd.act);
+            asm volatile("" : "+v"(gate0), "+v"(gate1));
+        } else if (part == 1) {
+            gate0 = __builtin_amdgcn_rcpf(1.0f + gate0);
+            gate1 = __builtin_amdgcn_rcpf(1.0f + gate1);
+            asm volatile("" : "+v"(gate0), "+v"(gate1));
+        } else {
+            gw = pack_bf16x2(bf16lo_to_f32(gw) * gate0 * bf16lo_to_f32(uw), bf16hi_to_f32(gw) * gate1 * bf16hi_to_f32(uw));
+            asm volatile("" : "+v"(gw));
+        }
+    };
+    const uint32_t kept_quad = KEEP ? (uint32_t)T::lane_row(l31 & ~3) * (uint32_t)g.N * 4u + (uint32_t)lh * 64u + (uint32_t)(l31 & 3) * 16u : 0u;
+    // store st of a tile: 4 of the gate and 4 of the up projection (KEEP), 4 of the product
+    auto gated_store = [&](int st) {
+        using Plan = GatedPlan<T, D, KEEP>;
+        const int i = Plan::stored(st) / 64, k = Plan::stored(st) % 64, u = k & 3;
+        const bool product = k >= Plan::KEPT;
+        const int jp = !product && k >= 4 ? 1 : 0;
+        if ((!T::EDGE || T::band_row(wm, i) + (lane_row & ~3) + u < rows_valid) && (!ANY || lh * 32 + (l31 & 3) * 8 < cols_valid)) {
+            const uint32_t *w = packed[i][2 * jp + (u >> 1)] + 4 * (u & 1);
+            const v4i v = {(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+            const uint8_t *spu = product ? sp + u * row_bytes : kept + u * 2 * row_bytes + (jp != 0 ? row_bytes : 0);
+            asm volatile("global_store_dwordx4 %0, %1, %2 nt\n\ts_nop 1" : : "v"(product ? out_quad : kept_quad), "v"(v), "s"(spu) : "memory");
+        }
+        if (k == Plan::KEPT + 3)
+            sp += next_band(i);
+        if (KEEP && k == Plan::KEPT - 1)
+            kept += 2 * next_band(i);
     };
     auto drain_store = [&](int st) {
         const int c = st / 4, u = st % 4, i = c >> 1, jp = c & 1;
@@ -679,7 +812,20 @@ __device__ __forceinline__ void defer_tiles(const GemmDev &g, const WORK &work, 
                         if ((LAST && T::convert_slot(h) == t) || (FIRST == 2 && T::convert_slot(h) == t + T::SLOTS))
                             convert_half(h);
                     // write-out of the previous tile
-                    if constexpr (DR >= 0) {
+                    if constexpr (DR >= 0 && GATE != 0) {
+                        using Plan = GatedPlanOf<T, D, KEEP>;
+                        static_assert(Plan::value.ok, "the write-out fits the first D stages");
+                        constexpr int ds = DR * T::SLOTS + t;
+                        constexpr int a_lo = Plan::value.alu_lo[ds], a_hi = Plan::value.alu_hi[ds], st = Plan::value.store[ds];
+                        if constexpr (a_lo < a_hi)
+                            gated_alu(a_lo);
+                        if constexpr (a_lo + 1 < a_hi)
+                            gated_alu(a_lo + 1);
+                        if constexpr (a_lo + 2 < a_hi)
+                            gated_alu(a_lo + 2);
+                        if constexpr (st >= 0)
+                            gated_store(st);
+                    } else if constexpr (DR >= 0) {
                         using Plan = DrainPlanOf<T, D, (PMODE != 0)>;
                         static_assert(Plan::value.ok, "the write-out fits the first D stages");
                         constexpr int ds = DR * T::SLOTS + t;
@@ -897,6 +1043,33 @@ __device__ __forceinline__ void defer_tiles(const GemmDev &g, const WORK &work, 
                     const uint32_t *w = &packed[i][j][4 * u];
                     *(uint4 *)(tb + (wr ^ (uint32_t)((8 * (j >> 1) + 2 * (j & 1) + u) << 4))) = make_uint4(w[0], w[1], w[2], w[3]);
                 }
+            if constexpr (GATE != 0) {
+                // eight rows at a time, a lane eight columns: places 8q .. +7, rows 4q .. +3 and 32 + 4q .. +3 of the band
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int p = 8 * q + (lane >> 3), c = lane & 7, row = 32 * (lane >> 5) + 4 * q + ((lane >> 3) & 3);
+                    const v4i gv = *(const v4i *)(tb + p * 256 + ((c ^ (p & 15)) << 4)), uv = *(const v4i *)(tb + p * 256 + (((c + 8) ^ (p & 15)) << 4));
+                    v4i h;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w)
+                        h[w] = (int)pack_bf16x2(gated(bf16lo_to_f32((uint32_t)gv[w]), bf16lo_to_f32((uint32_t)uv[w]), gd.act),
+                                                gated(bf16hi_to_f32((uint32_t)gv[w]), bf16hi_to_f32((uint32_t)uv[w]), gd.act));
+                    if ((!T::EDGE || T::band_row(wm, i) + row < rows_valid) && (!ANY || c * 8 < cols_valid)) {
+                        const uint32_t off = (uint32_t)row * (uint32_t)g.N * 2u + (uint32_t)c * 16u;
+                        asm volatile("global_store_dwordx4 %0, %1, %2 nt\n\ts_nop 1" : : "v"(off), "v"(h), "s"(sp) : "memory");
+                        if constexpr (KEEP) {
+                            const uint32_t twice = (uint32_t)row * (uint32_t)g.N * 4u + (uint32_t)c * 16u;
+                            const uint8_t *up = kept + row_bytes;
+                            asm volatile("global_store_dwordx4 %0, %1, %2 nt\n\ts_nop 1" : : "v"(twice), "v"(gv), "s"(kept) : "memory");
+                            asm volatile("global_store_dwordx4 %0, %1, %2 nt\n\ts_nop 1" : : "v"(twice), "v"(uv), "s"(up) : "memory");
+                        }
+                    }
+                }
+                sp += next_band(i);
+                if constexpr (KEEP)
+                    kept += 2 * next_band(i);
+                continue;
+            }
             // four rows at a time: places 8q + 4b .. +3, rows 32b + 4q .. +3 of the band
 #pragma unroll
             for (int ps = 0; ps < 8; ++ps) {
@@ -1001,10 +1174,18 @@ __global__ __launch_bounds__(256, 1) void gemm_nt_defer_kernel(GemmDev g)
     const int tiles = g.tiles_m * g.tiles_n;
     float pen = 0.0f;
     if constexpr (KSPLIT)
-        defer_tiles<INT8, PMODE, D, MT, A_E5M2, KSPLIT, RES, RAGGED, ANY>(g, DeferUnit{xcd_slot(), tiles, tiles * g.ksplit}, false, DeferEnd{}, pen);
+        defer_tiles<INT8, PMODE, D, MT, A_E5M2, KSPLIT, RES, RAGGED, ANY, 0, false>(g, DeferUnit{xcd_slot(), tiles, tiles * g.ksplit}, false, DeferEnd{}, pen);
     else
-        defer_tiles<INT8, PMODE, D, MT, A_E5M2, KSPLIT, RES, RAGGED, ANY>(g, DeferRounds{xcd_slot(), (int)gridDim.x, tiles}, false, DeferEnd{}, pen);
+        defer_tiles<INT8, PMODE, D, MT, A_E5M2, KSPLIT, RES, RAGGED, ANY, 0, false>(g, DeferRounds{xcd_slot(), (int)gridDim.x, tiles}, false, DeferEnd{}, pen);
     defer_penalty<PMODE>(g, pen);
+}
+
+// Both products of the gated feed-forward with its activation (gemm_gated.hip).
+template <int D, int MT, bool ANY, int GATE, bool KEEP>
+__global__ __launch_bounds__(256, 1) void gemm_nt_defer_gated_kernel(GemmDev g, GatedDev gd)
+{
+    float pen = 0.0f;
+    defer_tiles<false, 0, D, MT, false, false, 0, false, ANY, GATE, KEEP>(g, DeferRounds{xcd_slot(), (int)gridDim.x, g.tiles_m * g.tiles_n}, false, DeferEnd{}, pen, gd);
 }
 
 }  // namespace tweo

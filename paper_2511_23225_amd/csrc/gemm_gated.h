@@ -17,6 +17,10 @@ struct GatedDev {
     GateCoef act;
 };
 
+// host side (gemm_gated.hip, gemm_gated_any.hip)
+int gated_workgroups(int64_t M, int64_t F, int bm);
+hipError_t launch_defer_any_gated(const GemmArgs &a, bool gelu, const GatedDev &gd, hipStream_t s);
+
 // column, of the tile's, of the row-th of the eight rows of B's eight rows number `eight`
 __device__ __forceinline__ int gated_column(int eight, int row) { return (eight >> 2) * 16 + ((eight >> 1) & 1) * 8 + row; }
 

@@ -23,9 +23,9 @@ struct HeadsSide {
     uint16_t *y;
     int64_t x_token, x_head, dy_token, dy_head, y_token, y_head;
     int heads;
-    // a workgroup's share: so many heads of so many tokens; `splits` workgroups share the heads of a token
-    int block_heads, splits, blocks;
-    int64_t block_tokens;
+    // what a workgroup takes at a time: so many heads of so many tokens; `splits` workgroups share the heads of a token.  The gradients'
+    // go on in steps of all workgroups' tokens.
+    int block_heads, block_tokens, splits, blocks;
 };
 struct HeadsDev {
     HeadsSide side[2];
@@ -55,11 +55,24 @@ struct HeadsVector {  // 16-byte pieces: eight pairs a lane
     }
     __device__ __forceinline__ bool rotates(int) const { return turns; }
     __device__ __forceinline__ int angle(int e) const { return at + e; }
-    __device__ __forceinline__ void load(const uint16_t *p, float (&a)[PER], float (&b)[PER]) const
+    struct Raw {
+        v4i a, b;
+    };
+    template <bool ONCE>
+    __device__ __forceinline__ Raw fetch(const uint16_t *p) const
     {
-        const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-        const uint4 A = va ? *(const uint4 *)(p + 8 * ca) : zero, B = vb ? *(const uint4 *)(p + 8 * cb) : zero;
-        const uint32_t w[8] = {A.x, A.y, A.z, A.w, B.x, B.y, B.z, B.w};
+        Raw r{{0, 0, 0, 0}, {0, 0, 0, 0}};
+        const v4i *A = (const v4i *)(p + 8 * ca), *B = (const v4i *)(p + 8 * cb);
+        if (va)
+            r.a = ONCE ? __builtin_nontemporal_load(A) : *A;
+        if (vb)
+            r.b = ONCE ? __builtin_nontemporal_load(B) : *B;
+        return r;
+    }
+    __device__ __forceinline__ void widen(const Raw &r, float (&a)[PER], float (&b)[PER]) const
+    {
+        const uint32_t w[8] = {(uint32_t)r.a[0], (uint32_t)r.a[1], (uint32_t)r.a[2], (uint32_t)r.a[3],
+                               (uint32_t)r.b[0], (uint32_t)r.b[1], (uint32_t)r.b[2], (uint32_t)r.b[3]};
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             if constexpr (PAIRS) {
@@ -107,13 +120,27 @@ struct HeadsScalar {  // element by element: pairs lane, lane + 64, ...
         const int c = PAIRS || p >= half ? 2 * p + second : p + (second ? half : 0);
         return c < dim ? c : -1;
     }
-    __device__ __forceinline__ void load(const uint16_t *p, float (&a)[PER], float (&b)[PER]) const
+    struct Raw {
+        uint32_t w[2 * PER];
+    };
+    template <bool ONCE>
+    __device__ __forceinline__ Raw fetch(const uint16_t *p) const
     {
+        Raw r;
 #pragma unroll
         for (int e = 0; e < PER; ++e) {
             const int i = column(e, false), j = column(e, true);
-            a[e] = i >= 0 ? bits_to_f32((uint32_t)p[i] << 16) : 0.0f;
-            b[e] = j >= 0 ? bits_to_f32((uint32_t)p[j] << 16) : 0.0f;
+            r.w[2 * e] = i >= 0 ? p[i] : 0u;
+            r.w[2 * e + 1] = j >= 0 ? p[j] : 0u;
+        }
+        return r;
+    }
+    __device__ __forceinline__ void widen(const Raw &r, float (&a)[PER], float (&b)[PER]) const
+    {
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            a[e] = bits_to_f32(r.w[2 * e] << 16);
+            b[e] = bits_to_f32(r.w[2 * e + 1] << 16);
         }
     }
     __device__ __forceinline__ void store(uint16_t *p, const float (&a)[PER], const float (&b)[PER]) const
@@ -154,50 +181,42 @@ __device__ __forceinline__ float team_sum(float v)
         v += __shfl_xor(v, 32, kWave);
     return v;
 }
-template <int LANES>
-__device__ __forceinline__ double team_sum(double v)
-{
-#pragma unroll
-    for (int off = 1; off < LANES; off <<= 1)
-        v += __shfl_xor(v, off, kWave);
-    return v;
-}
-
-// x becomes xhat.  Squares that leave fp32 (values beyond 2^50, or, without an eps that covers them, below 2^-40) are taken in fp64.
+// x becomes xhat.  Squares whose sum leaves fp32 (beyond 2^100, or, without an eps that covers them, below 2^-80) are taken of values
+// moved by a power of two.
 template <int LANES, int PER>
-__device__ __forceinline__ float heads_normalise(float (&a)[PER], float (&b)[PER], int dim, float per_dim, float eps)
+__device__ __forceinline__ float heads_normalise(float (&a)[PER], float (&b)[PER], float per_dim, float eps)
 {
-    float ss = 0.0f;
+    auto squares = [&] {
+        float ss = 0.0f;
 #pragma unroll
-    for (int e = 0; e < PER; ++e)
-        ss = __builtin_fmaf(a[e], a[e], __builtin_fmaf(b[e], b[e], ss));
-    ss = team_sum<LANES>(ss);
-    if (ss < 0x1p100f && (ss > 0x1p-80f || eps > 0x1p-80f)) {
-        const float rstd = __builtin_amdgcn_rsqf(__builtin_fmaf(ss, per_dim, eps));
+        for (int e = 0; e < PER; ++e)
+            ss = __builtin_fmaf(a[e], a[e], __builtin_fmaf(b[e], b[e], ss));
+        return team_sum<LANES>(ss);
+    };
+    const float ss = squares();
+    float rstd = __builtin_amdgcn_rsqf(__builtin_fmaf(ss, per_dim, eps)), moved = 1.0f;
+    if (!(ss < 0x1p100f) || (ss < 0x1p-80f && eps < 0x1p-80f)) {
+        moved = ss < 1.0f ? 0x1p100f : 0x1p-90f;
 #pragma unroll
         for (int e = 0; e < PER; ++e) {
-            a[e] *= rstd;
-            b[e] *= rstd;
+            a[e] *= moved;
+            b[e] *= moved;
         }
-        return rstd;
+        rstd = (float)(1.0 / __builtin_sqrt((double)squares() * per_dim + (double)eps * moved * moved));
     }
-    double wide = 0.0;
-#pragma unroll
-    for (int e = 0; e < PER; ++e)
-        wide += (double)a[e] * a[e] + (double)b[e] * b[e];
-    const double rstd = 1.0 / __builtin_sqrt(team_sum<LANES>(wide) / dim + (double)eps);
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
-        a[e] = (float)(a[e] * rstd);
-        b[e] = (float)(b[e] * rstd);
+        a[e] *= rstd;
+        b[e] *= rstd;
     }
-    return (float)rstd;
+    return rstd * moved;
 }
 
 enum HeadsMode { kHeadsRotary, kHeadsNorm, kHeadsGrad };
 
-template <typename LANE, int LANES, int MODE>
-__global__ __launch_bounds__(kHeadsThreads) void heads_kernel(HeadsDev g)
+// ONCE: large calls; what is read is read past the caches.
+template <typename LANE, int LANES, int MODE, bool ONCE>
+__global__ __launch_bounds__(kHeadsThreads, 4) void heads_kernel(HeadsDev g)
 {
     constexpr int PER = LANE::PER, TEAMS = kHeadsThreads / LANES;
     __shared__ float2 angles[kHeadsAngles];
@@ -206,16 +225,15 @@ __global__ __launch_bounds__(kHeadsThreads) void heads_kernel(HeadsDev g)
     const HeadsSide &side = g.side[second];
     const int block = (int)blockIdx.x - (second ? g.side[0].blocks : 0), split = block % side.splits;
     const int h0 = split * side.block_heads, nh = min(side.block_heads, side.heads - h0);
-    const int64_t t0 = block / side.splits * side.block_tokens, t1 = min(t0 + side.block_tokens, g.tokens);
+    const int64_t t0 = (int64_t)(block / side.splits) * side.block_tokens, step = (int64_t)(side.blocks / side.splits) * side.block_tokens;
     const int tid = threadIdx.x, team = tid / LANES, half = g.rot >> 1;
     const LANE lane(tid & (LANES - 1), g.dim, g.rot);
-    const int at_once = half != 0 ? min(kHeadsTokens, kHeadsAngles / half) : kHeadsTokens;
     const float per_half = half != 0 ? 1.0f / (float)half : 0.0f, per_head = 1.0f / (float)nh, per_dim = 1.0f / (float)g.dim;
 
     float ga[PER], gb[PER];
     if constexpr (MODE != kHeadsRotary) {
         if (side.gain != nullptr) {
-            lane.load(side.gain, ga, gb);
+            lane.widen(lane.template fetch<false>(side.gain), ga, gb);
         } else {
 #pragma unroll
             for (int e = 0; e < PER; ++e)
@@ -228,8 +246,25 @@ __global__ __launch_bounds__(kHeadsThreads) void heads_kernel(HeadsDev g)
         for (int e = 0; e < PER; ++e)
             sa[e] = sb[e] = 0.0f;
 
-    for (int64_t t = t0; t < t1; t += at_once) {
-        const int nt = (int)min((int64_t)at_once, t1 - t);
+    for (int64_t t = t0; t < g.tokens; t += step) {
+        const int nt = (int)min((int64_t)side.block_tokens, g.tokens - t);
+        const uint16_t *x0 = side.x + t * side.x_token + (int64_t)h0 * side.x_head, *dy0 = side.dy + t * side.dy_token + (int64_t)h0 * side.dy_head;
+        uint16_t *y0 = side.y + t * side.y_token + (int64_t)h0 * side.y_head;
+        // an item is a head of a token; its heads are fetched one round ahead (padding too, which is there)
+        auto token_of = [&](int item) { return (int)(((float)item + 0.5f) * per_head); };
+        auto place = [&](int item, int64_t token, int64_t head) {
+            const int ti = token_of(item);
+            return (uint64_t)(uint32_t)ti * (uint64_t)token + (uint64_t)(uint32_t)(item - ti * nh) * (uint64_t)head;
+        };
+        typename LANE::Raw x{}, dy{};
+        auto fetch = [&](int item) {
+            x = lane.template fetch<ONCE>(x0 + place(item, side.x_token, side.x_head));
+            if constexpr (MODE == kHeadsGrad)
+                dy = lane.template fetch<ONCE>(dy0 + place(item, side.dy_token, side.dy_head));
+        };
+        const int items = nt * nh;
+        if (team < items)
+            fetch(team);
         if (t != t0)
             __syncthreads();
         for (int i = tid; i < nt * half; i += kHeadsThreads) {
@@ -245,23 +280,18 @@ __global__ __launch_bounds__(kHeadsThreads) void heads_kernel(HeadsDev g)
         }
         if (half != 0)
             __syncthreads();
-        for (int item = team; item < nt * nh; item += TEAMS) {
-            const int ti = (int)(((float)item + 0.5f) * per_head);
-            const int64_t token = t + ti, head = h0 + item - ti * nh;
+        for (int item = team; item < items; item += TEAMS) {
+            const int ti = token_of(item);
+            const float2 *cs = angles + ti * half;
+            float a[PER], b[PER], da[PER], db[PER];
+            lane.widen(x, a, b);
+            if constexpr (MODE == kHeadsGrad)
+                lane.widen(dy, da, db);
+            if (item + TEAMS < items)
+                fetch(item + TEAMS);
             if (half != 0 && padding[ti])
                 continue;
-            const float2 *cs = angles + ti * half;
-            float a[PER], b[PER];
-            lane.load(side.x + token * side.x_token + head * side.x_head, a, b);
-            if constexpr (MODE != kHeadsGrad) {
-                if constexpr (MODE == kHeadsNorm) {
-                    heads_normalise<LANES>(a, b, g.dim, per_dim, g.eps);
-#pragma unroll
-                    for (int e = 0; e < PER; ++e) {
-                        a[e] *= ga[e];
-                        b[e] *= gb[e];
-                    }
-                }
+            auto turn = [&](float (&a)[PER], float (&b)[PER]) {
 #pragma unroll
                 for (int e = 0; e < PER; ++e)
                     if (lane.rotates(e)) {
@@ -270,20 +300,23 @@ __global__ __launch_bounds__(kHeadsThreads) void heads_kernel(HeadsDev g)
                         a[e] = u;
                         b[e] = v;
                     }
-                lane.store(side.y + token * side.y_token + head * side.y_head, a, b);
+            };
+            if constexpr (MODE == kHeadsNorm) {
+                heads_normalise<LANES>(a, b, per_dim, g.eps);
+#pragma unroll
+                for (int e = 0; e < PER; ++e) {
+                    a[e] *= ga[e];
+                    b[e] *= gb[e];
+                }
+            }
+            if constexpr (MODE != kHeadsGrad) {
+                turn(a, b);
             } else {
-                float da[PER], db[PER];
-                lane.load(side.dy + token * side.dy_token + head * side.dy_head, da, db);
-                const float rstd = heads_normalise<LANES>(a, b, g.dim, per_dim, g.eps);
+                turn(da, db);
+                const float rstd = heads_normalise<LANES>(a, b, per_dim, g.eps);
                 float dot = 0.0f;
 #pragma unroll
                 for (int e = 0; e < PER; ++e) {
-                    if (lane.rotates(e)) {
-                        const float2 c = cs[lane.angle(e)];
-                        const float u = da[e] * c.x - db[e] * c.y, v = db[e] * c.x + da[e] * c.y;
-                        da[e] = u;
-                        db[e] = v;
-                    }
                     sa[e] = __builtin_fmaf(da[e], a[e], sa[e]);
                     sb[e] = __builtin_fmaf(db[e], b[e], sb[e]);
                     da[e] *= ga[e];
@@ -296,8 +329,8 @@ __global__ __launch_bounds__(kHeadsThreads) void heads_kernel(HeadsDev g)
                     a[e] = rstd * __builtin_fmaf(-a[e], dot, da[e]);
                     b[e] = rstd * __builtin_fmaf(-b[e], dot, db[e]);
                 }
-                lane.store(side.y + token * side.y_token + head * side.y_head, a, b);
             }
+            lane.store(y0 + place(item, side.y_token, side.y_head), a, b);
         }
     }
     if (MODE == kHeadsGrad && g.partials != nullptr) {
@@ -362,14 +395,15 @@ __global__ __launch_bounds__(256) void heads_gain_kernel(const float *__restrict
 }
 
 // ---- host side
+constexpr int64_t kHeadsOnceBytes = 128 << 20;
 constexpr int kHeadsBlockHeads = 2048;  // (a workgroup divides its items by them in fp32)
-constexpr int kHeadsGradBlocks = 640;   // workgroups of the gradients, two and a half a CU
+constexpr int kHeadsGradBlocks = 768;  // workgroups of the gradients, three a CU
+constexpr int kHeadsRounds = 4;  // heads of a team at a time
 
-// a row of dgain for each workgroup: a side has at most twice its share of them (a share rounded up), one more, and two for each
-// 2048 heads (at most 2^16); never more than heads
+// a row of dgain for each workgroup: each side has its share of them, one at least
 int64_t heads_grad_bytes(int64_t tokens, int64_t heads, int64_t dim)
 {
-    return std::min<int64_t>(2 * kHeadsGradBlocks + 2 + 2 * (heads / kHeadsBlockHeads + 2), tokens * heads) * dim * 4;
+    return std::min<int64_t>(tokens * heads, kHeadsGradBlocks + 1) * dim * 4;
 }
 
 static bool on_pieces(const void *p, int64_t token, int64_t head)
@@ -377,12 +411,15 @@ static bool on_pieces(const void *p, int64_t token, int64_t head)
     return ((uintptr_t)p & 15) == 0 && token % 8 == 0 && head % 8 == 0;
 }
 
-static void heads_share(HeadsSide &s, int64_t tokens, int64_t items, int at_once)
+// items: heads at a time; most: workgroups at most (a side has a 768th of all heads for each, so that its heads in that many parts
+// are 512 at a time at most)
+static void heads_share(HeadsSide &s, int64_t tokens, int64_t items, int64_t at_once, int64_t most)
 {
-    s.block_heads = (int)std::min<int64_t>({s.heads, items, kHeadsBlockHeads});
-    s.block_tokens = std::min<int64_t>(at_once, (items + s.block_heads - 1) / s.block_heads);
+    s.block_heads = (int)std::min<int64_t>(s.heads, std::max(std::min<int64_t>(items, kHeadsBlockHeads), (s.heads + most - 1) / most));
+    s.block_tokens = (int)std::min<int64_t>({tokens, at_once, (items + s.block_heads - 1) / s.block_heads});
     s.splits = (s.heads + s.block_heads - 1) / s.block_heads;
-    s.blocks = (int)(s.splits * ((tokens + s.block_tokens - 1) / s.block_tokens));
+    const int64_t rows = (tokens + s.block_tokens - 1) / s.block_tokens;
+    s.blocks = (int)(s.splits * std::min(rows, std::max<int64_t>(1, most / s.splits)));
 }
 
 template <typename LANE, int LANES>
@@ -396,19 +433,19 @@ static hipError_t launch_lanes(HeadsDev &g, int mode, int sides, hipStream_t s)
         all += g.tokens * g.side[i].heads;
     for (int i = 0; i < sides; ++i) {
         const int64_t mine = g.tokens * g.side[i].heads;
-        if (mode == kHeadsGrad) {
-            const int64_t most = std::max<int64_t>(1, kHeadsGradBlocks * mine / all);
-            heads_share(g.side[i], g.tokens, std::max<int64_t>(TEAMS, (mine + most - 1) / most), 1 << 30);
-        } else {
-            heads_share(g.side[i], g.tokens, std::min<int64_t>(8 * TEAMS, std::max<int64_t>(TEAMS, mine / 1024)), at_once);
-        }
+        const int64_t items = std::min<int64_t>(kHeadsRounds * TEAMS, std::max<int64_t>(TEAMS, mine / 1024));
+        heads_share(g.side[i], g.tokens, items, at_once, mode == kHeadsGrad ? std::max<int64_t>(1, kHeadsGradBlocks * mine / all) : (int64_t)1 << 31);
     }
     const dim3 grid((unsigned)(g.side[0].blocks + g.side[1].blocks)), block(kHeadsThreads);
-    switch (mode) {
-    case kHeadsRotary: hipLaunchKernelGGL((heads_kernel<LANE, LANES, kHeadsRotary>), grid, block, 0, s, g); break;
-    case kHeadsNorm: hipLaunchKernelGGL((heads_kernel<LANE, LANES, kHeadsNorm>), grid, block, 0, s, g); break;
-    default: hipLaunchKernelGGL((heads_kernel<LANE, LANES, kHeadsGrad>), grid, block, 0, s, g); break;
-    }
+    constexpr bool USUAL = LANES >= 4 && LANES <= 16;
+    if (mode == kHeadsRotary && USUAL && all * g.dim * 4 >= kHeadsOnceBytes)
+        hipLaunchKernelGGL((heads_kernel<LANE, LANES, kHeadsRotary, USUAL>), grid, block, 0, s, g);
+    else if (mode == kHeadsRotary)
+        hipLaunchKernelGGL((heads_kernel<LANE, LANES, kHeadsRotary, false>), grid, block, 0, s, g);
+    else if (mode == kHeadsNorm)
+        hipLaunchKernelGGL((heads_kernel<LANE, LANES, kHeadsNorm, false>), grid, block, 0, s, g);
+    else
+        hipLaunchKernelGGL((heads_kernel<LANE, LANES, kHeadsGrad, false>), grid, block, 0, s, g);
     return hipGetLastError();
 }
 

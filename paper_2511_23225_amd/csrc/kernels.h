@@ -315,6 +315,7 @@ bool take_profile_events(hipEvent_t *e0, hipEvent_t *e1);
 
 // Tile-shape override for benchmarking sweeps: 0 = heuristic.
 void set_gemm_tile_override(int variant);
+int gemm_tile_override();
 int gemm_num_variants();
 bool gemm_variant_exists(int v);
 

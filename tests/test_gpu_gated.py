@@ -98,6 +98,24 @@ def check_fp8_forward(M, F, K, act, rows=None, seed=0):
     assert off.max() <= 1, off.max()
 
 
+# the kernels that a call may run on, forced: 64x64 tiles (4, 18), 64x128 (19, 20), 128x128 (21), the deferred-epilogue kernel on whole tiles (15) and
+# with edges (24); where a variant does not take the sizes the usual choice runs
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("variant,shape", [(4, (130, 136, 272)), (18, (70, 40, 144)), (18, (65, 1000, 1040)), (19, (130, 136, 272)), (19, (64, 64, 128)), (20, (200, 328, 656)),
+                                           (20, (1, 64, 16)), (21, (300, 200, 400)), (21, (128, 64, 1152)),
+                                           (15, (256, 128, 768)), (15, (512, 256, 896)), (15, (1024, 2176, 1024)), (15, (768, 384, 1920)), (15, (2304, 4352, 2048)),
+                                           (15, (256, 128, 2176)), (24, (192, 128, 1024)), (24, (1, 8, 912)), (24, (193, 136, 928)), (24, (700, 1000, 1296)),
+                                           (24, (1000, 8200, 1168)), (24, (3000, 2056, 2320)), (24, (385, 264, 4096)), (24, (2049, 4104, 1024))])
+def test_fp8_forward_on(variant, shape, act):
+    M, F, K = shape
+    say("fp8 gated fwd on", variant, shape, act)
+    tw.tweo_set_gemm_tile(variant)
+    try:
+        check_fp8_forward(M, F, K, act, rows=min(M, 300))
+    finally:
+        tw.tweo_set_gemm_tile(0)
+
+
 def test_fp8_special_values():
     """A NaN code spoils its row, or its column and no other; projections that are infinite or overflow give what the formula gives."""
     M, F, K = 70, 72, 144
