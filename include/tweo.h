@@ -850,7 +850,8 @@ tweo_status tweo_w8a8_gated_i8out(const int8_t *xq, const int8_t *wq, int64_t M,
  * N % 4 == 0) = the weight-streaming kernel; elsewhere it means variant 4.  23 = the deferred-epilogue
  * kernel on both tile heights in one launch (any M, N a multiple of 256, K of 128 and at least 768, with a
  * residual 1408); where that has no use, 16.  24 = the same on 192x256 tiles for any N % 8 == 0 and K % 16
- * == 0 from 912 on, without a residual; elsewhere 3.  A variant whose K requirement is not met falls
+ * == 0 from 912 on, without a residual; elsewhere 3.  The gated feed-forward takes 4, 18 to 20, 21 (there two workgroups a CU) and, in FP8, 15 and 24,
+ * where they take its sizes, else what it chooses.  A variant whose K requirement is not met falls
  * back to the nearest one that fits.  Results are identical up to the fp32
  * summation order.  Returns TWEO_ERR_INVALID_ARG for an unknown (or retired:
  * 2, 5, 7, 9, 10, 12) variant.

@@ -1,7 +1,6 @@
 // Launches of the gated feed-forward's two products (gemm_gated.h): on the deferred-epilogue kernel (gemm_defer.h, GATE) where there are
 // tiles and stages enough, else on the ring kernel's tiles (gemm_ring.h).
 #include <algorithm>
-#include <cmath>
 #include "gemm_defer.h"
 #include "gemm_ring.h"
 
@@ -93,26 +92,58 @@ static bool shape_fits(int shape, int64_t M, int64_t F, int64_t K, bool int8)
     return true;
 }
 
-static int pick_shape(int64_t M, int64_t F, int64_t K, bool int8)
+// Per shape, us: a launch; a 128-byte stage with one workgroup on a CU and with two; the end of a round (its epilogue and the next
+// tile's first operands), more with both projections stored; how much longer a stage of rows takes that are no whole lines, no whole halves of
+// them; TB/s at which operands and results move at best, and the weights under one row of tiles (0.036 a workgroup).  Fitted to 420 shapes of 1 to 16384 rows, 128 to 14336 columns and contractions of
+// 128 to 8192, operands cold (10 % rms; the choice costs 1.8 % against the fastest in the geometric mean, 22 % at worst).  What it
+// decides, us: 1x5632 under 2048 6.3 on 64x64 tiles in two groups and 9.1 on 64x128; 512x2048 under 768 6.5 and 6.1; 926x7680 under 256 25.6
+// on 64x64 tiles and 17.0 on 128x128; 1395x9248 under 3616 156 on 128x128 tiles and 118 on 192x256; 768x9728 under 5632 98, 106 and on whole
+// 256x256 tiles 69.  INT8: 64x11008 under 4096 24.3 on 64x64 tiles and 21.8 on 64x128 in two groups, 256 rows 51 and on 128x128 42.
+struct GatedRate {
+    int bm, bn, per_cu;
+    double launch, one, two, round, keep, halves, pieces, tb, stream;
+};
+static const GatedRate kFp8Rates[kGatedShapes] = {
+    {64, 64, 2, 2.3, 0.144, 0.380, 1.3, 0.3, 1.17, 1.28, 5.1, 4.8},   {64, 64, 1, 2.0, 0.121, 0.217, 1.7, 0.3, 1.21, 1.35, 5.2, 6.0},
+    {64, 128, 2, 1.7, 0.266, 0.601, 1.8, 0.2, 1.13, 1.32, 3.75, 5.0}, {64, 128, 1, 1.3, 0.239, 0.338, 2.4, 0.3, 1.21, 1.39, 4.1, 5.3},
+    {128, 128, 2, 0.9, 0.596, 1.027, 2.5, 0.0, 1.08, 1.20, 2.9, 3.5}, {256, 256, 1, 0.5, 1.071, 1.071, 7.2, 0.0, 1.0, 1.0, 3.3, 3.3},
+    {192, 256, 1, 0.5, 0.889, 0.889, 5.3, 0.0, 1.0, 1.23, 4.5, 4.5},
+};
+static const GatedRate kInt8Rates[kGatedShapes] = {
+    {64, 64, 2, 2.2, 0.176, 0.394, 1.6, 0.0, 1.30, 1.27, 4.7, 5.2},   {64, 64, 1, 1.8, 0.158, 0.229, 2.1, 0.0, 1.30, 1.31, 4.45, 5.6},
+    {64, 128, 2, 1.7, 0.269, 0.616, 2.4, 0.0, 1.38, 1.40, 4.4, 5.35},  {64, 128, 1, 1.5, 0.239, 0.345, 2.9, 0.0, 1.48, 1.57, 4.6, 5.8},
+    {128, 128, 2, 0.9, 0.553, 1.010, 3.5, 0.0, 1.14, 1.27, 2.65, 3.5}, {}, {},
+};
+
+static int pick_shape(int64_t M, int64_t F, int64_t K, bool int8, bool keep)
 {
-    const int64_t tiles = ((M + 63) / 64) * ((F + 31) / 32);
+    const int64_t cus = num_cus_public(), kt = (K + 127) / 128;
     const int forced = gemm_tile_override();
-    for (int i = 0; forced != 0 && i < kGatedShapes; ++i) {
+    int best = kGated64x64;
+    double least = 1e300;
+    for (int i = 0; i < kGatedShapes; ++i) {
         static const int variant[kGatedShapes] = {4, 18, 19, 20, 21, 15, 24};
-        if (variant[i] == forced && shape_fits(i, M, F, K, int8))
+        if (!shape_fits(i, M, F, K, int8))
+            continue;
+        if (variant[i] == forced)
             return i;
+        const GatedRate &r = (int8 ? kInt8Rates : kFp8Rates)[i];
+        const int64_t tiles = ((M + r.bm - 1) / r.bm) * ((2 * F + r.bn - 1) / r.bn), slots = r.per_cu * cus;
+        const double rounds = (double)((tiles + slots - 1) / slots), ragged = K % 128 == 0 ? 1.0 : K % 64 == 0 ? r.halves : r.pieces;
+        const double mb = ((double)M * K + 2.0 * F * K + 2.0 * M * F * (keep ? 3 : 1)) * 1e-6;
+        const double us = std::max(r.launch + rounds * ((tiles <= cus ? r.one : r.two) * ragged * kt + r.round + (keep ? r.keep : 0.0)), 3.0 + mb / (M <= r.bm ? std::min(r.stream, 0.036 * (double)tiles) : r.tb));
+        if (us < least) {
+            least = us;
+            best = i;
+        }
     }
-    if (tiles <= num_cus_public())
-        return kGated64x64g2;
-    if (M <= 64 || tiles <= 2 * num_cus_public())
-        return kGated64x64;
-    return kGated128x128x2;
+    return best;
 }
 
 hipError_t launch_fp8_gated(const GemmArgs &a, bool gelu, void *gu, hipStream_t s)
 {
     const GatedDev gd{(uint16_t *)gu, gate_coef(gelu)};
-    const int shape = pick_shape(a.M, a.N, a.K, false);
+    const int shape = pick_shape(a.M, a.N, a.K, false, gu != nullptr);
     if (shape == kGated192)
         return launch_defer_any_gated(a, gelu, gd, s);
     if (shape != kGated256)
@@ -124,7 +155,7 @@ hipError_t launch_fp8_gated(const GemmArgs &a, bool gelu, void *gu, hipStream_t 
 
 hipError_t launch_i8_gated(const GemmArgs &a, bool gelu, hipStream_t s)
 {
-    return launch_ring_shape<true>(a, GatedDev{nullptr, gate_coef(gelu)}, pick_shape(a.M, a.N, a.K, true), s);
+    return launch_ring_shape<true>(a, GatedDev{nullptr, gate_coef(gelu)}, pick_shape(a.M, a.N, a.K, true, false), s);
 }
 
 }  // namespace tweo
