@@ -9,6 +9,7 @@ time - there is no fallback path.
 import ctypes
 import functools
 import os
+import struct
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libtweo_hip.so")
@@ -662,37 +663,53 @@ def tweo_rotary_freqs(rot_dim, base=10000.0, kind="plain", factor=1.0, context=0
 
 
 def _heads(device, shape, tensors, names):
-    """Refuses heads that are no [tokens, heads, dim] of bf16 on the current device with a contiguous last index."""
-    bf16 = _types()[0]
+    """Strides of heads, [tokens, heads, dim] of bf16 on the current device with a contiguous last index; refuses others."""
+    bf16, strides = _types()[0], []
     for i, t in enumerate(tensors):
-        if t.dtype is not bf16 or t.shape != shape or t.stride(2) != 1 and shape[2] != 1 or t.get_device() != device:
-            raise ValueError("%s: a %s tensor of shape %s on cuda:%d, the current device, with a contiguous last index is needed, got %s of %s, strides %s, on %s" %
-                             (names[i], bf16, tuple(shape), device, t.dtype, tuple(t.shape), t.stride(), t.device))
+        if t.dtype is bf16 and t.shape == shape and t.get_device() == device:
+            token, head, last = t.stride()
+            if last == 1 or shape[2] == 1:
+                strides += (token, head)
+                continue
+        raise ValueError("%s: a %s tensor of shape %s on cuda:%d, the current device, with a contiguous last index is needed, got %s of %s, strides %s, on %s" %
+                         (names[i], bf16, tuple(shape), device, t.dtype, tuple(t.shape), t.stride(), t.device))
+    return strides
 
 
-def _rotary(device, shape, positions, freqs, layout, scale):
-    """The rotation, or None where there is none."""
+def _rotary(device, tokens, positions, freqs, layout, scale):
+    """The rotation (a tweo_rotary_cfg), or None where there is none."""
     if positions is None and freqs is None:
         return None
     if layout not in ROTARY_LAYOUTS:
         raise ValueError("layout: halves or pairs is needed, got %r" % (layout,))
-    int64, f64 = _types()[5], _types()[2]
-    _same(device, shape[:1], int64, (positions,), ("positions",))
     if freqs is None or positions is None:
         raise ValueError("positions and freqs are needed together")
-    if freqs.dtype is not f64 or freqs.dim() != 1 or not freqs.is_contiguous() or freqs.get_device() != device:
+    types = _types()
+    _same(device, (tokens,), types[5], (positions,), ("positions",))
+    if freqs.dtype is not types[2] or freqs.dim() != 1 or not freqs.is_contiguous() or freqs.get_device() != device:
         raise ValueError("freqs: a contiguous %s vector on cuda:%d, the current device, is needed, got %s of %s on %s" %
-                         (f64, device, freqs.dtype, tuple(freqs.shape), freqs.device))
-    return ctypes.byref(RotaryCfg(positions.data_ptr(), freqs.data_ptr(), 2 * freqs.numel(), ROTARY_LAYOUTS[layout], scale))
+                         (types[2], device, freqs.dtype, tuple(freqs.shape), freqs.device))
+    return _ROTARY_CFG.pack(positions.data_ptr(), freqs.data_ptr(), 2 * freqs.numel(), ROTARY_LAYOUTS[layout], scale)
 
 
-def _groups(groups, width):
-    if not 1 <= len(groups) <= 2 or any(len(g) != width for g in groups):
-        raise ValueError("one or two groups of %d tensors are needed" % width)
-    shape = groups[0][0].shape
-    if len(shape) != 3 or any(g[0].dim() != 3 or g[0].shape[0] != shape[0] or g[0].shape[2] != shape[2] for g in groups):
-        raise ValueError("heads: [tokens, heads, dim] of the same tokens and dim are needed, got %s" % ", ".join(str(tuple(g[0].shape)) for g in groups))
-    return shape
+# tweo_rotary_cfg; one and two of tweo_heads and of tweo_heads_grad.  Packed bytes in the place of ctypes structures: two groups' fields, set one by
+# one, took 5 of the 14 us that issuing a rotation took.
+_ROTARY_CFG = struct.Struct("PPiif4x")
+_ROWS, _GRAD_ROWS = ([struct.Struct(row * n) for n in range(3)] for row in ("PPqqqqPi4x", "PPPqqqqqqPPi4x"))
+
+
+def _shape(groups, width):
+    """Shapes of one or two groups' heads, of the same tokens and dim."""
+    if len(groups) == 1 and len(groups[0]) == width:
+        shapes = (groups[0][0].shape,)
+        if len(shapes[0]) == 3:
+            return shapes
+    elif len(groups) == 2 and len(groups[0]) == len(groups[1]) == width:
+        shapes = a, b = groups[0][0].shape, groups[1][0].shape
+        if len(a) == len(b) == 3 and a[0] == b[0] and a[2] == b[2]:
+            return shapes
+    raise ValueError("one or two groups of %d tensors, the heads [tokens, heads, dim] of the same tokens and dim, are needed, got %s" %
+                     (width, ", ".join("%d, %s" % (len(g), tuple(g[0].shape)) for g in groups) or "none"))
 
 
 _HEADS, _HEADS_GRAD, _GAIN, _DGAIN = ("x", "y"), ("dy", "x", "dx"), ("gain",), ("dgain",)
@@ -701,49 +718,47 @@ _HEADS, _HEADS_GRAD, _GAIN, _DGAIN = ("x", "y"), ("dy", "x", "dx"), ("gain",), (
 def tweo_rotary(groups, positions, freqs, layout="halves", scale=1.0, transpose=False):
     """groups: one or two (x, y), bf16 [tokens, heads, dim] of any token and head stride; y may be x.  positions: int64 [tokens], negative:
     padding.  freqs: float64 [rot_dim / 2] (tweo_rotary_freqs)."""
-    shape, dev = _groups(groups, 2), _device()
-    cfg = _rotary(dev, shape, positions, freqs, layout, scale)
+    shapes, dev = _shape(groups, 2), _device()
+    tokens, _, dim = shapes[0]
+    cfg = _rotary(dev, tokens, positions, freqs, layout, scale)
     if cfg is None:
         raise ValueError("positions and freqs are needed")
-    rows = (Heads * len(groups))()
-    for row, (x, y) in zip(rows, groups):
-        _heads(dev, x.shape, (x, y), _HEADS)
-        row.x, row.y, row.heads = x.data_ptr(), y.data_ptr(), x.shape[1]
-        row.x_token, row.x_head, _ = x.stride()
-        row.y_token, row.y_head, _ = y.stride()
-    _check(load().tweo_rotary(rows, len(groups), shape[0], shape[2], cfg, 1 if transpose else 0, _stream()), "tweo_rotary")
+    fields = []
+    for shape, (x, y) in zip(shapes, groups):
+        fields += (x.data_ptr(), y.data_ptr(), *_heads(dev, shape, (x, y), _HEADS), 0, shape[1])
+    _check(load().tweo_rotary(_ROWS[len(groups)].pack(*fields), len(groups), tokens, dim, cfg, 1 if transpose else 0, _stream()), "tweo_rotary")
 
 
 def tweo_head_norm_rotary_fwd(groups, positions=None, freqs=None, layout="halves", scale=1.0, eps=1e-6):
     """groups: one or two (x, gain, y); x and y as in tweo_rotary, gain bf16 [dim] or None.  Without positions and freqs the norm alone."""
-    shape, dev = _groups(groups, 3), _device()
-    cfg = _rotary(dev, shape, positions, freqs, layout, scale)
-    rows = (Heads * len(groups))()
-    for row, (x, gain, y) in zip(rows, groups):
-        _heads(dev, x.shape, (x, y), _HEADS)
-        _same(dev, shape[2:], _types()[0], (gain,), _GAIN)
-        row.x, row.y, row.gain, row.heads = x.data_ptr(), y.data_ptr(), _ptr(gain), x.shape[1]
-        row.x_token, row.x_head, _ = x.stride()
-        row.y_token, row.y_head, _ = y.stride()
-    _check(load().tweo_head_norm_rotary_fwd(rows, len(groups), shape[0], shape[2], eps, cfg, _stream()), "tweo_head_norm_rotary_fwd")
+    shapes, dev, bf16 = _shape(groups, 3), _device(), _types()[0]
+    tokens, _, dim = shapes[0]
+    cfg = _rotary(dev, tokens, positions, freqs, layout, scale)
+    fields = []
+    for shape, (x, gain, y) in zip(shapes, groups):
+        if gain is not None:
+            _same(dev, (dim,), bf16, (gain,), _GAIN)
+        fields += (x.data_ptr(), y.data_ptr(), *_heads(dev, shape, (x, y), _HEADS), 0 if gain is None else gain.data_ptr(), shape[1])
+    _check(load().tweo_head_norm_rotary_fwd(_ROWS[len(groups)].pack(*fields), len(groups), tokens, dim, eps, cfg, _stream()), "tweo_head_norm_rotary_fwd")
 
 
 def tweo_head_norm_rotary_bwd(groups, positions=None, freqs=None, layout="halves", scale=1.0, eps=1e-6, workspace=None):
     """groups: one or two (dy, x, gain, dx, dgain): the gradient of the forward's y, its x and gain, where the gradient of x goes (dy or x
     itself, or another) and that of gain (float32 [dim], or None)."""
-    shape, dev = _groups(groups, 5), _device()
-    cfg = _rotary(dev, shape, positions, freqs, layout, scale)
-    rows = (HeadsGrad * len(groups))()
-    for row, (dy, x, gain, dx, dgain) in zip(rows, groups):
-        _heads(dev, dy.shape, (dy, x, dx), _HEADS_GRAD)
-        _same(dev, shape[2:], _types()[0], (gain,), _GAIN)
-        _same(dev, shape[2:], _types()[1], (dgain,), _DGAIN)
-        row.dy, row.x, row.dx, row.gain, row.dgain, row.heads = dy.data_ptr(), x.data_ptr(), dx.data_ptr(), _ptr(gain), _ptr(dgain), dy.shape[1]
-        row.dy_token, row.dy_head, _ = dy.stride()
-        row.x_token, row.x_head, _ = x.stride()
-        row.dx_token, row.dx_head, _ = dx.stride()
+    shapes, dev, (bf16, f32) = _shape(groups, 5), _device(), _types()[:2]
+    tokens, _, dim = shapes[0]
+    cfg = _rotary(dev, tokens, positions, freqs, layout, scale)
+    fields = []
+    for shape, (dy, x, gain, dx, dgain) in zip(shapes, groups):
+        if gain is not None:
+            _same(dev, (dim,), bf16, (gain,), _GAIN)
+        if dgain is not None:
+            _same(dev, (dim,), f32, (dgain,), _DGAIN)
+        fields += (dy.data_ptr(), x.data_ptr(), dx.data_ptr(), *_heads(dev, shape, (dy, x, dx), _HEADS_GRAD), 0 if gain is None else gain.data_ptr(),
+                   0 if dgain is None else dgain.data_ptr(), shape[1])
     wp, wb = _scratch(dev, workspace, "workspace")
-    _check(load().tweo_head_norm_rotary_bwd(rows, len(groups), shape[0], shape[2], eps, cfg, wp, wb, _stream()), "tweo_head_norm_rotary_bwd")
+    _check(load().tweo_head_norm_rotary_bwd(_GRAD_ROWS[len(groups)].pack(*fields), len(groups), tokens, dim, eps, cfg, wp, wb, _stream()),
+           "tweo_head_norm_rotary_bwd")
 
 
 ACTS = {"silu": 0, "gelu": 1}  # TWEO_ACT_SILU, TWEO_ACT_GELU
@@ -757,9 +772,10 @@ def _act(act):
 
 def _gated_shape(x, w, names):
     """M, F, K of [M, K] and [2F, K]."""
-    if x.dim() != 2 or w.dim() != 2 or x.shape[1] != w.shape[1] or w.shape[0] % 2 != 0:
-        raise ValueError("%s, %s: [M, K] and [2F, K] are needed, got %s and %s" % (names + (tuple(x.shape), tuple(w.shape))))
-    return x.shape[0], w.shape[0] // 2, x.shape[1]
+    a, b = x.shape, w.shape
+    if len(a) != 2 or len(b) != 2 or a[1] != b[1] or b[0] % 2 != 0:
+        raise ValueError("%s, %s: [M, K] and [2F, K] are needed, got %s and %s" % (names + (tuple(a), tuple(b))))
+    return a[0], b[0] // 2, a[1]
 
 
 @functools.lru_cache(maxsize=1)
@@ -790,7 +806,8 @@ def tweo_fp8_gated_fwd(xq, sx_inv, wq, sw_inv, h_bf16, gu_bf16=None, act="silu")
     _same(dev, (M, K), u8, (xq,), _XQ)
     _same(dev, (2 * F, K), u8, (wq,), _WQ)
     _same(dev, (M, F), bf16, (h_bf16,), _HB)
-    _same(dev, (M, 2 * F), bf16, (gu_bf16,), _GU)
+    if gu_bf16 is not None:
+        _same(dev, (M, 2 * F), bf16, (gu_bf16,), _GU)
     _scalar(dev, sx_inv, "sx_inv")
     _scalar(dev, sw_inv, "sw_inv")
     _check(load().tweo_fp8_gated_fwd(_ptr(xq), _ptr(sx_inv), _ptr(wq), _ptr(sw_inv), M, F, K, _act(act), _ptr(h_bf16), _ptr(gu_bf16), _stream()),
