@@ -665,14 +665,14 @@ def tweo_rotary_freqs(rot_dim, base=10000.0, kind="plain", factor=1.0, context=0
 def _heads(device, shape, tensors, names):
     """Strides of heads, [tokens, heads, dim] of bf16 on the current device with a contiguous last index; refuses others."""
     bf16, strides = _types()[0], []
-    for i, t in enumerate(tensors):
-        if t.dtype is bf16 and t.shape == shape and t.get_device() == device:
-            token, head, last = t.stride()
-            if last == 1 or shape[2] == 1:
-                strides += (token, head)
-                continue
-        raise ValueError("%s: a %s tensor of shape %s on cuda:%d, the current device, with a contiguous last index is needed, got %s of %s, strides %s, on %s" %
-                         (names[i], bf16, tuple(shape), device, t.dtype, tuple(t.shape), t.stride(), t.device))
+    for t in tensors:
+        token, head, last = t.stride() if t.dim() == 3 else (0, 0, 0)
+        if t.dtype is not bf16 or t.shape != shape or last != 1 and shape[2] != 1 or t.get_device() != device:
+            i = [u is t for u in tensors].index(True)
+            raise ValueError("%s: a %s tensor of shape %s on cuda:%d, the current device, with a contiguous last index is needed, got %s of %s, strides %s, on %s" %
+                             (names[i], bf16, tuple(shape), device, t.dtype, tuple(t.shape), t.stride(), t.device))
+        strides.append(token)
+        strides.append(head)
     return strides
 
 
@@ -680,15 +680,15 @@ def _rotary(device, tokens, positions, freqs, layout, scale):
     """The rotation (a tweo_rotary_cfg), or None where there is none."""
     if positions is None and freqs is None:
         return None
+    _, _, f64, _, _, i64 = _types()
+    if (positions is None or freqs is None or positions.dtype is not i64 or positions.shape != (tokens,) or freqs.dtype is not f64 or
+            positions.get_device() != device or freqs.get_device() != device or not positions.is_contiguous() or freqs.dim() != 1 or
+            not freqs.is_contiguous()):
+        raise ValueError("positions and freqs: contiguous vectors on cuda:%d, the current device, are needed, %d of %s and rot_dim / 2 of %s, got %s" %
+                         (device, tokens, i64, f64, " and ".join("None" if t is None else "%s of %s on %s" % (tuple(t.shape), t.dtype, t.device)
+                                                                 for t in (positions, freqs))))
     if layout not in ROTARY_LAYOUTS:
         raise ValueError("layout: halves or pairs is needed, got %r" % (layout,))
-    if freqs is None or positions is None:
-        raise ValueError("positions and freqs are needed together")
-    types = _types()
-    _same(device, (tokens,), types[5], (positions,), ("positions",))
-    if freqs.dtype is not types[2] or freqs.dim() != 1 or not freqs.is_contiguous() or freqs.get_device() != device:
-        raise ValueError("freqs: a contiguous %s vector on cuda:%d, the current device, is needed, got %s of %s on %s" %
-                         (types[2], device, freqs.dtype, tuple(freqs.shape), freqs.device))
     return _ROTARY_CFG.pack(positions.data_ptr(), freqs.data_ptr(), 2 * freqs.numel(), ROTARY_LAYOUTS[layout], scale)
 
 

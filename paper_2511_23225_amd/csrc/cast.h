@@ -82,9 +82,10 @@ __device__ __forceinline__ void transpose4x4_bytes(uint32_t a, uint32_t b, uint3
 // fixed before this tensor was seen and wants this tensor's amax back for the history: DELAYED
 // kernels read the scale itself from `amax`, and add the maximum magnitude pattern of what they
 // load to *amax_acc (one atomicMax per workgroup, skipped when already covered).
+template <int WAVES = kQuantThreads / kWave>
 __device__ __forceinline__ void quant_amax_commit(uint32_t m, uint32_t *amax_acc)
 {
-    __shared__ uint32_t red[kQuantThreads / kWave];
+    __shared__ uint32_t red[WAVES];
     uint32_t r = (m & 0xFFFFu) > (m >> 16) ? (m & 0xFFFFu) : (m >> 16);
     r = wave_reduce_max_u32(r);
     if ((threadIdx.x & (kWave - 1)) == 0)
@@ -92,7 +93,7 @@ __device__ __forceinline__ void quant_amax_commit(uint32_t m, uint32_t *amax_acc
     __syncthreads();
     if (threadIdx.x == 0) {
 #pragma unroll
-        for (int w = 1; w < kQuantThreads / kWave; ++w)
+        for (int w = 1; w < WAVES; ++w)
             r = red[w] > r ? red[w] : r;
         const uint32_t mine = r << 16;
         if (mine > __atomic_load_n(amax_acc, __ATOMIC_RELAXED))

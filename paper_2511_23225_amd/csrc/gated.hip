@@ -15,7 +15,7 @@ namespace tweo {
 
 int num_cus_public();
 
-constexpr int kGatedTile = 128;
+constexpr int kGatedTile = 128, kGatedCols = 4;
 
 struct GatedGradDev {
     const uint16_t *dh, *gu;
@@ -39,45 +39,74 @@ __device__ __forceinline__ void gated_grad_one(float dh, float g, float u, const
     dg = dh * u * __builtin_fmaf(gp * (1.0f - p), __builtin_fmaf(c.slope1, b * b, c.slope0), p);
 }
 
-__device__ __forceinline__ void gated_grad_vec(uint4 dh, uint4 g, uint4 u, const GatedGradDev &c, uint4 &dg, uint4 &du)
+// W elements (a pair a word): g becomes dg, u du
+template <int N>
+struct Words {
+    uint32_t w[N];
+};
+template <int N>
+__device__ __forceinline__ Words<N> load_words(const uint16_t *p)
 {
-    const uint32_t d[4] = {dh.x, dh.y, dh.z, dh.w}, gg[4] = {g.x, g.y, g.z, g.w}, uu[4] = {u.x, u.y, u.z, u.w};
-    uint32_t a[4], b[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        float dg0, dg1, du0, du1;
-        gated_grad_one(bf16lo_to_f32(d[k]), bf16lo_to_f32(gg[k]), bf16lo_to_f32(uu[k]), c, dg0, du0);
-        gated_grad_one(bf16hi_to_f32(d[k]), bf16hi_to_f32(gg[k]), bf16hi_to_f32(uu[k]), c, dg1, du1);
-        a[k] = pack_bf16x2(dg0, dg1);
-        b[k] = pack_bf16x2(du0, du1);
+    static_assert(N == 2 || N == 4, "8 or 16 bytes");
+    Words<N> r;
+    if constexpr (N == 4) {
+        const uint4 v = *(const uint4 *)p;
+        r = {{v.x, v.y, v.z, v.w}};
+    } else {
+        const uint2 v = *(const uint2 *)p;
+        r = {{v.x, v.y}};
     }
-    dg = make_uint4(a[0], a[1], a[2], a[3]);
-    du = make_uint4(b[0], b[1], b[2], b[3]);
+    return r;
+}
+template <int N>
+__device__ __forceinline__ void gated_grad_words(const Words<N> &dh, Words<N> &g, Words<N> &u, const GatedGradDev &c)
+{
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        float dg0, dg1, du0, du1;
+        gated_grad_one(bf16lo_to_f32(dh.w[k]), bf16lo_to_f32(g.w[k]), bf16lo_to_f32(u.w[k]), c, dg0, du0);
+        gated_grad_one(bf16hi_to_f32(dh.w[k]), bf16hi_to_f32(g.w[k]), bf16hi_to_f32(u.w[k]), c, dg1, du1);
+        g.w[k] = pack_bf16x2(dg0, dg1);
+        u.w[k] = pack_bf16x2(du0, du1);
+    }
 }
 
 enum GatedPass { kGatedAmax, kGatedCast, kGatedDelayed };
 
-// A workgroup takes tiles of 128 rows by 128 columns of h, a lane 8x8 elements of one, whose codes of dg and du lie F columns apart.
-template <int PASS, bool E5M2>
-__global__ __launch_bounds__(kQuantThreads) void gated_grad_kernel(GatedGradDev c)
+// rows of a tile and threads of its workgroup
+constexpr int gated_rows(int pass, bool small) { return !small ? 128 : pass == kGatedAmax ? 32 : 64; }
+constexpr int gated_threads(int pass, bool small) { return kGatedTile / kGatedCols * (gated_rows(pass, small) / (small && pass == kGatedAmax ? 2 : 8)); }
+
+// A workgroup takes tiles of 128 rows by 128 columns of h, a lane 8 rows by 4 columns of one, whose codes of dg and du lie F columns apart.
+// (Lanes of 8 by 8, 16-byte loads, have half the waves a SIMD: 16384x5632 both passes 10 us more.)
+// SMALL: tiles for fewer than two workgroups a CU.  The maximum takes 32 rows at a time (2 a lane), the cast 64 (half as many lanes), whose pieces of
+// the transposed copy are half lines.  1024x2048, 128 tiles of 128 rows: 6.2 and 10.1 us, now 5.1 and 9.2.
+template <int PASS, bool E5M2, bool SMALL>
+__global__ __launch_bounds__(gated_threads(PASS, SMALL)) void gated_grad_kernel(GatedGradDev c)
 {
-    __shared__ uint4 turned[PASS == kGatedAmax ? 1 : 2 * kGatedTile * kGatedTile / 16];
-    __shared__ uint32_t red[kQuantThreads / kWave];
-    const int t = threadIdx.x, cg = t & 15, rg = t >> 4;
+    constexpr int THREADS = gated_threads(PASS, SMALL), W = kGatedCols, ACROSS = kGatedTile / W, N = W / 2, WAVES = THREADS / kWave;
+    constexpr int ROWS = SMALL && PASS == kGatedAmax ? 2 : 8, TILE_ROWS = gated_rows(PASS, SMALL), PIECES = TILE_ROWS / 16;
+    static_assert(THREADS == TILE_ROWS / ROWS * ACROSS, "a lane's block");
+    __shared__ uint4 turned[PASS == kGatedAmax ? 1 : 2 * kGatedTile * PIECES];
+    __shared__ uint32_t red[WAVES];
+    const int t = threadIdx.x, cg = t % ACROSS, rg = t / ACROSS;
     const int64_t wide = 2 * c.cols;
     uint32_t mx = 0;
     float scale = 0.0f;
     bool have_scale = PASS == kGatedAmax;
     for (int64_t tile = blockIdx.x; tile < c.tiles; tile += gridDim.x) {
-        const int64_t R = tile / c.tiles_x * kGatedTile, C = tile % c.tiles_x * kGatedTile, r0 = R + rg * 8, c0 = C + cg * 8;
-        const bool active = r0 < c.rows && c0 < c.cols;  // whole 8x8 blocks: in or out
+        // the cast goes the other way: what the first pass read last may still be in the memory-side cache (16384x5632 both passes
+        // 290 us, 280)
+        const int64_t id = PASS == kGatedCast ? c.tiles - 1 - tile : tile;
+        const int64_t R = id / c.tiles_x * TILE_ROWS, C = id % c.tiles_x * kGatedTile, r0 = R + rg * ROWS, c0 = C + cg * W;
+        const bool active = r0 < c.rows && c0 < c.cols;  // whole blocks: in or out
         const uint16_t *dh = c.dh + (active ? r0 * c.cols + c0 : 0), *g = c.gu + (active ? r0 * wide + c0 : 0);
-        uint4 a[8], b[8], d[8];
+        Words<N> a[ROWS], b[ROWS], d[ROWS];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            d[i] = *(const uint4 *)(dh + i * c.cols);
-            a[i] = *(const uint4 *)(g + i * wide);
-            b[i] = *(const uint4 *)(g + i * wide + c.cols);
+        for (int i = 0; i < ROWS; ++i) {
+            d[i] = load_words<N>(dh + i * c.cols);
+            a[i] = load_words<N>(g + i * wide);
+            b[i] = load_words<N>(g + i * wide + c.cols);
         }
         if (!have_scale) {  // behind the first loads, so that the latencies overlap
             have_scale = true;
@@ -85,14 +114,14 @@ __global__ __launch_bounds__(kQuantThreads) void gated_grad_kernel(GatedGradDev 
                 scale = *c.scale;
             } else {
                 uint32_t m = 0;
-                for (int i = t; i < c.n_partials; i += kQuantThreads)
+                for (int i = t; i < c.n_partials; i += THREADS)
                     m = max(m, c.partials[i]);
                 m = wave_reduce_max_u32(m);
                 if ((t & (kWave - 1)) == 0)
                     red[t / kWave] = m;
                 __syncthreads();
 #pragma unroll
-                for (int w = 0; w < kQuantThreads / kWave; ++w)
+                for (int w = 0; w < WAVES; ++w)
                     m = max(m, red[w]);
                 scale = scale_f8<E5M2>(bits_to_f32(m));
                 if (blockIdx.x == 0 && t == 0) {
@@ -103,13 +132,15 @@ __global__ __launch_bounds__(kQuantThreads) void gated_grad_kernel(GatedGradDev 
             }
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            gated_grad_vec(d[i], a[i], b[i], c, a[i], b[i]);
+        for (int i = 0; i < ROWS; ++i)
+            gated_grad_words<N>(d[i], a[i], b[i], c);
         if constexpr (PASS != kGatedCast) {
             uint32_t m = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                m = pk_absmax4(pk_absmax4(m, a[i]), b[i]);
+            for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+                for (int k = 0; k < N; ++k)
+                    m = pk_absmax(pk_absmax(m, a[i].w[k]), b[i].w[k]);
             mx = active ? pk_absmax(m, mx) : mx;
         }
         if constexpr (PASS != kGatedAmax) {
@@ -118,31 +149,37 @@ __global__ __launch_bounds__(kQuantThreads) void gated_grad_kernel(GatedGradDev 
             uint8_t *q = c.q + (active ? r0 * wide + c0 : 0);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                uint32_t lo[8], hi[8];
+                uint32_t code[N / 2][8];  // four columns each, by rows
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const uint4 v = half ? b[i] : a[i];
-                    lo[i] = cvt4_f8<E5M2>(bf16lo_to_f32(v.x) * scale, bf16hi_to_f32(v.x) * scale, bf16lo_to_f32(v.y) * scale, bf16hi_to_f32(v.y) * scale);
-                    hi[i] = cvt4_f8<E5M2>(bf16lo_to_f32(v.z) * scale, bf16hi_to_f32(v.z) * scale, bf16lo_to_f32(v.w) * scale, bf16hi_to_f32(v.w) * scale);
-                    if (active)
-                        *(uint2 *)(q + i * wide + half * c.cols) = make_uint2(lo[i], hi[i]);
-                }
-                uint32_t ta[8], tb[8];  // column j of the block: rows 0-3, rows 4-7
-                transpose4x4_bytes(lo[0], lo[1], lo[2], lo[3], ta[0], ta[1], ta[2], ta[3]);
-                transpose4x4_bytes(hi[0], hi[1], hi[2], hi[3], ta[4], ta[5], ta[6], ta[7]);
-                transpose4x4_bytes(lo[4], lo[5], lo[6], lo[7], tb[0], tb[1], tb[2], tb[3]);
-                transpose4x4_bytes(hi[4], hi[5], hi[6], hi[7], tb[4], tb[5], tb[6], tb[7]);
-                uint8_t *w = (uint8_t *)turned + half * kGatedTile * kGatedTile + cg * 8 * kGatedTile + (((rg >> 1) ^ (cg & 7)) << 4) + (rg & 1) * 8;
+                    const Words<N> &v = half ? b[i] : a[i];
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    *(uint2 *)(w + j * kGatedTile) = make_uint2(ta[j], tb[j]);
+                    for (int k = 0; k < N / 2; ++k)
+                        code[k][i] = cvt4_f8<E5M2>(bf16lo_to_f32(v.w[2 * k]) * scale, bf16hi_to_f32(v.w[2 * k]) * scale,
+                                                   bf16lo_to_f32(v.w[2 * k + 1]) * scale, bf16hi_to_f32(v.w[2 * k + 1]) * scale);
+                    if (active) {
+                        static_assert(W == 4, "a word of codes");
+                        *(uint32_t *)(q + i * wide + half * c.cols) = code[0][i];
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < N / 2; ++k) {
+                    uint32_t ta[4], tb[4];  // column j of the four: rows 0-3, rows 4-7
+                    transpose4x4_bytes(code[k][0], code[k][1], code[k][2], code[k][3], ta[0], ta[1], ta[2], ta[3]);
+                    transpose4x4_bytes(code[k][4], code[k][5], code[k][6], code[k][7], tb[0], tb[1], tb[2], tb[3]);
+                    const int col = cg * W + 4 * k;
+                    uint8_t *w = (uint8_t *)turned + (half * kGatedTile + col) * TILE_ROWS + (((rg >> 1) ^ ((col >> 3) & (PIECES - 1))) << 4) + (rg & 1) * 8;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        *(uint2 *)(w + j * TILE_ROWS) = make_uint2(ta[j], tb[j]);
+                }
             }
             __syncthreads();
-            const int piece = t & 7;
+            const int piece = t % PIECES;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int half = i >> 2, col = (t >> 3) + 32 * (i & 3);
-                const v4i v = __builtin_bit_cast(v4i, turned[half * (kGatedTile * kGatedTile / 16) + col * (kGatedTile / 16) + (piece ^ ((col >> 3) & 7))]);
+            for (int i = 0; i < 2 * kGatedTile * PIECES / THREADS; ++i) {
+                const int at = t / PIECES + THREADS / PIECES * i, half = at / kGatedTile, col = at % kGatedTile;
+                const v4i v = __builtin_bit_cast(v4i, turned[at * PIECES + (piece ^ ((col >> 3) & (PIECES - 1)))]);
                 if (C + col < c.cols && R + piece * 16 < c.rows)
                     *(v4i *)(c.qT + (half * c.cols + C + col) * c.rows + R + piece * 16) = v;
             }
@@ -156,41 +193,48 @@ __global__ __launch_bounds__(kQuantThreads) void gated_grad_kernel(GatedGradDev 
         __syncthreads();
         if (t == 0) {
 #pragma unroll
-            for (int w = 1; w < kQuantThreads / kWave; ++w)
+            for (int w = 1; w < WAVES; ++w)
                 r = max(r, red[w]);
             const_cast<uint32_t *>(c.partials)[blockIdx.x] = r << 16;
         }
     }
     if constexpr (PASS == kGatedDelayed)
-        quant_amax_commit(mx, c.amax_acc);
+        quant_amax_commit<WAVES>(mx, c.amax_acc);
+}
+
+template <int PASS, bool E5M2, bool SMALL>
+static hipError_t launch_pass(GatedGradDev &c, int64_t most, hipStream_t s)
+{
+    c.tiles = c.tiles_x * ((c.rows + gated_rows(PASS, SMALL) - 1) / gated_rows(PASS, SMALL));
+    const unsigned n = (unsigned)std::min(c.tiles, most);
+    if (PASS == kGatedAmax)
+        c.n_partials = (int)n;
+    hipLaunchKernelGGL((gated_grad_kernel<PASS, E5M2, SMALL>), dim3(n), dim3(gated_threads(PASS, SMALL)), 0, s, c);
+    return hipGetLastError();
 }
 
 template <bool E5M2>
 static hipError_t launch_grad(const GatedGradCall &call, GatedGradDev c, hipStream_t s)
 {
-    const unsigned tiles = (unsigned)c.tiles;
+    const bool small = c.tiles_x * ((c.rows + kGatedTile - 1) / kGatedTile) < 2 * (int64_t)num_cus_public();
     // each workgroup ends in a word of its own, or in an atomic: three a CU walk the tiles
-    const unsigned few = (unsigned)std::min<int64_t>({(int64_t)c.tiles, 3 * (int64_t)num_cus_public(), kGatedPartials});
+    const int64_t few = std::min<int64_t>(3 * (int64_t)num_cus_public(), kGatedPartials), all = (int64_t)1 << 31;
     float *state = (float *)call.state;
     if (state != nullptr && !call.bootstrap) {
         c.scale = state + 17;
         c.amax_acc = (uint32_t *)state + 16;
-        hipLaunchKernelGGL((gated_grad_kernel<kGatedDelayed, E5M2>), dim3(few), dim3(kQuantThreads), 0, s, c);
-        const hipError_t e = hipGetLastError();
+        const hipError_t e = launch_pass<kGatedDelayed, E5M2, false>(c, few, s);
         return e == hipSuccess ? launch_delayed_update(state, false, E5M2, nullptr, 0, call.scalars, s) : e;
     }
     c.partials = call.partials;
-    c.n_partials = (int)few;
-    hipLaunchKernelGGL((gated_grad_kernel<kGatedAmax, false>), dim3(few), dim3(kQuantThreads), 0, s, c);
-    hipError_t e = hipGetLastError();
+    hipError_t e = small ? launch_pass<kGatedAmax, false, true>(c, kGatedPartials, s) : launch_pass<kGatedAmax, false, false>(c, few, s);
     if (e == hipSuccess && state != nullptr) {
-        e = launch_delayed_update(state, true, E5M2, call.partials, (int)few, call.scalars, s);
+        e = launch_delayed_update(state, true, E5M2, call.partials, c.n_partials, call.scalars, s);
         c.scale = state + 21;
     }
     if (e != hipSuccess)
         return e;
-    hipLaunchKernelGGL((gated_grad_kernel<kGatedCast, E5M2>), dim3(tiles), dim3(kQuantThreads), 0, s, c);
-    return hipGetLastError();
+    return small ? launch_pass<kGatedCast, E5M2, true>(c, all, s) : launch_pass<kGatedCast, E5M2, false>(c, all, s);
 }
 
 hipError_t launch_gated_grad(const GatedGradCall &call, hipStream_t s)
@@ -201,7 +245,6 @@ hipError_t launch_gated_grad(const GatedGradCall &call, hipStream_t s)
     c.rows = call.M;
     c.cols = call.F;
     c.tiles_x = (call.F + kGatedTile - 1) / kGatedTile;
-    c.tiles = c.tiles_x * ((call.M + kGatedTile - 1) / kGatedTile);
     c.act = gate_coef(call.gelu);
     constexpr double k = 1.5957691216057307118;  // 2 sqrt(2 / pi)
     c.slope0 = call.gelu ? (float)k : 1.0f;

@@ -164,6 +164,16 @@ __device__ __forceinline__ float dpp_add_f32(float v)
     const int o = __builtin_amdgcn_update_dpp((int)f32_to_bits(v), (int)f32_to_bits(v), CTRL, 0xF, 0xF, false);
     return v + bits_to_f32((uint32_t)o);
 }
+// v of this lane and of lane ^ OFF, 16 or 32, without the LDS (through which sixteen sums over three steps took 1 of 8 us)
+template <int OFF>
+__device__ __forceinline__ float add_across(float v)
+{
+    typedef uint32_t pair __attribute__((ext_vector_type(2)));
+    const uint32_t b = f32_to_bits(v);
+    const pair r = OFF == 16 ? __builtin_bit_cast(pair, __builtin_amdgcn_permlane16_swap(b, b, false, false))
+                             : __builtin_bit_cast(pair, __builtin_amdgcn_permlane32_swap(b, b, false, false));
+    return bits_to_f32(r[0]) + bits_to_f32(r[1]);
+}
 template <int LANES>
 __device__ __forceinline__ float team_sum(float v)
 {
@@ -176,11 +186,31 @@ __device__ __forceinline__ float team_sum(float v)
     if constexpr (LANES >= 16)
         v = dpp_add_f32<0x140>(v);  // the other eight of sixteen
     if constexpr (LANES >= 32)
-        v += __shfl_xor(v, 16, kWave);
+        v = add_across<16>(v);
     if constexpr (LANES >= 64)
-        v += __shfl_xor(v, 32, kWave);
+        v = add_across<32>(v);
     return v;
 }
+// over the teams of a wave, lane by lane
+template <int LANES>
+__device__ __forceinline__ float teams_sum(float v)
+{
+    // rows of 16 turned by 8, 4, 2 and 1
+    if constexpr (LANES <= 8)
+        v = dpp_add_f32<0x128>(v);
+    if constexpr (LANES <= 4)
+        v = dpp_add_f32<0x124>(v);
+    if constexpr (LANES <= 2)
+        v = dpp_add_f32<0x122>(v);
+    if constexpr (LANES <= 1)
+        v = dpp_add_f32<0x121>(v);
+    if constexpr (LANES <= 16)
+        v = add_across<16>(v);
+    if constexpr (LANES <= 32)
+        v = add_across<32>(v);
+    return v;
+}
+
 // x becomes xhat.  Squares whose sum leaves fp32 (beyond 2^100, or, without an eps that covers them, below 2^-80) are taken of values
 // moved by a power of two.
 template <int LANES, int PER>
@@ -334,37 +364,32 @@ __global__ __launch_bounds__(kHeadsThreads, 4) void heads_kernel(HeadsDev g)
         }
     }
     if (MODE == kHeadsGrad && g.partials != nullptr) {
-        // over the teams of a wave, then over the waves, in this order
+        // over the teams of a wave, then, column by column, over the waves
         constexpr int WAVES = kHeadsThreads / kWave;
         float *sums = (float *)angles;
-        static_assert(WAVES * LANES * 2 * PER <= 2 * kHeadsAngles, "the angles' room");
-        const int wave = tid / kWave, l = tid & (kWave - 1);
+        static_assert(WAVES * kHeadsMaxDim <= 2 * kHeadsAngles, "the angles' room");
+        const int wave = tid / kWave;
 #pragma unroll
-        for (int e = 0; e < PER; ++e)
-#pragma unroll
-            for (int off = kWave / 2; off >= LANES; off >>= 1) {
-                sa[e] += __shfl_xor(sa[e], off, kWave);
-                sb[e] += __shfl_xor(sb[e], off, kWave);
-            }
+        for (int e = 0; e < PER; ++e) {
+            sa[e] = teams_sum<LANES>(sa[e]);
+            sb[e] = teams_sum<LANES>(sb[e]);
+        }
         __syncthreads();
-        if (l < LANES)
-#pragma unroll
-            for (int e = 0; e < PER; ++e) {
-                sums[(wave * 2 * PER + 2 * e) * LANES + l] = sa[e];
-                sums[(wave * 2 * PER + 2 * e + 1) * LANES + l] = sb[e];
-            }
-        __syncthreads();
-        if (tid < LANES)
+        if ((tid & (kWave - 1)) < LANES)
 #pragma unroll
             for (int e = 0; e < 2 * PER; ++e) {
-                float s = 0.0f;
-#pragma unroll
-                for (int w = 0; w < WAVES; ++w)
-                    s += sums[(w * 2 * PER + e) * LANES + l];
                 const int c = lane.column(e >> 1, e & 1);
                 if (c >= 0)
-                    g.partials[(int64_t)blockIdx.x * g.dim + c] = s;
+                    sums[wave * kHeadsMaxDim + c] = e & 1 ? sb[e >> 1] : sa[e >> 1];
             }
+        __syncthreads();
+        for (int c = tid; c < g.dim; c += kHeadsThreads) {
+            float s = sums[c];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w)
+                s += sums[w * kHeadsMaxDim + c];
+            g.partials[(int64_t)blockIdx.x * g.dim + c] = s;
+        }
     }
 }
 
