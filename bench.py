@@ -305,6 +305,67 @@ def time_training_rest(tw, torch, layers, dev, iters=12):
     return out
 
 
+def time_between_linears(tw, torch, dev, rows=16384, cols=2048, hidden=5632, dim=64, iters=12, sets=3):
+    """What a block runs between its linears, operands cold (three sets in turn): norm and rotation of queries and keys as they lie in the
+    qkv linear's output, its gradients, the gated feed-forward's first half on FP8 codes and its backward pass.  Rates: the bytes, or the
+    products, that each can not do without."""
+    g = torch.Generator(device=dev)
+    g.manual_seed(13)
+    heads = cols // dim
+    bf = lambda *shape: torch.randn(shape, device=dev, generator=g).to(torch.bfloat16)  # noqa: E731
+    s, e = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+
+    def timed(fn, nbytes=None, flops=None):
+        for k in range(sets):
+            fn(k)
+        s.record()
+        for k in range(iters):
+            fn(k % sets)
+        e.record()
+        torch.cuda.synchronize()
+        us = s.elapsed_time(e) / iters * 1e3
+        if flops:
+            return {"us": round(us, 2), "TFLOP/s": round(flops / us / 1e6, 1), "frac_of_fp8_peak": round(flops / us / 1e6 / FP8_PEAK_TFLOPS, 4)}
+        return {"us": round(us, 2), "GB/s": round(nbytes / us / 1e3, 1), "frac_of_hbm_peak": round(nbytes / us / 1e3 / HBM_PEAK_GBS, 3)}
+
+    out = {"heads": "%d tokens x 2 x %d of %d" % (rows, heads, dim), "gated": "%dx%d -> %d" % (rows, cols, hidden)}
+    freqs, positions = tw.tweo_rotary_freqs(dim).to(dev), torch.arange(rows, device=dev) % 4096
+    gain, dgain = [bf(dim) for _ in range(2)], [torch.empty(dim, device=dev) for _ in range(2)]
+    ws = torch.empty(tw.tweo_workspace_bytes(tw.TWEO_OP_HEAD_NORM_ROTARY_BWD, rows, 2 * heads, dim), dtype=torch.uint8, device=dev)
+    qkv, y, dy = ([bf(rows, n * cols) for _ in range(sets)] for n in (3, 2, 2))
+    parts = lambda t: [t[:, i * cols:(i + 1) * cols].unflatten(1, (heads, dim)) for i in range(2)]  # noqa: E731
+    n = 2 * rows * cols
+    out["rotary"] = timed(lambda k: tw.tweo_rotary(list(zip(parts(qkv[k]), parts(y[k]))), positions, freqs), 4 * n)
+    out["head_norm_rotary_fwd"] = timed(lambda k: tw.tweo_head_norm_rotary_fwd(list(zip(parts(qkv[k]), gain, parts(y[k]))), positions, freqs), 4 * n)
+    out["head_norm_rotary_bwd"] = timed(lambda k: tw.tweo_head_norm_rotary_bwd(list(zip(parts(dy[k]), parts(qkv[k]), gain, parts(y[k]), dgain)), positions, freqs,
+                                                                               workspace=ws), 6 * n)
+    del qkv, y, dy
+    u8 = lambda *shape: torch.empty(shape, dtype=torch.uint8, device=dev)  # noqa: E731
+    F, ops = hidden, (tw.TWEO_OP_FP8_GATED_FWD_BF16, tw.TWEO_OP_FP8_GATED_BWD_BF16)
+    ws = u8(max(tw.tweo_workspace_bytes(op, rows, F, cols) for op in ops))
+    t = []
+    for _ in range(sets):
+        x, w = bf(rows, cols), (bf(2 * F, cols) * 0.02).to(torch.bfloat16)
+        buf, sc, h, gu = [u8(rows, cols), u8(cols, rows), u8(2 * F, cols), u8(cols, 2 * F)], torch.zeros(16, device=dev), bf(rows, F), bf(rows, 2 * F)
+        saved = tw.make_saved(*buf, sc)
+        tw.tweo_fp8_gated_fwd_bf16(x, w, h, gu, saved, workspace=ws)
+        t.append(dict(buf=buf, sc=sc, h=h, gu=gu, saved=saved, dh=bf(rows, F), q=u8(rows, 2 * F), qT=u8(2 * F, rows), dx=bf(rows, cols), dw=bf(2 * F, cols)))
+
+    def gated(k, keep):
+        v = t[k]
+        tw.tweo_fp8_gated_fwd(v["buf"][0], v["sc"][2:3], v["buf"][2], v["sc"][5:6], v["h"], gu_bf16=v["gu"] if keep else None)
+
+    def gated_bwd(k):
+        v = t[k]
+        tw.tweo_fp8_gated_bwd_bf16(v["dh"], v["gu"], v["saved"], cols, v["q"], v["qT"], v["dx"], v["dw"], workspace=ws)
+
+    flops = 4.0 * rows * F * cols
+    out["gated_fwd"] = timed(lambda k: gated(k, False), flops=flops)
+    out["gated_fwd_projections_kept"] = timed(lambda k: gated(k, True), flops=flops)
+    out["gated_bwd"] = timed(gated_bwd, flops=2 * flops)
+    return out
+
+
 def vendor_library_context(torch, layers, reps=6):
     """Context, not a product path: the FP8 GEMM of the vendor's library (hipBLASLt behind
     torch._scaled_mm) on the same 15 GEMMs, fed with the codes the step above left in the layers'
@@ -769,6 +830,7 @@ def main():
         out["penalty_cost"] = time_penalty_cost(tw, torch, layers[0])
         out["layernorm"] = time_layernorm(tw, torch, dev)
         out["training_step_beside_the_linears"] = time_training_rest(tw, torch, layers, dev)
+        out["block_between_the_linears"] = time_between_linears(tw, torch, dev)
         del layers, big
         torch.cuda.empty_cache()
         out["w8a8_7b"] = time_w8a8(tw, torch, synth, dev)
