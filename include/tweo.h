@@ -697,8 +697,7 @@ typedef struct {
 
 /* Heads of a tensor [tokens, heads, dim], bf16, whose last index is contiguous; the strides of a token and of a
  * head, in elements, not negative, are the caller's: queries and keys as they lie in the output of a qkv linear are two of
- * these.  Element-aligned; 16-byte aligned heads (addresses, strides and dim multiples of 8, rot_dim of 16) run
- * several times as fast as others. */
+ * these.  Aligned to an element.  Heads of dim % 8 == 0 and rot_dim % 16 == 0 run fastest, then those of dim % 2 == 0 and rot_dim % 4 == 0. */
 typedef struct {
     const void *x;
     void *y;

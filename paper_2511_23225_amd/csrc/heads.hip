@@ -6,8 +6,8 @@
 //   norm   : xhat = x * rstd, rstd = 1 / sqrt(mean(x^2) + eps), y = R (xhat * gain)
 //   grad   : d = R^T dy, w = d * gain, dx = rstd * (w - xhat * mean(w * xhat)), dgain = sum over tokens and heads of d * xhat
 //
-// A head belongs to a team of 1 to 32 lanes (a power of two, 16 values each) that hold both members of a pair in one lane; a
-// head that its strides, its width or the rotated part let fall between 16-byte pieces to a wave, element by element.  The angles of a
+// A head belongs to a team of 1 to 32 lanes (a power of two, 16 values each) that hold both members of a pair in one lane: in 16-byte pieces, or, where
+// width and turned part do not divide so, in words or single elements (HeadsLane).  The angles of a
 // workgroup's tokens are worked out once, one a thread, into LDS and serve all heads; nothing else is shared, so
 // memory bounds the large calls.
 #include <algorithm>
@@ -37,122 +37,115 @@ struct HeadsDev {
     float *partials;         // grad: a row of dim for each workgroup
 };
 
-// ---- where a lane's pairs lie.  a, b: its pairs' members, or what is not rotated, two by two.
-template <bool PAIRS>
-struct HeadsVector {  // 16-byte pieces: eight pairs a lane
-    static constexpr int PER = 8;
-    int ca, cb, at;
-    bool va, vb, turns;
-    __device__ __forceinline__ HeadsVector(int l, int dim, int rot)
+// ---- where a lane's eight pairs lie: in 8 / V chunks of V pairs, chunk l + LANES k of the head's (V pairs each: of the turned part first, then
+// of what is left, two by two).  a, b: the members of a pair, or of what is not turned, what lies there.
+template <bool PAIRS, int V, int LANES>
+struct HeadsLane {
+    static constexpr int PER = 8, CHUNKS = 8 / V, WORDS = V == 1 ? 16 : 8;
+    static_assert(V == 1 || V == 2 || V == 8, "elements, words or 16-byte pieces");
+    typedef uint32_t vec __attribute__((ext_vector_type(V / 2 > 1 ? V / 2 : 2), aligned(2)));  // any even address will do
+    typedef uint32_t word __attribute__((aligned(2)));
+    int at_a[CHUNKS], at_b[CHUNKS];  // first elements, -1: none
+    int turned, first;
+    __device__ __forceinline__ HeadsLane(int l, int dim, int rot) : turned((rot >> 1) / V), first(l)
     {
-        const int pieces = dim >> 3, lanes = rot >> 4;
-        turns = l < lanes;
-        ca = turns ? (PAIRS ? 2 * l : l) : 2 * l;
-        cb = turns && !PAIRS ? l + lanes : ca + 1;
-        va = ca < pieces;
-        vb = cb < pieces;
-        at = 8 * l;
+#pragma unroll
+        for (int k = 0; k < CHUNKS; ++k) {
+            const int c = l + LANES * k, rest = rot + 2 * V * (c - turned);
+            const bool turns = c < turned;
+            const int i = turns ? (PAIRS ? 2 * V * c : V * c) : rest, j = turns && !PAIRS ? (rot >> 1) + V * c : i + V;
+            at_a[k] = i < dim ? i : -1;
+            at_b[k] = j < dim ? j : -1;
+        }
     }
-    __device__ __forceinline__ bool rotates(int) const { return turns; }
-    __device__ __forceinline__ int angle(int e) const { return at + e; }
+    __device__ __forceinline__ bool rotates(int e) const { return first + LANES * (e / V) < turned; }
+    __device__ __forceinline__ int angle(int e) const { return V * (first + LANES * (e / V)) + e % V; }
+    // a column of the head, or -1
+    __device__ __forceinline__ int column(int e, bool second) const
+    {
+        const int k = e / V, pos = PAIRS ? 2 * (e % V) + second : second ? V + e % V : e % V, from = pos < V ? at_a[k] : at_b[k];
+        return from < 0 ? -1 : from + pos % V;
+    }
     struct Raw {
-        v4i a, b;
+        uint32_t w[WORDS];
     };
+    template <bool ONCE>
+    static __device__ __forceinline__ void fetch_chunk(const uint16_t *p, int at, uint32_t *w)
+    {
+        if constexpr (V == 8) {
+            vec v = {0, 0, 0, 0};
+            if (at >= 0)
+                v = ONCE ? __builtin_nontemporal_load((const vec *)(p + at)) : *(const vec *)(p + at);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                w[k] = v[k];
+        } else if constexpr (V == 2) {
+            *w = at >= 0 ? *(const word *)(p + at) : 0u;
+        } else {
+            *w = at >= 0 ? (uint32_t)p[at] : 0u;
+        }
+    }
+    static __device__ __forceinline__ void store_chunk(uint16_t *p, int at, const uint32_t *w)
+    {
+        if (at < 0)
+            return;
+        if constexpr (V == 8)
+            *(vec *)(p + at) = vec{w[0], w[1], w[2], w[3]};
+        else if constexpr (V == 2)
+            *(word *)(p + at) = *w;
+        else
+            p[at] = (uint16_t)*w;
+    }
     template <bool ONCE>
     __device__ __forceinline__ Raw fetch(const uint16_t *p) const
     {
-        Raw r{{0, 0, 0, 0}, {0, 0, 0, 0}};
-        const v4i *A = (const v4i *)(p + 8 * ca), *B = (const v4i *)(p + 8 * cb);
-        if (va)
-            r.a = ONCE ? __builtin_nontemporal_load(A) : *A;
-        if (vb)
-            r.b = ONCE ? __builtin_nontemporal_load(B) : *B;
+        constexpr int N = WORDS / (2 * CHUNKS);
+        Raw r;
+#pragma unroll
+        for (int k = 0; k < CHUNKS; ++k) {
+            fetch_chunk<ONCE>(p, at_a[k], r.w + 2 * N * k);
+            fetch_chunk<ONCE>(p, at_b[k], r.w + 2 * N * k + N);
+        }
         return r;
     }
     __device__ __forceinline__ void widen(const Raw &r, float (&a)[PER], float (&b)[PER]) const
     {
-        const uint32_t w[8] = {(uint32_t)r.a[0], (uint32_t)r.a[1], (uint32_t)r.a[2], (uint32_t)r.a[3],
-                               (uint32_t)r.b[0], (uint32_t)r.b[1], (uint32_t)r.b[2], (uint32_t)r.b[3]};
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            if constexpr (PAIRS) {
-                a[k] = bf16lo_to_f32(w[k]);
-                b[k] = bf16hi_to_f32(w[k]);
+        for (int e = 0; e < PER; ++e) {
+            if constexpr (V == 1) {
+                a[e] = bits_to_f32(r.w[2 * e] << 16);
+                b[e] = bits_to_f32(r.w[2 * e + 1] << 16);
+            } else if constexpr (PAIRS) {
+                a[e] = bf16lo_to_f32(r.w[e]);
+                b[e] = bf16hi_to_f32(r.w[e]);
             } else {
-                float *h = k < 4 ? a : b;
-                h[2 * (k & 3)] = bf16lo_to_f32(w[k]);
-                h[2 * (k & 3) + 1] = bf16hi_to_f32(w[k]);
+                const uint32_t wa = r.w[e / V * V + (e % V) / 2], wb = r.w[e / V * V + V / 2 + (e % V) / 2];
+                a[e] = e & 1 ? bf16hi_to_f32(wa) : bf16lo_to_f32(wa);
+                b[e] = e & 1 ? bf16hi_to_f32(wb) : bf16lo_to_f32(wb);
             }
         }
     }
     __device__ __forceinline__ void store(uint16_t *p, const float (&a)[PER], const float (&b)[PER]) const
     {
-        uint32_t w[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const float *h = k < 4 ? a : b;
-            w[k] = PAIRS ? pack_bf16x2(a[k], b[k]) : pack_bf16x2(h[2 * (k & 3)], h[2 * (k & 3) + 1]);
-        }
-        if (va)
-            *(uint4 *)(p + 8 * ca) = make_uint4(w[0], w[1], w[2], w[3]);
-        if (vb)
-            *(uint4 *)(p + 8 * cb) = make_uint4(w[4], w[5], w[6], w[7]);
-    }
-    // a column of the head, or -1
-    __device__ __forceinline__ int column(int e, bool second) const
-    {
-        if constexpr (PAIRS)
-            return (e < 4 ? va : vb) ? 8 * (e < 4 ? ca : cb) + 2 * (e & 3) + second : -1;
-        else
-            return (second ? vb : va) ? 8 * (second ? cb : ca) + e : -1;
-    }
-};
-template <bool PAIRS>
-struct HeadsScalar {  // element by element: pairs lane, lane + 64, ...
-    static constexpr int PER = 4;
-    int lane, dim, rot;
-    __device__ __forceinline__ HeadsScalar(int l, int dim_, int rot_) : lane(l), dim(dim_), rot(rot_) {}
-    __device__ __forceinline__ bool rotates(int e) const { return angle(e) < rot / 2; }
-    __device__ __forceinline__ int angle(int e) const { return lane + kWave * e; }
-    __device__ __forceinline__ int column(int e, bool second) const
-    {
-        const int p = angle(e), half = rot / 2;
-        const int c = PAIRS || p >= half ? 2 * p + second : p + (second ? half : 0);
-        return c < dim ? c : -1;
-    }
-    struct Raw {
-        uint32_t w[2 * PER];
-    };
-    template <bool ONCE>
-    __device__ __forceinline__ Raw fetch(const uint16_t *p) const
-    {
-        Raw r;
+        constexpr int N = WORDS / (2 * CHUNKS);
+        uint32_t w[WORDS];
 #pragma unroll
         for (int e = 0; e < PER; ++e) {
-            const int i = column(e, false), j = column(e, true);
-            r.w[2 * e] = i >= 0 ? p[i] : 0u;
-            r.w[2 * e + 1] = j >= 0 ? p[j] : 0u;
+            if constexpr (V == 1) {
+                const uint32_t d = pack_bf16x2(a[e], b[e]);
+                w[2 * e] = d;
+                w[2 * e + 1] = d >> 16;
+            } else if constexpr (PAIRS) {
+                w[e] = pack_bf16x2(a[e], b[e]);
+            } else if (e % 2 == 0) {
+                w[e / V * V + (e % V) / 2] = pack_bf16x2(a[e], a[e + 1]);
+                w[e / V * V + V / 2 + (e % V) / 2] = pack_bf16x2(b[e], b[e + 1]);
+            }
         }
-        return r;
-    }
-    __device__ __forceinline__ void widen(const Raw &r, float (&a)[PER], float (&b)[PER]) const
-    {
 #pragma unroll
-        for (int e = 0; e < PER; ++e) {
-            a[e] = bits_to_f32(r.w[2 * e] << 16);
-            b[e] = bits_to_f32(r.w[2 * e + 1] << 16);
-        }
-    }
-    __device__ __forceinline__ void store(uint16_t *p, const float (&a)[PER], const float (&b)[PER]) const
-    {
-#pragma unroll
-        for (int e = 0; e < PER; ++e) {
-            const int i = column(e, false), j = column(e, true);
-            const uint32_t w = pack_bf16x2(a[e], b[e]);
-            if (i >= 0)
-                p[i] = (uint16_t)w;
-            if (j >= 0)
-                p[j] = (uint16_t)(w >> 16);
+        for (int k = 0; k < CHUNKS; ++k) {
+            store_chunk(p, at_a[k], w + 2 * N * k);
+            store_chunk(p, at_b[k], w + 2 * N * k + N);
         }
     }
 };
@@ -187,8 +180,6 @@ __device__ __forceinline__ float team_sum(float v)
         v = dpp_add_f32<0x140>(v);  // the other eight of sixteen
     if constexpr (LANES >= 32)
         v = add_across<16>(v);
-    if constexpr (LANES >= 64)
-        v = add_across<32>(v);
     return v;
 }
 // over the teams of a wave, lane by lane
@@ -246,7 +237,7 @@ enum HeadsMode { kHeadsRotary, kHeadsNorm, kHeadsGrad };
 
 // ONCE: large calls; what is read is read past the caches.
 template <typename LANE, int LANES, int MODE, bool ONCE>
-__global__ __launch_bounds__(kHeadsThreads, 4) void heads_kernel(HeadsDev g)
+__global__ __launch_bounds__(kHeadsThreads, MODE != kHeadsGrad ? 4 : LANE::CHUNKS < 8 ? 3 : 2) void heads_kernel(HeadsDev g)
 {
     constexpr int PER = LANE::PER, TEAMS = kHeadsThreads / LANES;
     __shared__ float2 angles[kHeadsAngles];
@@ -420,20 +411,19 @@ __global__ __launch_bounds__(256) void heads_gain_kernel(const float *__restrict
 }
 
 // ---- host side
+// Rotation, from so many bytes on, by teams whose loads cover whole lines: 16384x32 of 128 53 us, read past the caches 50; of 64, whose
+// pieces of a line are fetched by two loads, 53 and 55; the norm 55 both ways, gradients 83 and 88.
 constexpr int64_t kHeadsOnceBytes = 128 << 20;
 constexpr int kHeadsBlockHeads = 2048;  // (a workgroup divides its items by them in fp32)
 constexpr int kHeadsGradBlocks = 768;  // workgroups of the gradients, three a CU
-constexpr int kHeadsRounds = 4;  // heads of a team at a time
+// Heads of a team at a time.  us, 1 / 2 / 4 / 8: rotation of 16384x32 of 128 53 / 50 / 52 / 57, 4096x40 of 128 17.8 / 16.5 / 16.6 / -; norm of
+// 16384x64 of 64 68 / 56 / 55 / 64
+constexpr int kHeadsRounds = 4, kHeadsRoundsRotary = 2;
 
 // a row of dgain for each workgroup: each side has its share of them, one at least
 int64_t heads_grad_bytes(int64_t tokens, int64_t heads, int64_t dim)
 {
     return std::min<int64_t>(tokens * heads, kHeadsGradBlocks + 1) * dim * 4;
-}
-
-static bool on_pieces(const void *p, int64_t token, int64_t head)
-{
-    return ((uintptr_t)p & 15) == 0 && token % 8 == 0 && head % 8 == 0;
 }
 
 // items: heads at a time; most: workgroups at most (a side has a 768th of all heads for each, so that its heads in that many parts
@@ -447,9 +437,10 @@ static void heads_share(HeadsSide &s, int64_t tokens, int64_t items, int64_t at_
     s.blocks = (int)(s.splits * std::min(rows, std::max<int64_t>(1, most / s.splits)));
 }
 
-template <typename LANE, int LANES>
+template <bool PAIRS, int V, int LANES>
 static hipError_t launch_lanes(HeadsDev &g, int mode, int sides, hipStream_t s)
 {
+    typedef HeadsLane<PAIRS, V, LANES> LANE;
     constexpr int TEAMS = kHeadsThreads / LANES;
     const int half = g.rot / 2;
     const int64_t at_once = half != 0 ? std::min(kHeadsTokens, kHeadsAngles / half) : kHeadsTokens;
@@ -458,11 +449,11 @@ static hipError_t launch_lanes(HeadsDev &g, int mode, int sides, hipStream_t s)
         all += g.tokens * g.side[i].heads;
     for (int i = 0; i < sides; ++i) {
         const int64_t mine = g.tokens * g.side[i].heads;
-        const int64_t items = std::min<int64_t>(kHeadsRounds * TEAMS, std::max<int64_t>(TEAMS, mine / 1024));
+        const int64_t items = std::min<int64_t>((mode == kHeadsRotary ? kHeadsRoundsRotary : kHeadsRounds) * TEAMS, std::max<int64_t>(TEAMS, mine / 1024));
         heads_share(g.side[i], g.tokens, items, at_once, mode == kHeadsGrad ? std::max<int64_t>(1, kHeadsGradBlocks * mine / all) : (int64_t)1 << 31);
     }
     const dim3 grid((unsigned)(g.side[0].blocks + g.side[1].blocks)), block(kHeadsThreads);
-    constexpr bool USUAL = LANES >= 4 && LANES <= 16;
+    constexpr bool USUAL = V == 8 && LANES >= 8 && LANES <= 16;
     if (mode == kHeadsRotary && USUAL && all * g.dim * 4 >= kHeadsOnceBytes)
         hipLaunchKernelGGL((heads_kernel<LANE, LANES, kHeadsRotary, USUAL>), grid, block, 0, s, g);
     else if (mode == kHeadsRotary)
@@ -474,23 +465,33 @@ static hipError_t launch_lanes(HeadsDev &g, int mode, int sides, hipStream_t s)
     return hipGetLastError();
 }
 
-template <bool PAIRS>
-static hipError_t launch_layout(HeadsDev &g, int mode, int sides, bool pieces, hipStream_t s)
+template <bool PAIRS, int V>
+static hipError_t launch_width(HeadsDev &g, int mode, int sides, hipStream_t s)
 {
-    if (!pieces)
-        return launch_lanes<HeadsScalar<PAIRS>, 64>(g, mode, sides, s);
     const int lanes = (g.dim + 15) / 16;
-    if (lanes <= 1)
-        return launch_lanes<HeadsVector<PAIRS>, 1>(g, mode, sides, s);
-    if (lanes <= 2)
-        return launch_lanes<HeadsVector<PAIRS>, 2>(g, mode, sides, s);
+    if constexpr (V == 8) {
+        if (lanes <= 1)
+            return launch_lanes<PAIRS, V, 1>(g, mode, sides, s);
+        if (lanes <= 2)
+            return launch_lanes<PAIRS, V, 2>(g, mode, sides, s);
+    }
     if (lanes <= 4)
-        return launch_lanes<HeadsVector<PAIRS>, 4>(g, mode, sides, s);
+        return launch_lanes<PAIRS, V, 4>(g, mode, sides, s);
     if (lanes <= 8)
-        return launch_lanes<HeadsVector<PAIRS>, 8>(g, mode, sides, s);
+        return launch_lanes<PAIRS, V, 8>(g, mode, sides, s);
     if (lanes <= 16)
-        return launch_lanes<HeadsVector<PAIRS>, 16>(g, mode, sides, s);
-    return launch_lanes<HeadsVector<PAIRS>, 32>(g, mode, sides, s);
+        return launch_lanes<PAIRS, V, 16>(g, mode, sides, s);
+    return launch_lanes<PAIRS, V, 32>(g, mode, sides, s);
+}
+
+// chunks of V pairs, where both members' chunks and what is left are whole ones
+template <bool PAIRS>
+static hipError_t launch_layout(HeadsDev &g, int mode, int sides, hipStream_t s)
+{
+    const int pairs = g.rot / 2;
+    if (pairs % 8 == 0 && g.dim % 8 == 0)
+        return launch_width<PAIRS, 8>(g, mode, sides, s);
+    return pairs % 2 == 0 && g.dim % 2 == 0 ? launch_width<PAIRS, 2>(g, mode, sides, s) : launch_width<PAIRS, 1>(g, mode, sides, s);
 }
 
 hipError_t launch_heads(const HeadsCall &c, int mode, hipStream_t s)
@@ -505,7 +506,6 @@ hipError_t launch_heads(const HeadsCall &c, int mode, hipStream_t s)
     g.eps = c.eps;
     g.sign = c.transpose || mode == kHeadsGrad ? -1.0f : 1.0f;
     g.partials = c.partials;
-    bool pieces = c.dim % 8 == 0 && c.rot % 16 == 0;
     for (int i = 0; i < c.sides; ++i) {
         const HeadsCallSide &f = c.side[i];
         HeadsSide &t = g.side[i];
@@ -522,10 +522,8 @@ hipError_t launch_heads(const HeadsCall &c, int mode, hipStream_t s)
         t.dy_head = stride(f.dy_head, f.heads);
         t.y_token = stride(f.y_token, c.tokens);
         t.y_head = stride(f.y_head, f.heads);
-        pieces = pieces && on_pieces(t.x, t.x_token, t.x_head) && on_pieces(t.y, t.y_token, t.y_head) &&
-                 on_pieces(t.dy, t.dy_token, t.dy_head) && on_pieces(t.gain, 0, 0);
     }
-    const hipError_t e = c.pairs ? launch_layout<true>(g, mode, c.sides, pieces, s) : launch_layout<false>(g, mode, c.sides, pieces, s);
+    const hipError_t e = c.pairs ? launch_layout<true>(g, mode, c.sides, s) : launch_layout<false>(g, mode, c.sides, s);
     if (e != hipSuccess || mode != kHeadsGrad || (c.side[0].dgain == nullptr && c.side[1].dgain == nullptr))
         return e;
     hipLaunchKernelGGL(heads_gain_kernel, dim3((unsigned)((c.dim + 15) / 16), (unsigned)c.sides), dim3(256), 0, s, g.partials,
