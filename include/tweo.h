@@ -680,8 +680,8 @@ tweo_status tweo_adamw_step(const tweo_optim_plan *plan, const tweo_adamw_cfg *c
  * (TWEO_ROTARY_PAIRS); the other dim - rot_dim values stay as they are.  The angle is taken in fp64 and
  * reduced to a turn there (to 2^-51 of the turns gone through: a position of 10^9 costs nothing that bf16 shows), the rest is
  * fp32, one rounding to bf16.
- *   positions  int64 [tokens] on the device.  A negative one marks padding: that token's heads are neither
- *              read nor written, and count in no gradient.
+ *   positions  int64 [tokens] on the device.  A negative one marks padding: that token's heads are not
+ *              written, and what they hold counts nowhere, in no gradient either.
  *   freqs      fp64 [rot_dim / 2] on the device, radians a position: whatever a scaling for long contexts makes of
  *              them (tweo_rotary_freqs), once for a model.
  *   scale      factor of the turned part (an attention factor that goes with such a scaling), 1 without; finite.

@@ -1454,8 +1454,8 @@ tweo_status tweo_fp8_gated_bwd_bf16(const void *dh_bf16, const void *gu_bf16, co
     const size_t mf = (size_t)(M * F), x = (size_t)(M * K), w = (size_t)(2 * F * K);
     add(dh_bf16, 2 * mf, false);
     add(gu_bf16, 4 * mf, false);
-    add(saved->xqT, x, false);
-    add(saved->wqT, w, false);
+    add(dw_bf16 ? saved->xqT : nullptr, x, false);
+    add(dx_bf16 ? saved->wqT : nullptr, w, false);
     add(saved->scalars, 64, true);
     add(dguq, 2 * mf, true);
     add(dguqT, 2 * mf, true);

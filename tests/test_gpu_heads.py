@@ -263,6 +263,15 @@ def test_in_place_and_inside_one_tensor():
             tw.tweo_head_norm_rotary_bwd(list(zip(parts(d), parts(x), gain, parts(d if target == "dy" else x), dg)), pos, f, workspace=ws)
             assert all((a == b).all() for a, b in zip(parts(d if target == "dy" else x), out))
             assert all((a == b).all() for a, b in zip(dg, first))
+    # a part of each head turned, the rest untouched, in place and back
+    t = bf(np.random.default_rng(10).standard_normal((21, 3, 96))).to(DEV)
+    pos, f, own = torch.arange(21, device=DEV), tw.tweo_rotary_freqs(48).to(DEV), t.clone()
+    for layout in ("halves", "pairs"):
+        tw.tweo_rotary([(own, own)], pos, f, layout=layout)
+        assert (own[..., 48:] == t[..., 48:]).all() and not (own[1:, :, :48] == t[1:, :, :48]).all()
+        tw.tweo_rotary([(own, own)], pos, f, layout=layout, transpose=True)
+        assert ((own.float() - t.float()).abs() <= 2.0 ** -7 * t.float().abs().amax(-1, keepdim=True)).all()
+        own.copy_(t)
     # heads of queries and keys in turn
     t = bf(np.random.default_rng(8).standard_normal((19, 5, 2, 32))).to(DEV)
     pos, f = torch.arange(19, device=DEV), tw.tweo_rotary_freqs(32).to(DEV)
