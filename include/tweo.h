@@ -697,7 +697,7 @@ typedef struct {
 
 /* Heads of a tensor [tokens, heads, dim], bf16, whose last index is contiguous; the strides of a token and of a
  * head, in elements, not negative, are the caller's: queries and keys as they lie in the output of a qkv linear are two of
- * these.  Aligned to an element.  Heads of dim % 8 == 0 and rot_dim % 16 == 0 run fastest, then those of dim % 2 == 0 and rot_dim % 4 == 0. */
+ * these.  Aligned to an element.  Heads of dim % 8 == 0 and rot_dim % 16 == 0 run fastest. */
 typedef struct {
     const void *x;
     void *y;

@@ -6,11 +6,12 @@
 //   norm   : xhat = x * rstd, rstd = 1 / sqrt(mean(x^2) + eps), y = R (xhat * gain)
 //   grad   : d = R^T dy, w = d * gain, dx = rstd * (w - xhat * mean(w * xhat)), dgain = sum over tokens and heads of d * xhat
 //
-// A head belongs to a team of 1 to 32 lanes (a power of two, 16 values each) that hold both members of a pair in one lane: in 16-byte pieces, or, where
-// width and turned part do not divide so, in words or single elements (HeadsLane).  The angles of a
-// workgroup's tokens are worked out once, one a thread, into LDS and serve all heads; nothing else is shared, so
-// memory bounds the large calls.
+// A head belongs to a team of 1 to 32 lanes (a power of two, 16 values each) that hold both members of a pair in one lane, in 16-byte pieces, which
+// overlap where width and turned part are no whole ones.  The angles of a workgroup's tokens are worked out once, one a thread, into LDS and serve
+// all heads; nothing else is shared, so memory bounds the large calls: 16384 tokens of 32 heads of 128, rotation 50.5 us (5.3 TB/s, a copy's
+// rate), 64 of 64, norm 55 and gradients 81.5 (78 and the joining of dgain's rows).
 #include <algorithm>
+#include <type_traits>
 #include "device_utils.h"
 #include "kernels.h"
 
@@ -37,74 +38,145 @@ struct HeadsDev {
     float *partials;         // grad: a row of dim for each workgroup
 };
 
-// ---- where a lane's eight pairs lie: in 8 / V chunks of V pairs, chunk l + LANES k of the head's (V pairs each: of the turned part first, then
-// of what is left, two by two).  a, b: the members of a pair, or of what is not turned, what lies there.
-template <bool PAIRS, int V, int LANES>
-struct HeadsLane {
-    static constexpr int PER = 8, CHUNKS = 8 / V, WORDS = V == 1 ? 16 : 8;
-    static_assert(V == 1 || V == 2 || V == 8, "elements, words or 16-byte pieces");
-    typedef uint32_t vec __attribute__((ext_vector_type(V / 2 > 1 ? V / 2 : 2), aligned(2)));  // any even address will do
-    typedef uint32_t word __attribute__((aligned(2)));
-    int at_a[CHUNKS], at_b[CHUNKS];  // first elements, -1: none
-    int turned, first;
-    __device__ __forceinline__ HeadsLane(int l, int dim, int rot) : turned((rot >> 1) / V), first(l)
-    {
+// ---- where a lane's eight pairs lie.  a, b: the members of a pair, or of what is not turned, what lies there.
+typedef uint32_t HeadsPiece __attribute__((ext_vector_type(4), aligned(2)));  // 16 bytes at any even address
+
+template <bool ONCE>
+__device__ __forceinline__ void fetch_piece(const uint16_t *p, int at, uint32_t *w)
+{
+    HeadsPiece v = {0, 0, 0, 0};
+    if (at >= 0)
+        v = ONCE ? __builtin_nontemporal_load((const HeadsPiece *)(p + at)) : *(const HeadsPiece *)(p + at);
 #pragma unroll
-        for (int k = 0; k < CHUNKS; ++k) {
-            const int c = l + LANES * k, rest = rot + 2 * V * (c - turned);
-            const bool turns = c < turned;
-            const int i = turns ? (PAIRS ? 2 * V * c : V * c) : rest, j = turns && !PAIRS ? (rot >> 1) + V * c : i + V;
-            at_a[k] = i < dim ? i : -1;
-            at_b[k] = j < dim ? j : -1;
+    for (int k = 0; k < 4; ++k)
+        w[k] = v[k];
+}
+
+// Sixteen elements in two pieces: first and second members (halves), or pairs one behind the other, of the turned part, then of what is left.
+// OVER: parts that are no whole pieces.  A part's last pieces then end where the part does and hold some elements that those in front of them
+// hold too: both lanes come to the same results and store them, one counts them in sums.  Less than sixteen elements that are left are the end of
+// pieces whose other elements belong to the turned part; they are stored one by one.  us, 16384x32 of 100, rotation / norm / gradients: 51 / 54 /
+// 93, in words (pairs l, l + LANES, ..) 66 / 66 / 84; of 98 with 66 turned 50 / 57 / 73 (in pairs), element by element 84 / 91 / 169.
+template <bool PAIRS, int LANES, bool OVER>
+struct HeadsPieces {
+    static constexpr int PER = 8;
+    static constexpr bool FAST = !OVER;
+    int at_a, at_b;  // first elements, -1: none
+    int pair0;       // first pair's number
+    int from_a, from_b;  // OVER: the pairs, by member, from which on they count
+    bool turns, part;    // part: only what counts is stored
+    __device__ __forceinline__ HeadsPieces(int l, int dim, int rot)
+    {
+        if constexpr (!OVER) {
+            const int lanes = rot >> 4;
+            turns = l < lanes;
+            at_a = turns && !PAIRS ? 8 * l : 16 * l;
+            at_b = turns && !PAIRS ? 8 * (l + lanes) : at_a + 8;
+            at_a = at_a < dim ? at_a : -1;
+            at_b = at_b < dim ? at_b : -1;
+            pair0 = 8 * l;
+            from_a = from_b = 0;
+            part = false;
+        } else {
+            const int lanes = (rot + 15) >> 4, left = dim - rot;
+            turns = l < lanes;
+            // sixteen elements from `at` of a part of `len` (its first, `first`), `shift` of them counted by the lane before
+            const int first = turns ? 0 : rot, len = turns ? rot : left, at = 16 * (turns ? l : l - lanes);
+            const bool none = at >= len;
+            const int start = at + 16 <= len ? at : len - 16, shift = none ? 16 : at - start;
+            part = !turns && len < 16;  // (start is negative: into the turned part)
+            if (turns && !PAIRS) {  // members of eight pairs, from pair start / 2 on; shift / 2 pairs too many
+                at_a = start >> 1;
+                at_b = at_a + (rot >> 1);
+                from_a = from_b = shift >> 1;
+            } else {
+                at_a = first + start;
+                at_b = at_a + 8;
+                from_a = PAIRS ? (shift + 1) >> 1 : shift;
+                from_b = PAIRS ? shift >> 1 : shift - 8;
+            }
+            if (none)
+                at_a = at_b = -1;
+            pair0 = start >> 1;
         }
     }
-    __device__ __forceinline__ bool rotates(int e) const { return first + LANES * (e / V) < turned; }
-    __device__ __forceinline__ int angle(int e) const { return V * (first + LANES * (e / V)) + e % V; }
-    // a column of the head, or -1
+    __device__ __forceinline__ bool rotates(int) const { return turns; }
+    __device__ __forceinline__ int angle(int e) const { return pair0 + e; }
+    __device__ __forceinline__ bool counts(int e, bool second) const { return !OVER || e >= (second ? from_b : from_a); }
+    // a column of the head that counts, or -1
     __device__ __forceinline__ int column(int e, bool second) const
     {
-        const int k = e / V, pos = PAIRS ? 2 * (e % V) + second : second ? V + e % V : e % V, from = pos < V ? at_a[k] : at_b[k];
-        return from < 0 ? -1 : from + pos % V;
+        const int pos = PAIRS ? 2 * e + second : second ? 8 + e : e, from = pos < 8 ? at_a : at_b;
+        return from < 0 || !counts(e, second) ? -1 : from + (pos & 7);
     }
     struct Raw {
-        uint32_t w[WORDS];
+        uint32_t w[8];
     };
-    template <bool ONCE>
-    static __device__ __forceinline__ void fetch_chunk(const uint16_t *p, int at, uint32_t *w)
-    {
-        if constexpr (V == 8) {
-            vec v = {0, 0, 0, 0};
-            if (at >= 0)
-                v = ONCE ? __builtin_nontemporal_load((const vec *)(p + at)) : *(const vec *)(p + at);
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                w[k] = v[k];
-        } else if constexpr (V == 2) {
-            *w = at >= 0 ? *(const word *)(p + at) : 0u;
-        } else {
-            *w = at >= 0 ? (uint32_t)p[at] : 0u;
-        }
-    }
-    static __device__ __forceinline__ void store_chunk(uint16_t *p, int at, const uint32_t *w)
-    {
-        if (at < 0)
-            return;
-        if constexpr (V == 8)
-            *(vec *)(p + at) = vec{w[0], w[1], w[2], w[3]};
-        else if constexpr (V == 2)
-            *(word *)(p + at) = *w;
-        else
-            p[at] = (uint16_t)*w;
-    }
     template <bool ONCE>
     __device__ __forceinline__ Raw fetch(const uint16_t *p) const
     {
-        constexpr int N = WORDS / (2 * CHUNKS);
+        Raw r;
+        fetch_piece<ONCE>(p, at_a, r.w);
+        fetch_piece<ONCE>(p, at_b, r.w + 4);
+        return r;
+    }
+    __device__ __forceinline__ void widen(const Raw &r, float (&a)[PER], float (&b)[PER]) const
+    {
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            const uint32_t wa = r.w[PAIRS ? e : e >> 1], wb = r.w[PAIRS ? e : 4 + (e >> 1)];
+            a[e] = !PAIRS && (e & 1) ? bf16hi_to_f32(wa) : bf16lo_to_f32(wa);
+            b[e] = PAIRS || (e & 1) ? bf16hi_to_f32(wb) : bf16lo_to_f32(wb);
+        }
+    }
+    __device__ __forceinline__ void store(uint16_t *p, const float (&a)[PER], const float (&b)[PER]) const
+    {
+        uint32_t w[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            w[k] = PAIRS ? pack_bf16x2(a[k], b[k]) : k < 4 ? pack_bf16x2(a[2 * (k & 3)], a[2 * (k & 3) + 1]) : pack_bf16x2(b[2 * (k & 3)], b[2 * (k & 3) + 1]);
+        if (OVER && part) {
+#pragma unroll
+            for (int e = 0; e < 2 * PER; ++e) {
+                const int c = column(e >> 1, e & 1), k = PAIRS ? e >> 1 : (e & 1) * 4 + (e >> 2);
+                if (c >= 0)
+                    p[c] = (uint16_t)(PAIRS ? w[k] >> (16 * (e & 1)) : w[k] >> (16 * ((e >> 1) & 1)));
+            }
+            return;
+        }
+        if (at_a >= 0)
+            *(HeadsPiece *)(p + at_a) = HeadsPiece{w[0], w[1], w[2], w[3]};
+        if (at_b >= 0)
+            *(HeadsPiece *)(p + at_b) = HeadsPiece{w[4], w[5], w[6], w[7]};
+    }
+};
+
+// Element by element, pairs l, l + LANES, ..: heads of less than sixteen elements, or with less than sixteen turned, and the widest that are no whole pieces
+template <bool PAIRS, int LANES>
+struct HeadsElements {
+    static constexpr int PER = 8;
+    static constexpr bool FAST = false;
+    int l, dim, half;
+    __device__ __forceinline__ HeadsElements(int l_, int dim_, int rot) : l(l_), dim(dim_), half(rot >> 1) {}
+    __device__ __forceinline__ bool rotates(int e) const { return angle(e) < half; }
+    __device__ __forceinline__ int angle(int e) const { return l + LANES * e; }
+    __device__ __forceinline__ bool counts(int, bool) const { return true; }
+    __device__ __forceinline__ int column(int e, bool second) const
+    {
+        const int p = angle(e), c = PAIRS || p >= half ? 2 * p + second : second ? p + half : p;
+        return c < dim ? c : -1;
+    }
+    struct Raw {
+        uint32_t w[2 * PER];
+    };
+    template <bool ONCE>
+    __device__ __forceinline__ Raw fetch(const uint16_t *p) const
+    {
         Raw r;
 #pragma unroll
-        for (int k = 0; k < CHUNKS; ++k) {
-            fetch_chunk<ONCE>(p, at_a[k], r.w + 2 * N * k);
-            fetch_chunk<ONCE>(p, at_b[k], r.w + 2 * N * k + N);
+        for (int e = 0; e < 2 * PER; ++e) {
+            const int c = column(e >> 1, e & 1);
+            r.w[e] = c >= 0 ? (uint32_t)p[c] << 16 : 0u;
         }
         return r;
     }
@@ -112,40 +184,20 @@ struct HeadsLane {
     {
 #pragma unroll
         for (int e = 0; e < PER; ++e) {
-            if constexpr (V == 1) {
-                a[e] = bits_to_f32(r.w[2 * e] << 16);
-                b[e] = bits_to_f32(r.w[2 * e + 1] << 16);
-            } else if constexpr (PAIRS) {
-                a[e] = bf16lo_to_f32(r.w[e]);
-                b[e] = bf16hi_to_f32(r.w[e]);
-            } else {
-                const uint32_t wa = r.w[e / V * V + (e % V) / 2], wb = r.w[e / V * V + V / 2 + (e % V) / 2];
-                a[e] = e & 1 ? bf16hi_to_f32(wa) : bf16lo_to_f32(wa);
-                b[e] = e & 1 ? bf16hi_to_f32(wb) : bf16lo_to_f32(wb);
-            }
+            a[e] = bits_to_f32(r.w[2 * e]);
+            b[e] = bits_to_f32(r.w[2 * e + 1]);
         }
     }
     __device__ __forceinline__ void store(uint16_t *p, const float (&a)[PER], const float (&b)[PER]) const
     {
-        constexpr int N = WORDS / (2 * CHUNKS);
-        uint32_t w[WORDS];
 #pragma unroll
         for (int e = 0; e < PER; ++e) {
-            if constexpr (V == 1) {
-                const uint32_t d = pack_bf16x2(a[e], b[e]);
-                w[2 * e] = d;
-                w[2 * e + 1] = d >> 16;
-            } else if constexpr (PAIRS) {
-                w[e] = pack_bf16x2(a[e], b[e]);
-            } else if (e % 2 == 0) {
-                w[e / V * V + (e % V) / 2] = pack_bf16x2(a[e], a[e + 1]);
-                w[e / V * V + V / 2 + (e % V) / 2] = pack_bf16x2(b[e], b[e + 1]);
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < CHUNKS; ++k) {
-            store_chunk(p, at_a[k], w + 2 * N * k);
-            store_chunk(p, at_b[k], w + 2 * N * k + N);
+            const uint32_t d = pack_bf16x2(a[e], b[e]);
+            const int i = column(e, false), j = column(e, true);
+            if (i >= 0)
+                p[i] = (uint16_t)d;
+            if (j >= 0)
+                p[j] = (uint16_t)(d >> 16);
         }
     }
 };
@@ -204,14 +256,16 @@ __device__ __forceinline__ float teams_sum(float v)
 
 // x becomes xhat.  Squares whose sum leaves fp32 (beyond 2^100, or, without an eps that covers them, below 2^-80) are taken of values
 // moved by a power of two.
-template <int LANES, int PER>
-__device__ __forceinline__ float heads_normalise(float (&a)[PER], float (&b)[PER], float per_dim, float eps)
+template <int LANES, int PER, typename LANE>
+__device__ __forceinline__ float heads_normalise(const LANE &lane, float (&a)[PER], float (&b)[PER], float per_dim, float eps)
 {
     auto squares = [&] {
         float ss = 0.0f;
 #pragma unroll
-        for (int e = 0; e < PER; ++e)
-            ss = __builtin_fmaf(a[e], a[e], __builtin_fmaf(b[e], b[e], ss));
+        for (int e = 0; e < PER; ++e) {
+            const float u = lane.counts(e, false) ? a[e] : 0.0f, v = lane.counts(e, true) ? b[e] : 0.0f;
+            ss = __builtin_fmaf(u, u, __builtin_fmaf(v, v, ss));
+        }
         return team_sum<LANES>(ss);
     };
     const float ss = squares();
@@ -237,7 +291,7 @@ enum HeadsMode { kHeadsRotary, kHeadsNorm, kHeadsGrad };
 
 // ONCE: large calls; what is read is read past the caches.
 template <typename LANE, int LANES, int MODE, bool ONCE>
-__global__ __launch_bounds__(kHeadsThreads, MODE != kHeadsGrad ? 4 : LANE::CHUNKS < 8 ? 3 : 2) void heads_kernel(HeadsDev g)
+__global__ __launch_bounds__(kHeadsThreads, MODE != kHeadsGrad ? 4 : LANE::FAST ? 3 : 2) void heads_kernel(HeadsDev g)
 {
     constexpr int PER = LANE::PER, TEAMS = kHeadsThreads / LANES;
     __shared__ float2 angles[kHeadsAngles];
@@ -323,7 +377,7 @@ __global__ __launch_bounds__(kHeadsThreads, MODE != kHeadsGrad ? 4 : LANE::CHUNK
                     }
             };
             if constexpr (MODE == kHeadsNorm) {
-                heads_normalise<LANES>(a, b, per_dim, g.eps);
+                heads_normalise<LANES>(lane, a, b, per_dim, g.eps);
 #pragma unroll
                 for (int e = 0; e < PER; ++e) {
                     a[e] *= ga[e];
@@ -334,7 +388,7 @@ __global__ __launch_bounds__(kHeadsThreads, MODE != kHeadsGrad ? 4 : LANE::CHUNK
                 turn(a, b);
             } else {
                 turn(da, db);
-                const float rstd = heads_normalise<LANES>(a, b, per_dim, g.eps);
+                const float rstd = heads_normalise<LANES>(lane, a, b, per_dim, g.eps);
                 float dot = 0.0f;
 #pragma unroll
                 for (int e = 0; e < PER; ++e) {
@@ -342,7 +396,8 @@ __global__ __launch_bounds__(kHeadsThreads, MODE != kHeadsGrad ? 4 : LANE::CHUNK
                     sb[e] = __builtin_fmaf(db[e], b[e], sb[e]);
                     da[e] *= ga[e];
                     db[e] *= gb[e];
-                    dot = __builtin_fmaf(da[e], a[e], __builtin_fmaf(db[e], b[e], dot));
+                    const float u = lane.counts(e, false) ? da[e] : 0.0f, v = lane.counts(e, true) ? db[e] : 0.0f;
+                    dot = __builtin_fmaf(u, a[e], __builtin_fmaf(v, b[e], dot));
                 }
                 dot = team_sum<LANES>(dot) * per_dim;
 #pragma unroll
@@ -437,10 +492,9 @@ static void heads_share(HeadsSide &s, int64_t tokens, int64_t items, int64_t at_
     s.blocks = (int)(s.splits * std::min(rows, std::max<int64_t>(1, most / s.splits)));
 }
 
-template <bool PAIRS, int V, int LANES>
+template <typename LANE, int LANES>
 static hipError_t launch_lanes(HeadsDev &g, int mode, int sides, hipStream_t s)
 {
-    typedef HeadsLane<PAIRS, V, LANES> LANE;
     constexpr int TEAMS = kHeadsThreads / LANES;
     const int half = g.rot / 2;
     const int64_t at_once = half != 0 ? std::min(kHeadsTokens, kHeadsAngles / half) : kHeadsTokens;
@@ -453,7 +507,7 @@ static hipError_t launch_lanes(HeadsDev &g, int mode, int sides, hipStream_t s)
         heads_share(g.side[i], g.tokens, items, at_once, mode == kHeadsGrad ? std::max<int64_t>(1, kHeadsGradBlocks * mine / all) : (int64_t)1 << 31);
     }
     const dim3 grid((unsigned)(g.side[0].blocks + g.side[1].blocks)), block(kHeadsThreads);
-    constexpr bool USUAL = V == 8 && LANES >= 8 && LANES <= 16;
+    constexpr bool USUAL = LANE::FAST && LANES >= 8 && LANES <= 16;
     if (mode == kHeadsRotary && USUAL && all * g.dim * 4 >= kHeadsOnceBytes)
         hipLaunchKernelGGL((heads_kernel<LANE, LANES, kHeadsRotary, USUAL>), grid, block, 0, s, g);
     else if (mode == kHeadsRotary)
@@ -465,33 +519,41 @@ static hipError_t launch_lanes(HeadsDev &g, int mode, int sides, hipStream_t s)
     return hipGetLastError();
 }
 
-template <bool PAIRS, int V>
-static hipError_t launch_width(HeadsDev &g, int mode, int sides, hipStream_t s)
+enum HeadsWidth { kHeadsWhole, kHeadsOver, kHeadsElement };
+template <bool PAIRS, int WIDTH>
+static hipError_t launch_width(HeadsDev &g, int mode, int sides, int lanes, hipStream_t s)
 {
-    const int lanes = (g.dim + 15) / 16;
-    if constexpr (V == 8) {
+    auto launch = [&](auto lanes_c) {
+        constexpr int LANES = decltype(lanes_c)::value;
+        if constexpr (WIDTH == kHeadsElement)
+            return launch_lanes<HeadsElements<PAIRS, LANES>, LANES>(g, mode, sides, s);
+        else
+            return launch_lanes<HeadsPieces<PAIRS, LANES, WIDTH == kHeadsOver>, LANES>(g, mode, sides, s);
+    };
+    if constexpr (WIDTH == kHeadsWhole)
         if (lanes <= 1)
-            return launch_lanes<PAIRS, V, 1>(g, mode, sides, s);
+            return launch(std::integral_constant<int, 1>{});
+    if constexpr (WIDTH != kHeadsElement)
         if (lanes <= 2)
-            return launch_lanes<PAIRS, V, 2>(g, mode, sides, s);
-    }
+            return launch(std::integral_constant<int, 2>{});
     if (lanes <= 4)
-        return launch_lanes<PAIRS, V, 4>(g, mode, sides, s);
+        return launch(std::integral_constant<int, 4>{});
     if (lanes <= 8)
-        return launch_lanes<PAIRS, V, 8>(g, mode, sides, s);
+        return launch(std::integral_constant<int, 8>{});
     if (lanes <= 16)
-        return launch_lanes<PAIRS, V, 16>(g, mode, sides, s);
-    return launch_lanes<PAIRS, V, 32>(g, mode, sides, s);
+        return launch(std::integral_constant<int, 16>{});
+    return launch(std::integral_constant<int, 32>{});
 }
 
-// chunks of V pairs, where both members' chunks and what is left are whole ones
 template <bool PAIRS>
 static hipError_t launch_layout(HeadsDev &g, int mode, int sides, hipStream_t s)
 {
-    const int pairs = g.rot / 2;
-    if (pairs % 8 == 0 && g.dim % 8 == 0)
-        return launch_width<PAIRS, 8>(g, mode, sides, s);
-    return pairs % 2 == 0 && g.dim % 2 == 0 ? launch_width<PAIRS, 2>(g, mode, sides, s) : launch_width<PAIRS, 1>(g, mode, sides, s);
+    const int left = g.dim - g.rot, over = (g.rot + 15) / 16 + (left + 15) / 16;
+    if (g.rot % 16 == 0 && g.dim % 8 == 0)
+        return launch_width<PAIRS, kHeadsWhole>(g, mode, sides, (g.dim + 15) / 16, s);
+    if (g.dim >= 16 && (g.rot == 0 || g.rot >= 16) && over <= 32)
+        return launch_width<PAIRS, kHeadsOver>(g, mode, sides, over, s);
+    return launch_width<PAIRS, kHeadsElement>(g, mode, sides, (g.dim + 15) / 16, s);
 }
 
 hipError_t launch_heads(const HeadsCall &c, int mode, hipStream_t s)

@@ -81,9 +81,9 @@ def near(got, want, bound, what):
     assert worst <= 1.0, (what, worst)
 
 
-# dims of one lane to a team of 32, whole and partly turned, and such that fall between 16-byte pieces
+# dims of one lane to a team of 32, whole and partly turned, and such that fall between 16-byte pieces or are less than one
 DIMS = [(16, 16), (32, 16), (64, 64), (64, 32), (72, 64), (80, 80), (96, 96), (96, 48), (128, 128), (128, 64), (192, 128), (256, 256), (504, 16), (512, 512),
-        (8, 8), (20, 20), (64, 20), (33, 10), (2, 2), (3, 2), (100, 100), (510, 510), (511, 4)]
+        (8, 8), (20, 20), (64, 20), (33, 10), (2, 2), (3, 2), (100, 100), (510, 510), (511, 4), (17, 16), (18, 18), (24, 18), (40, 34), (98, 66), (130, 96), (259, 100), (500, 484), (505, 34)]
 SHAPES = [(1, (1,)), (1, (32, 8)), (3, (5, 3)), (77, (4, 4)), (600, (6, 1))]
 
 
