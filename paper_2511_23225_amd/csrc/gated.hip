@@ -34,7 +34,7 @@ struct GatedGradDev {
 // dg and du of one element
 __device__ __forceinline__ void gated_grad_one(float dh, float g, float u, const GatedGradDev &c, float &dg, float &du)
 {
-    const float p = gate_share(g, c.act), b = __builtin_amdgcn_fmed3f(g, -0x1p60f, 0x1p60f), gp = g * p;
+    const float p = gate_share_near(g, c.act), b = __builtin_amdgcn_fmed3f(g, -0x1p60f, 0x1p60f), gp = g * p;
     du = dh * gp;
     dg = dh * u * __builtin_fmaf(gp * (1.0f - p), __builtin_fmaf(c.slope1, b * b, c.slope0), p);
 }
