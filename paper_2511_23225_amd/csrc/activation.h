@@ -21,17 +21,6 @@ __device__ __forceinline__ float gate_share(float g, const GateCoef &c)
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-z));
 }
 
-// The same with the sum's rounding and the reciprocal's taken back, where memory leaves time for it: p is within |z| 2^-23 (1 - p) + 2^-24 of itself.
-// (Beyond what the reciprocal of a number gives the correction is not one, and times 0.)  The gradients of 16384x5632 take 1 % longer by it.
-__device__ __forceinline__ float gate_share_near(float g, const GateCoef &c)
-{
-    const float b = __builtin_amdgcn_fmed3f(g, -0x1p60f, 0x1p60f);
-    const float e = __builtin_amdgcn_exp2f(-(b * __builtin_fmaf(c.c1, b * b, c.c0)));
-    const float d = 1.0f + e, p = __builtin_amdgcn_rcpf(d);
-    const float r = __builtin_fmaf(-(e - (d - 1.0f)), p, __builtin_fmaf(-d, p, 1.0f));
-    return __builtin_fmaf(p, __builtin_amdgcn_fmed3f(r, -0x1p-20f, 0x1p-20f), p);
-}
-
 // The exponential of it by itself, p = 1 / (1 + this): the same bits
 template <bool GELU>
 __device__ __forceinline__ float gate_exp(float g, const GateCoef &c)
@@ -41,6 +30,16 @@ __device__ __forceinline__ float gate_exp(float g, const GateCoef &c)
         return __builtin_amdgcn_exp2f(-(b * __builtin_fmaf(c.c1, b * b, c.c0)));
     }
     return __builtin_amdgcn_exp2f(-(g * c.c0));
+}
+
+// The share with the sum's rounding and the reciprocal's taken back, where memory leaves time for it: p is within |z| 2^-23 (1 - p) + 2^-24 of itself.
+// (Beyond what the reciprocal of a number gives the correction is not one, and times 0.)
+template <bool GELU>
+__device__ __forceinline__ float gate_share_near(float g, const GateCoef &c)
+{
+    const float e = gate_exp<GELU>(g, c), d = 1.0f + e, p = __builtin_amdgcn_rcpf(d);
+    const float r = __builtin_fmaf(-(e - (d - 1.0f)), p, __builtin_fmaf(-d, p, 1.0f));
+    return __builtin_fmaf(p, __builtin_amdgcn_fmed3f(r, -0x1p-20f, 0x1p-20f), p);
 }
 
 __device__ __forceinline__ float gated(float g, float u, const GateCoef &c) { return g * gate_share(g, c) * u; }

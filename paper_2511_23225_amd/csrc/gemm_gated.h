@@ -5,7 +5,8 @@
 // A 32-row block of B holds, in place 8q + 4b + r, column 8 (q / 2) + 4b + r of 16: the gate's for even q, the up
 // projection's for odd.  A lane (l31, lh) of the MFMA layout has places 8q + 4lh + r in its registers 4q + r: gate and up of one
 // column are four registers apart.  The rows that a wave brings into LDS, eight at a time, are all of one kind (an even number of
-// waves goes round them), so that its base address alone says which.
+// waves goes round them), so that its base address alone says which.  One row of tokens is bound by the weights (90 MB of INT8: 16 us, 5.7 TB/s),
+// 2048 by the matrix instructions between two barriers a stage (11008 columns under 4096, INT8: 200 us, 1.84 POP/s, of 5.4 rounds of tiles).
 #pragma once
 #include "gemm_common.h"
 #include "activation.h"
