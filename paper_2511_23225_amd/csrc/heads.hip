@@ -470,6 +470,7 @@ __global__ __launch_bounds__(256) void heads_gain_kernel(const float *__restrict
 // pieces of a line are fetched by two loads, 53 and 55; the norm 55 both ways, gradients 83 and 88.
 constexpr int64_t kHeadsOnceBytes = 128 << 20;
 constexpr int kHeadsBlockHeads = 2048;  // (a workgroup divides its items by them in fp32)
+constexpr int64_t kHeadsMostBlocks = (int64_t)1 << 22;  // of a group: a launch holds less than 2^32 threads
 constexpr int kHeadsGradBlocks = 768;  // workgroups of the gradients, three a CU
 // Heads of a team at a time.  us, 1 / 2 / 4 / 8: rotation of 16384x32 of 128 53 / 50 / 52 / 57, 4096x40 of 128 17.8 / 16.5 / 16.6 / -; norm of
 // 16384x64 of 64 68 / 56 / 55 / 64
@@ -504,7 +505,7 @@ static hipError_t launch_lanes(HeadsDev &g, int mode, int sides, hipStream_t s)
     for (int i = 0; i < sides; ++i) {
         const int64_t mine = g.tokens * g.side[i].heads;
         const int64_t items = std::min<int64_t>((mode == kHeadsRotary ? kHeadsRoundsRotary : kHeadsRounds) * TEAMS, std::max<int64_t>(TEAMS, mine / 1024));
-        heads_share(g.side[i], g.tokens, items, at_once, mode == kHeadsGrad ? std::max<int64_t>(1, kHeadsGradBlocks * mine / all) : (int64_t)1 << 31);
+        heads_share(g.side[i], g.tokens, items, at_once, mode == kHeadsGrad ? std::max<int64_t>(1, kHeadsGradBlocks * mine / all) : kHeadsMostBlocks);
     }
     const dim3 grid((unsigned)(g.side[0].blocks + g.side[1].blocks)), block(kHeadsThreads);
     constexpr bool USUAL = LANE::FAST && LANES >= 8 && LANES <= 16;

@@ -181,6 +181,26 @@ def test_far_positions(dim):
     near(y, want, (8 * U + 2.0 ** -17) * size, "far")
 
 
+@pytest.mark.parametrize("norm", [False, True])
+def test_most_tokens(norm):
+    """2^30 tokens of one head of 2: more workgroups of 64 tokens than a launch holds threads for."""
+    tokens, part = 1 << 30, torch.from_numpy(np.random.default_rng(8).standard_normal((1 << 20, 1, 2)).astype(np.float32)).to(torch.bfloat16)
+    x = part.to(DEV).repeat(1 << 10, 1, 1)
+    pos = torch.arange(tokens, device=DEV).remainder_(100003)
+    freqs = tw.tweo_rotary_freqs(2)
+    if norm:
+        tw.tweo_head_norm_rotary_fwd([(x, None, x)], pos, freqs.to(DEV), eps=EPS)
+    else:
+        tw.tweo_rotary([(x, x)], pos, freqs.to(DEV))
+    for at in (0, 12345, (1 << 28) - 500, (1 << 29) + 77, tokens - 1000):
+        src = f64(part[torch.arange(at, at + 1000) % (1 << 20)])
+        if norm:
+            want, size = block.head_norm_rotary(src, np.ones(2), EPS, pos[at:at + 1000].cpu().numpy(), freqs.numpy(), "halves", 1.0)
+        else:
+            want, size = block.rotary(src, pos[at:at + 1000].cpu().numpy(), freqs.numpy())
+        near(x[at:at + 1000], want, (17 if norm else 8) * U * size, at)
+
+
 @pytest.mark.parametrize("dim", [64, 20])
 def test_padding(dim):
     """Tokens of a negative position: their rows stay as they were, whatever they hold, and count in no gradient."""
