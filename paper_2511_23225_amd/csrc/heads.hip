@@ -371,7 +371,8 @@ __global__ __launch_bounds__(kHeadsThreads, MODE != kHeadsGrad ? 4 : LANE::FAST 
                 for (int e = 0; e < PER; ++e)
                     if (lane.rotates(e)) {
                         const float2 c = cs[lane.angle(e)];
-                        const float u = a[e] * c.x - b[e] * c.y, v = b[e] * c.x + a[e] * c.y;
+                        // (spelled out: a value that two lanes hold has to come out the same in both)
+                        const float u = __builtin_fmaf(a[e], c.x, -(b[e] * c.y)), v = __builtin_fmaf(b[e], c.x, a[e] * c.y);
                         a[e] = u;
                         b[e] = v;
                     }

@@ -301,6 +301,35 @@ def test_in_place_and_inside_one_tensor():
     assert all((t[:, :, i] == out[i]).all() for i in range(2))
 
 
+@pytest.mark.parametrize("layout", ["halves", "pairs"])
+@pytest.mark.parametrize("dim,rot", [(98, 66), (40, 34), (100, 100), (17, 16), (130, 96), (259, 100)])
+def test_in_place_of_odd_widths(dim, rot, layout):
+    """Heads whose pieces overlap, where they lie: every call as out of place, bit by bit and again."""
+    rng = np.random.default_rng(12)
+    x, dy = (bf(rng.standard_normal((701, 7, dim))).to(DEV) for _ in range(2))
+    gain = bf(1 + 0.3 * rng.standard_normal(dim)).to(DEV)
+    turn = dict(positions=torch.arange(701, device=DEV) * 31, freqs=tw.tweo_rotary_freqs(rot).to(DEV), layout=layout)
+    ws = torch.empty(tw.tweo_workspace_bytes(tw.TWEO_OP_HEAD_NORM_ROTARY_BWD, 701, 7, dim), dtype=torch.uint8, device=DEV)
+    outs = [torch.empty_like(x) for _ in range(3)]
+    dgain, again = torch.empty(dim, device=DEV), torch.empty(dim, device=DEV)
+    tw.tweo_rotary([(x, outs[0])], **turn)
+    tw.tweo_head_norm_rotary_fwd([(x, gain, outs[1])], **turn)
+    tw.tweo_head_norm_rotary_bwd([(dy, x, gain, outs[2], dgain)], workspace=ws, **turn)
+    for _ in range(3):
+        own = x.clone()
+        tw.tweo_rotary([(own, own)], **turn)
+        assert torch.equal(own, outs[0])
+        own = x.clone()
+        tw.tweo_head_norm_rotary_fwd([(own, gain, own)], **turn)
+        assert torch.equal(own, outs[1])
+        own = x.clone()
+        tw.tweo_head_norm_rotary_bwd([(dy, own, gain, own, again)], workspace=ws, **turn)
+        assert torch.equal(own, outs[2]) and torch.equal(again, dgain)
+        own = dy.clone()
+        tw.tweo_head_norm_rotary_bwd([(own, x, gain, own, again)], workspace=ws, **turn)
+        assert torch.equal(own, outs[2]) and torch.equal(again, dgain)
+
+
 def test_strides_beyond_32_bits():
     """Two tokens, or two heads, more than 2^32 bytes apart."""
     whole = torch.zeros((1 << 31) + (1 << 28) + 256, dtype=torch.bfloat16, device=DEV)
