@@ -223,8 +223,9 @@ template <bool E5M2, bool GELU>
 static hipError_t launch_grad(const GatedGradCall &call, GatedGradDev c, hipStream_t s)
 {
     const bool small = c.tiles_x * ((c.rows + kGatedTile - 1) / kGatedTile) < 2 * (int64_t)num_cus_public();
-    // each workgroup ends in a word of its own, or in an atomic: three a CU walk the tiles
-    const int64_t few = std::min<int64_t>(3 * (int64_t)num_cus_public(), kGatedPartials), all = (int64_t)1 << 31;
+    // each workgroup ends in a word of its own, or in an atomic: three a CU walk the tiles.  The cast has one a tile, as far as a launch goes:
+    // less than 2^32 threads (2^30 rows of 128 columns are 2^23 tiles of 512).
+    const int64_t few = std::min<int64_t>(3 * (int64_t)num_cus_public(), kGatedPartials), all = (int64_t)1 << 22;
     float *state = (float *)call.state;
     if (state != nullptr && !call.bootstrap) {
         c.scale = state + 17;
