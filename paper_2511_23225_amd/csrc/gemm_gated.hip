@@ -33,9 +33,24 @@ static hipError_t launch_inst(const GemmArgs &a, const GatedDev &gd, hipStream_t
             return e;
         done = true;
     }
-    const GemmDev g = gemm_dev(a, T::BM, T::BN / 2);
-    launch_gemm_kernel(kernel, dim3((unsigned)(g.tiles_m * g.tiles_n)), dim3(T::THREADS), T::LDS_BYTES, s, g, gd);
-    return hipGetLastError();
+    // A launch holds less than 2^32 threads: rows beyond that (2^30 under 8 columns are 2^24 tiles of 64) go into launches of their own.
+    constexpr int64_t most = (((int64_t)1 << 32) - 1) / T::THREADS;
+    const int64_t tiles_n = (a.N + T::BN / 2 - 1) / (T::BN / 2), rows = std::max<int64_t>(1, most / tiles_n) * T::BM;
+    for (int64_t m = 0; m < a.M; m += rows) {
+        GemmArgs part = a;
+        part.M = std::min(rows, a.M - m);
+        part.A += m * a.K;
+        part.out = (uint8_t *)a.out + m * a.N * (INT8 && a.out_i8 ? 1 : 2);
+        if (INT8)
+            part.row_step += m * a.row_step_stride;
+        const GatedDev keep{gd.gu != nullptr ? gd.gu + 2 * m * a.N : nullptr, gd.act};
+        const GemmDev g = gemm_dev(part, T::BM, T::BN / 2);
+        launch_gemm_kernel(kernel, dim3((unsigned)(g.tiles_m * g.tiles_n)), dim3(T::THREADS), T::LDS_BYTES, s, g, keep);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess)
+            return e;
+    }
+    return hipSuccess;
 }
 
 template <typename T, bool INT8>
