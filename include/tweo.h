@@ -710,7 +710,12 @@ typedef struct {
  * Turns one or two groups of heads (queries and keys: as many heads each as they have) of the same tokens, one
  * launch.  transpose != 0: the transposed map, the gradient's (also times scale).
  *   groups: host array of `count` (1 or 2); y may be the same group's x (the same address and strides), else nothing that
- *   is written overlaps anything.  dim 1 .. 512, heads of a group up to 2^16, tokens up to 2^30.
+ *   is written overlaps anything.  dim 1 .. 512, heads of a group up to 2^16, tokens up to 2^30, tokens * heads of a
+ *   group up to 2^34, tokens * a token's stride and heads * a head's stride up to 2^46 elements (a stride that no second token
+ *   or head is reached by may be anything that is not negative).
+ *   Heads of a group lie one stride apart.  A qkv tensor [tokens, key heads, queries of a key + 2, dim] has two strides of
+ *   queries: its groups are those of tokens * key heads tokens, [.., queries of a key, dim] and [.., 1, dim], each position given
+ *   key heads times.
  * Errors: TWEO_ERR_INVALID_ARG (null, misaligned, sizes below 1, an odd or too large rot_dim, negative strides, a
  * scale that is not finite, overlap), TWEO_ERR_UNSUPPORTED (beyond these sizes).
  */
@@ -780,6 +785,7 @@ tweo_status tweo_head_norm_rotary_bwd(const tweo_heads_grad *groups, int count, 
  *   act: TWEO_ACT_SILU, g * sigmoid(g); TWEO_ACT_GELU, the tanh form g/2 (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))).
  *   A gate below -88 gives 0 (its true value is below 2^-120 of the up projection's); infinite ones what the formula does.
  *   xq [M,K], wq [2F,K] codes, K % 16 == 0; h_bf16 [M,F], F % 8 == 0; gu_bf16 [M,2F] or NULL.
+ *   M up to 2^30, 2F and K up to 2^24, M * 2F below 2^40 (as of every call below).
  * Needs no workspace.  Errors: TWEO_ERR_INVALID_ARG (null, misaligned, an unknown act, an output that overlaps anything),
  * TWEO_ERR_UNSUPPORTED (shape rules).
  */
@@ -821,7 +827,8 @@ tweo_status tweo_fp8_gated_bwd_bf16(const void *dh_bf16, const void *gu_bf16, co
  *   g, u    = (fp32( sum_k xq[m,k] wq[n,k] ) * x_step[m or 0]) * w_step[n or 0]      (exact int32 accumulation)
  *   h[m,n]  = bf16( act(g) * u )                                                     (fp32, one rounding)
  *   xq [M,K], wq [2F,K] int8; w_step: fp32 [2F] when w_step_per_channel = 1, [1] when 0; x_step [M] or [1] likewise.
- *   K % 16 == 0, F % 8 == 0; any M: one token and prompts.  Needs no workspace.
+ *   K % 16 == 0, F % 8 == 0; any M: one token and prompts.  Needs no workspace.  The sums have to fit int32, as those of K up to
+ *   131056 do whatever the codes.
  * tweo_w8a8_gated_i8out: hq [M,F] int8 = clamp( rne( act(g) * u * inv_step_h ), -127, 127 ) in its place, NaN -> 0: the down
  * projection's input under a static step, inv_step_h = 127 / s.
  * Errors as tweo_w8a8_linear_scaled, an unknown act, an output that overlaps anything, a NaN inv_step_h.
