@@ -6,7 +6,8 @@ import torch
 import paper_2511_23225_amd as tw
 from oracle import block
 from gpu_util import DEV
-from test_gpu_heads import EPS, U, bf, f64, freqs_of, near
+from test_gpu_heads import EPS, U, bf, f64, freqs_of, inputs, near
+from test_heads_sums import CASES, gain_steps
 
 pytestmark = pytest.mark.gpu
 
@@ -39,3 +40,50 @@ def test_queries_key_by_key():
             else:
                 want, size = block.rotary(x, pos.numpy()[keep], f.numpy())
             near(own[:, :, i][torch.from_numpy(keep).to(DEV)], want, (dim / 2 + 16 if norm else 8) * U * size, (norm, i))
+
+
+def grads_of(t, gains, turn, eps, tokens, heads, dim):
+    """dx and dgain, with the workspace of as many bytes as are asked for in front of others, which stay as they were."""
+    dev = lambda v: v.to(DEV)  # noqa: E731
+    need = tw.tweo_workspace_bytes(tw.TWEO_OP_HEAD_NORM_ROTARY_BWD, tokens, sum(heads), dim)
+    whole = torch.full((need + 4096,), 0xA5, dtype=torch.uint8, device=DEV)
+    dx = [torch.empty(v.shape, dtype=v.dtype, device=DEV) for v in t["x"]]
+    dgain = [torch.full((dim + 8,), 7.0, device=DEV) for _ in heads]
+    tw.tweo_head_norm_rotary_bwd([(dev(dy), dev(x), None if g is None else dev(g), o, d[:dim]) for dy, x, g, o, d in zip(t["dy"], t["x"], gains, dx, dgain)],
+                                 eps=eps, workspace=whole[:need], **turn)
+    torch.cuda.synchronize()
+    assert (whole[need:] == 0xA5).all() and all((d[dim:] == 7.0).all() for d in dgain)
+    return dx, [f64(d[:dim]) for d in dgain]
+
+
+@pytest.mark.parametrize("tokens,heads,dim,rot", CASES)
+def test_gain_gradients(tokens, heads, dim, rot):
+    """Sums over more heads than the workgroups take at a time, to the additions that a term goes through (test_heads_sums.py)."""
+    say("gain gradients", tokens, heads, dim, rot)
+    t, freqs = inputs(tokens, heads, dim, 31), freqs_of(rot)
+    layout = "pairs" if tokens % 2 else "halves"
+    turn = dict(positions=t["positions"].to(DEV), freqs=freqs.to(DEV), layout=layout, scale=1.25)
+    dx, dgain = grads_of(t, t["gain"], turn, EPS, tokens, heads, dim)
+    for i in range(len(heads)):
+        args = f64(t["dy"][i]), f64(t["x"][i]), f64(t["gain"][i]), EPS, t["positions"].numpy(), freqs.numpy(), layout, 1.25
+        want, total, size, gsize = block.head_norm_rotary_bwd(*args)
+        near(dx[i], want, (dim + 32) * U * size, (tokens, heads))
+        off = np.abs(dgain[i] - total) / (gain_steps(tokens, heads, i, dim, rot) * U * gsize)
+        say("  ", round(float(off.max()), 4))
+        assert off.max() <= 1, off.max()
+
+
+@pytest.mark.parametrize("layout", ["halves", "pairs"])
+@pytest.mark.parametrize("tokens,heads,dim,rot", [(20011, (3, 1), 64, 64), (4099, (32, 8), 128, 128), (9001, (1,), 256, 256), (2500, (2, 300), 32, 32), (3, (5000, 1), 64, 64),
+                                                  (2777, (3, 5), 512, 512), (30011, (1, 2), 32, 20), (40009, (2,), 8, 8), (50000, (1,), 64, 0), (1, (7, 1), 16, 16), (100003, (1, 1), 16, 16)])
+def test_gain_gradients_of_whole_numbers(tokens, heads, dim, rot, layout):
+    """Heads of ones and minus ones, whose norm is one to the bit (widths that are powers of two), not turned (positions of 0): the sums of whole numbers
+    below 2^24 are exact in any order, and no contribution is lost, counted twice or put elsewhere."""
+    say("whole numbers", tokens, heads, dim, rot, layout)
+    rng = np.random.default_rng(tokens)
+    t = dict(x=[bf(rng.choice([-1.0, 1.0], (tokens, h, dim))) for h in heads], dy=[bf(rng.integers(-9, 10, (tokens, h, dim))) for h in heads])
+    turn = dict(positions=torch.zeros(tokens, dtype=torch.int64, device=DEV), freqs=freqs_of(rot).to(DEV), layout=layout) if rot else {}
+    _, dgain = grads_of(t, [None] * len(heads), turn, 0.0, tokens, heads, dim)
+    for x, dy, d in zip(t["x"], t["dy"], dgain):
+        want = (f64(x) * f64(dy)).sum((0, 1))
+        assert np.abs(f64(dy)).sum((0, 1)).max() < 2 ** 24 and (d == want).all()
