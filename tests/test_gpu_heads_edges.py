@@ -87,3 +87,44 @@ def test_gain_gradients_of_whole_numbers(tokens, heads, dim, rot, layout):
     for x, dy, d in zip(t["x"], t["dy"], dgain):
         want = (f64(x) * f64(dy)).sum((0, 1))
         assert np.abs(f64(dy)).sum((0, 1)).max() < 2 ** 24 and (d == want).all()
+
+
+@pytest.mark.parametrize("dim,rot", [(64, 64), (20, 0), (98, 66), (7, 4)])
+@pytest.mark.parametrize("eps", [1e-6, 1e-30, 0.0])
+def test_gradients_of_extreme_rows(dim, rot, eps):
+    """Heads whose squares leave fp32 at either end (to the least root mean square that has an fp32 reciprocal), gradients to match; zeros, infinities and
+    NaN spoil their own head, and dgain what the formula says."""
+    say("gradients of extreme rows", dim, rot, eps)
+    rng = np.random.default_rng(11)
+    x, dy = rng.standard_normal((13, 1, dim)), rng.standard_normal((13, 1, dim))
+    x[0] *= 1e30
+    x[1] *= 1e-25
+    x[2] *= 2.0 ** 49
+    x[3] = rng.choice([-3.3e38, 3.3e38], (1, dim))
+    x[4] *= 1e-6
+    x[5] *= 1e30
+    dy[5] *= 1e28
+    x[6] *= 2.0 ** -41  # squares about the border of the second way
+    x[7] *= 1e-14
+    x[8] = rng.choice([-4e-39, 4e-39], (1, dim))
+    dy[8] *= 0.05
+    finite = 9
+    x[9] = 0.0
+    x[10, 0, dim // 2] = np.inf
+    x[11, 0, dim - 1] = np.nan
+    dy[12, 0, 0] = np.nan
+    x, dy, g = bf(x), bf(dy), bf(1 + 0.3 * rng.standard_normal(dim))
+    pos, f = torch.from_numpy(rng.integers(0, 1000, 13)), freqs_of(rot)
+
+    def both(n):
+        turn = dict(positions=pos[:n].to(DEV), freqs=f.to(DEV), layout="pairs") if rot else {}
+        dx, dgain = grads_of(dict(x=[x[:n]], dy=[dy[:n]]), [g], turn, eps, n, (1,), dim)
+        return dx[0], dgain[0], block.head_norm_rotary_bwd(f64(dy[:n]), f64(x[:n]), f64(g), float(np.float32(eps)), pos.numpy()[:n], f.numpy() if rot else None, "pairs", 1.0)
+
+    dx, dgain, (want, total, size, gsize) = both(finite)
+    assert np.isfinite(want).all() and np.abs(want).max() < 3e38
+    near(dx, want, (dim + 32) * U * size, eps)
+    assert (np.abs(dgain - total) <= gain_steps(finite, (1,), 0, dim, rot) * U * gsize).all()
+    dx, dgain, (want, total, size, gsize) = both(13)
+    near(dx, want, (dim + 32) * U * np.nan_to_num(size), eps)
+    assert (np.isnan(dgain) == np.isnan(total)).all()
