@@ -876,7 +876,8 @@ tweo_status tweo_set_gemm_tile(int variant);
  * in the call; 0: none.  kernel: a variant of tweo_set_gemm_tile; runs > 1: the contraction in so many runs, added by a second launch, on
  * variant 15, 6 or a ring variant's tiles; shared: both gradients in one launch, runs then those of the weight
  * gradient and kernel that of the input gradient's tiles (15, 16: the deferred-epilogue kernel); backward without it: kernel and
- * runs of the weight gradient.  Returns TWEO_ERR_INVALID_ARG for a null plan or sizes below 1, TWEO_ERR_UNSUPPORTED for another op.
+ * runs of the weight gradient.  op TWEO_OP_FP8_GATED_FWD_BF16: the gated feed-forward's product (M, N = F, K), residual non-zero: both
+ * projections are kept; the rest is ignored.  Returns TWEO_ERR_INVALID_ARG for a null plan or sizes below 1, TWEO_ERR_UNSUPPORTED for another op.
  */
 typedef struct tweo_gemm_plan_info {
     int kernel, runs, shared;

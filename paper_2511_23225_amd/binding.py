@@ -248,7 +248,8 @@ def tweo_set_stream_k(on):
 
 
 def tweo_gemm_plan(op, M, N, K, p=0, residual=False, workspace_bytes=0):
-    """(kernel variant, runs of the contraction, both gradients in one launch) of an FP8 call of these sizes."""
+    """(kernel variant, runs of the contraction, both gradients in one launch) of an FP8 call of these sizes.  The gated feed-forward's product:
+    N = F, residual: both projections are kept."""
     plan = GemmPlan()
     _check(load().tweo_gemm_plan(op, M, N, K, p, 1 if residual else 0, workspace_bytes, ctypes.byref(plan)), "tweo_gemm_plan")
     return plan.kernel, plan.runs, bool(plan.shared)

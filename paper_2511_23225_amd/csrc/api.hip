@@ -175,6 +175,12 @@ tweo_status tweo_gemm_plan(int op, int64_t M, int64_t N, int64_t K, int p, int r
 {
     if (plan == nullptr || M <= 0 || N <= 0 || K <= 0)
         return TWEO_ERR_INVALID_ARG;
+    if (op == TWEO_OP_FP8_GATED_FWD_BF16) {
+        if (N > kMaxCols || !dims_ok(M, 2 * N, K))
+            return TWEO_ERR_UNSUPPORTED;
+        *plan = tweo_gemm_plan_info{fp8_gated_variant(M, N, K, residual != 0), 1, 0};
+        return TWEO_OK;
+    }
     if ((op != TWEO_OP_FP8_LINEAR_FWD && op != TWEO_OP_FP8_LINEAR_BWD) || !dims_ok(M, N, K))
         return TWEO_ERR_UNSUPPORTED;
     // an address for what is there; nothing reads it

@@ -16,6 +16,7 @@ typedef TileR<64, 128, 2, 2, 2, 6> G64x128g2;
 typedef TileR<128, 128, 2, 2, 1, 2> G128x128x2;
 
 enum GatedShape { kGated64x64, kGated64x64g2, kGated64x128, kGated64x128g2, kGated128x128x2, kGated256, kGated192, kGatedShapes };
+static const int kGatedVariant[kGatedShapes] = {4, 18, 19, 20, 21, 15, 24};  // as tweo_set_gemm_tile counts them
 
 int gated_workgroups(int64_t M, int64_t F, int bm)
 {
@@ -137,10 +138,9 @@ static int pick_shape(int64_t M, int64_t F, int64_t K, bool int8, bool keep)
     int best = kGated64x64;
     double least = 1e300;
     for (int i = 0; i < kGatedShapes; ++i) {
-        static const int variant[kGatedShapes] = {4, 18, 19, 20, 21, 15, 24};
         if (!shape_fits(i, M, F, K, int8))
             continue;
-        if (variant[i] == forced)
+        if (kGatedVariant[i] == forced)
             return i;
         const GatedRate &r = (int8 ? kInt8Rates : kFp8Rates)[i];
         const int64_t tiles = ((M + r.bm - 1) / r.bm) * ((2 * F + r.bn - 1) / r.bn), slots = r.per_cu * cus;
@@ -154,6 +154,8 @@ static int pick_shape(int64_t M, int64_t F, int64_t K, bool int8, bool keep)
     }
     return best;
 }
+
+int fp8_gated_variant(int64_t M, int64_t F, int64_t K, bool keep) { return kGatedVariant[pick_shape(M, F, K, false, keep)]; }
 
 hipError_t launch_fp8_gated(const GemmArgs &a, bool gelu, void *gu, hipStream_t s)
 {

@@ -219,6 +219,7 @@ struct GateCoef {
     float c0, c1;
 };
 hipError_t launch_fp8_gated(const GemmArgs &a, bool gelu, void *gu, hipStream_t s);
+int fp8_gated_variant(int64_t M, int64_t F, int64_t K, bool keep);  // the kernel it runs on, as tweo_set_gemm_tile counts them
 hipError_t launch_i8_gated(const GemmArgs &a, bool gelu, hipStream_t s);
 // Its gradients by gate and up projection, bf16 (dg | du) [M, 2F], cast without being stored (gated.hip); M % 16 == 0, F % 8 == 0.
 struct GatedGradCall {

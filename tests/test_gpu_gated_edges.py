@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import paper_2511_23225_amd as tw
+from oracle import block
 from gpu_util import DEV
 
 pytestmark = pytest.mark.gpu
@@ -107,3 +108,32 @@ def test_int8_forward_of_most_rows(F, i8):
         assert ((got - (want * 20.0).clamp(-127, 127)).abs() <= 0.5 + 20.0 * fp32).all()
     else:
         assert ((got - want).abs() <= 2.0 ** -8 * want.abs() + fp32 + 2.0 ** -134).all()
+
+
+@pytest.mark.parametrize("M,K,F", [(1, 272, 136), (70, 144, 40), (130, 1040, 264), (300, 400, 200), (257, 4112, 328)])
+def test_int8_forward_on(M, K, F):
+    """The kernels that an INT8 call may run on, forced: their sums are exact, so that all give the same bits, and those of fp64 but for the fp32 part."""
+    say("w8a8 gated on", M, K, F)
+    rng = np.random.default_rng(M + K)
+    xq, wq = (torch.from_numpy(rng.integers(-127, 128, s, dtype=np.int8)) for s in ((M, K), (2 * F, K)))
+    xs, ws = (torch.from_numpy(rng.uniform(0.5, 2.0, n).astype(np.float32)) * c for n, c in ((M, 1 / 127), (2 * F, 0.03 / K ** 0.5)))
+    outs = []
+    for variant in (0, 4, 18, 19, 20, 21):
+        h, hq = b16(M + 1, F).fill_(7), torch.full((M + 1, F), 7, dtype=torch.int8, device=DEV)
+        tw.tweo_set_gemm_tile(variant)
+        try:
+            tw.tweo_w8a8_gated(xq.to(DEV), wq.to(DEV), xs.to(DEV), ws.to(DEV), h[:M], act="gelu")
+            tw.tweo_w8a8_gated_i8out(xq.to(DEV), wq.to(DEV), xs.to(DEV), ws.to(DEV), 30.0, hq[:M], act="gelu")
+        finally:
+            tw.tweo_set_gemm_tile(0)
+        torch.cuda.synchronize()
+        assert (h[M:] == 7).all() and (hq[M:] == 7).all()
+        outs.append((h.view(torch.int16), hq))
+    assert all(torch.equal(a, b) for o in outs for a, b in zip(o, outs[0]))
+    p = ((xq.double() @ wq.double().t()).float() * xs[:, None] * ws).double()
+    g, u = p[:, :F].numpy(), p[:, F:].numpy()
+    want = block.activation(g, "gelu") * u
+    z = np.minimum(np.abs(block.gate_argument(g, "gelu")[0]), 130.0)
+    fp32 = (z + 8) * 2.0 ** -22 * np.abs(want) + np.where(g < -5, 90 * 2.0 ** -115, 0) * np.abs(u)
+    assert (np.abs(outs[0][0][:M].view(torch.bfloat16).double().cpu().numpy() - want) <= 2.0 ** -8 * np.abs(want) + fp32 + 2.0 ** -134).all()
+    assert (np.abs(outs[0][1][:M].double().cpu().numpy() - np.clip(want * 30.0, -127, 127)) <= 0.5 + 30.0 * (fp32 + 2.0 ** -24 * np.abs(want))).all()
