@@ -12,7 +12,8 @@ static inline GateCoef gate_coef(bool gelu)
     return gelu ? GateCoef{(float)(k * log2e), (float)(k * 0.044715 * log2e)} : GateCoef{(float)log2e, 0.0f};
 }
 
-// The base-2 exponential and the reciprocal are the hardware's, 1 step each; z loses 2 more, so p is within |z| 2^-23 + 2^-22 of
+// z is within e |z| of itself: e = 2^-23 for SiLU (the constant's rounding and the product's), 2^-22 for GELU (those of both constants, the square, the
+// sum and the product).  The base-2 exponential and the reciprocal are the hardware's, 1 step each, so p is within e |z| + 2^-21 of
 // itself.  A g that would square to infinity (0 times that is NaN) counts as 2^60.  Below p = 2^-128 (g under -88) p is 0.
 __device__ __forceinline__ float gate_share(float g, const GateCoef &c)
 {
@@ -32,7 +33,8 @@ __device__ __forceinline__ float gate_exp(float g, const GateCoef &c)
     return __builtin_amdgcn_exp2f(-(g * c.c0));
 }
 
-// The share with the sum's rounding and the reciprocal's taken back, where memory leaves time for it: p is within |z| 2^-23 (1 - p) + 2^-24 of itself.
+// The share with the sum's rounding and the reciprocal's taken back, where memory leaves time for it: p is within (e |z| + 2^-22) (1 - p) and the
+// half step of its own rounding, 2^-24, of itself.
 // (Beyond what the reciprocal of a number gives the correction is not one, and times 0.)
 template <bool GELU>
 __device__ __forceinline__ float gate_share_near(float g, const GateCoef &c)
