@@ -272,7 +272,7 @@ struct DeferEnd {
 // GATE (FP8): 1 SiLU, 2 GELU: g.N columns of the gated feed-forward.  A tile holds 128 of them: its B's pieces are 64 rows of the gate and the same
 // 64 of the up projection in turn, so that a wave's first pair of blocks is the gate's and its second the up projection's, lane by lane the
 // same elements.  They are rounded to bf16 as in a plain product; the product of a band is formed from its two pairs behind their exchanges.
-// KEEP: both are stored (gd.gu).  16384 x 2 x 5632 under 2048, both stored: 283-296 us, 2.55-2.67 PFLOP/s, as the plain product of that size
+// KEEP: both are stored (gd.gu).  16384 x 2 x 5632 under 2048, both stored: 289-308 us, 2.45-2.61 PFLOP/s, as the plain product of that size
 // (the ring kernel's 128x128 tiles 469); bound by its matrix instructions at the clock that they leave.
 template <bool INT8, int PMODE, int D, int MT, bool A_E5M2, bool KSPLIT, int RES, bool RAGGED, bool ANY, int GATE, bool KEEP, typename WORK, typename BETWEEN>
 __device__ __forceinline__ void defer_tiles(const GemmDev &g, const WORK &work, bool opened, BETWEEN between, float &pen, const GatedDev &gd = GatedDev{})

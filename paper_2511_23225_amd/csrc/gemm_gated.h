@@ -6,7 +6,8 @@
 // projection's for odd.  A lane (l31, lh) of the MFMA layout has places 8q + 4lh + r in its registers 4q + r: gate and up of one
 // column are four registers apart.  The rows that a wave brings into LDS, eight at a time, are all of one kind (an even number of
 // waves goes round them), so that its base address alone says which.  One row of tokens is bound by the weights (90 MB of INT8: 16 us, 5.7 TB/s),
-// 2048 by the matrix instructions between two barriers a stage (11008 columns under 4096, INT8: 200 us, 1.84 POP/s, of 5.4 rounds of tiles).
+// 2048 by the matrix instructions between two barriers a stage (11008 columns under 4096, INT8: 200 us, 1.85 POP/s, of 5.4 rounds of tiles; 4096 rows
+// 370, 2.0 POP/s).
 #pragma once
 #include "gemm_common.h"
 #include "activation.h"

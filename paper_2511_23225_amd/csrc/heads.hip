@@ -8,8 +8,8 @@
 //
 // A head belongs to a team of 1 to 32 lanes (a power of two, 16 values each) that hold both members of a pair in one lane, in 16-byte pieces, which
 // overlap where width and turned part are no whole ones.  The angles of a workgroup's tokens are worked out once, one a thread, into LDS and serve
-// all heads; nothing else is shared, so memory bounds the large calls: 16384 tokens of 32 heads of 128, rotation 50.5 us (5.3 TB/s, a copy's
-// rate), 64 of 64, norm 55 and gradients 81.5 (78.5 and the joining of dgain's rows).
+// all heads; nothing else is shared, so memory bounds the large calls: 16384 tokens of 32 heads of 128, rotation 49 us (5.5 TB/s, a copy's
+// rate and more), 64 of 64, norm 55 and gradients 81.5 (78.5 and the joining of dgain's rows).
 #include <algorithm>
 #include <type_traits>
 #include "device_utils.h"
